@@ -18,6 +18,13 @@
  *   msa_sparse_attn_backward training: Main Branch gradients dQ, dK, dV
  *   msa_sparse_kl_backward   training: sparse KL loss and its index-projection gradients
  *
+ * and what a layer needs around them:
+ *
+ *   msa_qk_norm_rope(_fp8)   RMS norm of each query and key head and the rotation by position
+ *   msa_qk_norm_rope_backward   its gradients
+ *   msa_kv_append(_fp8)      new keys, values and index keys into the (paged) cache
+ *   msa_dense_attn_paged(_fp8)   dense causal attention over a paged cache
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Every tensor argument is a DEVICE pointer to contiguous row-major memory
@@ -70,7 +77,9 @@
  * page_size.  Page ids outside [0, total_kv_rows /
  * page_size) are clamped into it (results unspecified, memory safe).  This
  * is a serving layout, not part of the paper.  Every call accepts it except
- * msa_dense_attn, which returns MSA_ERR_UNSUPPORTED for a paged layout; the
+ * msa_dense_attn, which returns MSA_ERR_UNSUPPORTED for a paged layout
+ * (msa_dense_attn_paged takes it; that call and msa_kv_append, which have no
+ * block size, accept any power of two from 16 to 8192 as page_size); the
  * training calls then write dK, dV and d index_k in the pool's rows (rows of
  * pages no sequence lists get zero; keys in pages shared by several
  * sequences get the sum of their gradients).
@@ -291,6 +300,167 @@ size_t msa_dense_attn_workspace_size(const msa_seqs* seqs, int num_q_heads, int 
 int msa_dense_attn(const void* q, const void* k, const void* v, const msa_seqs* seqs,
                    int num_q_heads, int num_kv_heads, int head_dim, float softmax_scale, void* o,
                    float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * msa_dense_attn_paged / msa_dense_attn_paged_fp8 -- dense causal GQA attention
+ * of each sequence's new rows over its paged keys: the layers and phases
+ * without block selection, on the cache that the sparse calls read.
+ *
+ * Arguments, layouts, outputs and errors are those of msa_dense_attn (and, for
+ * E4M3, the codes and scales of msa_sparse_attn_prefill_fp8), with a paged
+ * seqs: block_table != NULL, page_size a power of two from 16 to 8192 (a
+ * contiguous key side returns MSA_ERR_UNSUPPORTED).  Any number of new rows per
+ * sequence, from one (decode) to a whole prompt, mixed in a batch.  A row
+ * without a visible key gets O = 0 and LSE = -inf; rows of o and lse behind the
+ * last sequence are left as they are.  What the cache holds behind a sequence's
+ * last key (the rest of its last page, other pages) does not matter, NaN
+ * included; a NaN or infinity among a sequence's own new keys may reach rows
+ * before it.  How keys are split over the chip follows the sizes in seqs and
+ * the lengths on the device: a result is bit-reproducible for equal inputs.
+ *
+ * Supported: head_dim == 128; 1 <= num_q_heads / num_kv_heads <= 16;
+ * num_kv_heads <= 64; total_kv_rows < 2^35.
+ * ------------------------------------------------------------------------ */
+size_t msa_dense_attn_paged_workspace_size(const msa_seqs* seqs, int num_q_heads, int num_kv_heads,
+                                           int head_dim);
+int msa_dense_attn_paged(const void* q, const void* k, const void* v, const msa_seqs* seqs,
+                         int num_q_heads, int num_kv_heads, int head_dim, float softmax_scale,
+                         void* o, float* lse, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+int msa_dense_attn_paged_fp8(const void* q, const void* k, const void* v, float q_scale,
+                             float k_scale, float v_scale, const msa_seqs* seqs, int num_q_heads,
+                             int num_kv_heads, int head_dim, float softmax_scale, void* o,
+                             float* lse, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Rotation by position (struct msa_rope)
+ *
+ * The first rot_dim elements of a head are turned in pairs: pair i, at position
+ * p, by the angle p * inv_freq[i], cosine and sine both times `scale`; the rest
+ * of the head passes unchanged.  Pair i is elements (i, i + rot_dim / 2), or,
+ * interleaved, (2i, 2i + 1):
+ *     y_a = x_a cos - x_b sin,  y_b = x_b cos + x_a sin.
+ * Frequencies are the caller's, so that every scaling for long contexts is a
+ * choice of them (and of `scale`).  Angles are formed in 64 bits.  rot_dim == 0
+ * (or a NULL msa_rope) is no rotation.
+ *
+ * Supported: rot_dim a multiple of 8, at most the head's size; scale finite.
+ * ------------------------------------------------------------------------ */
+typedef struct msa_rope {
+  int32_t rot_dim;          /* host */
+  int32_t interleaved;      /* host: 0 = pairs (i, i + rot_dim / 2), else (2i, 2i + 1) */
+  float scale;              /* host: factor of cosine and sine, 1 if none */
+  const double* inv_freq;   /* device [rot_dim / 2]: radians per position */
+} msa_rope;
+
+/* ------------------------------------------------------------------------
+ * msa_qk_norm_rope / msa_qk_norm_rope_fp8 -- RMS norm of each head of the new
+ * rows' queries and keys, and their rotation, in one pass:
+ *     n = x / sqrt(mean(x^2) + eps) * weight  over each head's head_dim elements,
+ *     y = rotation of n by the row's position (Sequence layout above).
+ * A NULL weight leaves that tensor without the norm (the rotation alone).
+ * Queries and keys of the Main Branch, or index queries and index keys.
+ *
+ *   q      bf16 rows [total_q_rows], q_stride elements apart, each num_q_heads
+ *          heads of head_dim, e.g. columns of a joint projection's output
+ *   k      bf16 rows [total_q_rows], k_stride apart, num_kv_heads heads
+ *   q_weight, k_weight   fp32 [head_dim], or NULL
+ *   q_out  bf16 (fp8: E4M3 codes of y / q_scale, to nearest even, at most 448 in
+ *          size) [total_q_rows, num_q_heads, head_dim] contiguous   OUTPUT
+ *   k_out  the same with num_kv_heads, k_scale                      OUTPUT
+ *
+ * Either tensor is left out with 0 heads.  fp32 in between, one rounding.  The
+ * bf16 outputs may be the inputs themselves where those are contiguous; other
+ * overlaps are not allowed.  Rows behind the last sequence are left as they are.
+ * With eps 0 a head of zeros gives NaN; sums of squares beyond fp32 (elements
+ * of about 2^60) give 0.  No workspace.
+ *
+ * Supported: head_dim 64 or 128; up to 1024 heads each; strides a multiple of 4
+ * elements, tensors 8-byte aligned (else MSA_ERR_UNSUPPORTED).
+ * ------------------------------------------------------------------------ */
+int msa_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                     const msa_seqs* seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                     const float* q_weight, const float* k_weight, float eps,
+                     const msa_rope* rope, void* q_out, void* k_out, hipStream_t stream);
+int msa_qk_norm_rope_fp8(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         float q_scale, float k_scale, const msa_seqs* seqs, int num_q_heads,
+                         int num_kv_heads, int head_dim, const float* q_weight,
+                         const float* k_weight, float eps, const msa_rope* rope, void* q_out,
+                         void* k_out, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * msa_qk_norm_rope_backward -- gradients of msa_qk_norm_rope.
+ *
+ * For upstream gradients g of q_out and k_out, h = g turned back (the transposed
+ * rotation, times the same scale) and u = x / sqrt(mean(x^2) + eps):
+ *     d weight = sum over rows and heads of h * u,
+ *     d x      = (h * weight - u * mean(h * weight * u)) / sqrt(mean(x^2) + eps);
+ * without the norm d x = h.
+ *
+ *   q, k, weights, eps, rope   as passed to the forward call (q or k of a tensor
+ *              without weight is not read and may be NULL)
+ *   d_q_out, d_k_out   bf16, contiguous, as the outputs
+ *   d_q, d_k   bf16 rows d_q_stride / d_k_stride elements apart   OUTPUT (each may
+ *              be the contiguous gradient it is formed from)
+ *   d_q_weight, d_k_weight   fp32 [head_dim]   OUTPUT, or NULL to skip; written,
+ *              not added to
+ *
+ * fp32 in between.  Every output is bit-reproducible: the weight gradients add
+ * rows in an order that the sizes fix.  Rows behind the last sequence are left
+ * as they are and take no part.  The workspace is needed where a weight is given.
+ * Supported sizes as for msa_qk_norm_rope.
+ * ------------------------------------------------------------------------ */
+size_t msa_qk_norm_rope_backward_workspace_size(const msa_seqs* seqs, int num_q_heads,
+                                                int num_kv_heads, int head_dim);
+int msa_qk_norm_rope_backward(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              const void* d_q_out, const void* d_k_out, const msa_seqs* seqs,
+                              int num_q_heads, int num_kv_heads, int head_dim,
+                              const float* q_weight, const float* k_weight, float eps,
+                              const msa_rope* rope, void* d_q, int64_t d_q_stride, void* d_k,
+                              int64_t d_k_stride, float* d_q_weight, float* d_k_weight,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * msa_kv_append / msa_kv_append_fp8 -- the new rows' keys, values and index keys
+ * into the cache, keys and index keys with norm and rotation on the way.
+ *
+ * Row t of sequence s goes to the cache row of its position (Sequence layout
+ * above; kv_lens count the new rows already): kv_starts[s] + p, or its row in
+ * the page that the block table lists.  A row whose page id lies outside the
+ * pool (a table filled with -1, say) or whose position lies outside the cache
+ * is not stored; nothing else in the cache is written.  Cache rows must not be
+ * shared between new rows (two sequences listing the same page for new
+ * positions): what such a row holds is unspecified.
+ *
+ *   k, v       bf16 rows [total_q_rows], k_stride / v_stride elements apart, each
+ *              num_kv_heads heads of head_dim
+ *   index_k    bf16 rows, index_k_stride apart, of d_idx elements; NULL together
+ *              with index_k_cache: no index keys (d_idx, its stride, weight and
+ *              rope are then ignored)
+ *   k_weight, index_k_weight, eps, rope, index_rope   as in msa_qk_norm_rope
+ *   k_cache, v_cache   bf16 (fp8: E4M3 codes of y / k_scale and v / v_scale, to
+ *              nearest even, at most 448 in size)
+ *              [total_kv_rows, num_kv_heads, head_dim]   UPDATED
+ *   index_k_cache      bf16 [total_kv_rows, d_idx]        UPDATED
+ *
+ * Values are stored as they are (bf16) or as codes.  No workspace.
+ * Supported: head_dim == 128; num_kv_heads <= 64; d_idx 64 or 128; contiguous, or
+ * pages of a power of two from 16 to 8192 rows; strides and alignment as for
+ * msa_qk_norm_rope.
+ * ------------------------------------------------------------------------ */
+int msa_kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  const void* index_k, int64_t index_k_stride, const msa_seqs* seqs,
+                  int num_kv_heads, int head_dim, int d_idx, const float* k_weight,
+                  const float* index_k_weight, float eps, const msa_rope* rope,
+                  const msa_rope* index_rope, void* k_cache, void* v_cache, void* index_k_cache,
+                  hipStream_t stream);
+int msa_kv_append_fp8(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                      float k_scale, float v_scale, const void* index_k, int64_t index_k_stride,
+                      const msa_seqs* seqs, int num_kv_heads, int head_dim, int d_idx,
+                      const float* k_weight, const float* index_k_weight, float eps,
+                      const msa_rope* rope, const msa_rope* index_rope, void* k_cache,
+                      void* v_cache, void* index_k_cache, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * msa_sparse_attn_backward -- training backward of the Main Branch.

@@ -508,3 +508,43 @@ def sparse_kl(index_q_bits, index_k_bits, q_bits, k_bits, block_ids: np.ndarray,
                                               scale_idx, scale_main)
             d_ik[kv0 + toks] += dk
     return kl, d_iq, d_ik
+
+
+# --------------------------------------------------------------------------
+# Norm of each head, rotation by position, E4M3 rounding
+# --------------------------------------------------------------------------
+def rotation_matrix(angles: np.ndarray, dim: int, interleaved: bool, scale: float) -> np.ndarray:
+    """The dim x dim matrix that turns the pairs of one head: pair i of the first
+    2 len(angles) elements by angles[i], times scale; the identity on the rest."""
+    n = len(angles)
+    R = np.eye(dim)
+    for i, a in enumerate(angles):
+        x, y = (2 * i, 2 * i + 1) if interleaved else (i, i + n)
+        R[x, x], R[x, y] = scale * math.cos(a), -scale * math.sin(a)
+        R[y, x], R[y, y] = scale * math.sin(a), scale * math.cos(a)
+    return R
+
+
+def norm_rope(x: np.ndarray, positions: Sequence[int], weight: Optional[np.ndarray], eps: float, inv_freq: np.ndarray,
+              interleaved: bool = False, scale: float = 1.0) -> np.ndarray:
+    """Rows [T, H, D] (float64): each head divided by its root mean square, times
+    weight (both skipped without weight), then turned by its row's position."""
+    x = np.asarray(x, dtype=np.float64)
+    if weight is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * weight
+    return np.stack([x[t] @ rotation_matrix(p * np.asarray(inv_freq, dtype=np.float64), x.shape[-1], interleaved, scale).T
+                     for t, p in enumerate(positions)]) if len(positions) else x
+
+
+def norm_rope_backward(x: np.ndarray, g: np.ndarray, positions: Sequence[int], weight: Optional[np.ndarray], eps: float,
+                       inv_freq: np.ndarray, interleaved: bool = False, scale: float = 1.0):
+    """(d x, d weight or None) of sum(g * norm_rope(x))."""
+    x = np.asarray(x, dtype=np.float64)
+    h = np.stack([g[t] @ rotation_matrix(p * np.asarray(inv_freq, dtype=np.float64), x.shape[-1], interleaved, scale)
+                  for t, p in enumerate(positions)])
+    if weight is None:
+        return h, None
+    rms = np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    u = x / rms
+    hw = h * weight
+    return (hw - u * (hw * u).mean(-1, keepdims=True)) / rms, (h * u).sum((0, 1))

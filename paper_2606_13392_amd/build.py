@@ -13,7 +13,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmsa.so")
 SOURCES = ["index_topk.hip", "sparse_attn.hip", "sparse_attn_prefill.hip", "sparse_attn_tile.hip",
            "sparse_attn_backward.hip",
-           "sparse_kl_backward.hip", "dense_attn.hip",
+           "sparse_kl_backward.hip", "dense_attn.hip", "dense_attn_paged.hip", "norm_rope.hip",
            "msa_profile.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

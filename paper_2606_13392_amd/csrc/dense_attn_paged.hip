@@ -1,0 +1,498 @@
+// Dense causal GQA attention of new rows over a paged key / value cache on
+// gfx950: a chunk of a prompt behind a cached context, a few draft rows, or
+// one token per sequence; bf16 or E4M3.
+//
+// A CTA owns one KV group and a tile of consecutive query rows of one sequence
+// (each of its 1, 2, 4 or 8 waves holds 32 (query row, head) rows) and streams
+// the sequence's keys, 64 at a time, through a double-buffered LDS ring one
+// sub-block ahead: S^T = K Q^T and O^T += V^T P^T on MFMA 32x32x16, the online
+// softmax of one sub-block between the O MFMAs of the one before (running
+// maximum and sum per row in registers, fp32).  The layout of a sub-block in
+// LDS and the transposing reads are those of flash_tile.h.
+//
+// Pages: 16 .. 8192 rows, a power of two.  Each lane holds the place of one
+// unit of min(page, 64) rows of the sequence, so 64 units' page ids arrive
+// with one load, a window ahead of their use, and a copy's scalar base comes
+// from a lane read.  Rows past the end of the sequence are never read.
+#include "flash_tile.h"
+
+namespace {
+
+using namespace msa;
+using flash::add_bf16_pair;
+using flash::dma16;
+using flash::kAhead;
+using flash::kDim;
+using flash::kLn_2;
+using flash::kLog2E;
+using flash::kSub;
+using flash::k_seg;
+using flash::lds_tr4;
+using flash::Ring;
+using flash::v_seg;
+using flash::xor32f;
+
+// Places of a sequence's key rows in the pool, in units of min(page, 64) rows:
+// a window of 64 units and the one behind it, one unit per lane.
+struct PageWindow {
+  const int32_t* table;                  // the sequence's block-table row
+  int lg_unit, lg_page;
+  int units;                             // units of the sequence
+  int64_t max_page;
+  int w0;                                // first unit of `cur`
+  uint32_t cur, nxt;                     // first row of the lane's unit / 16
+
+  __device__ __forceinline__ uint32_t fetch(int unit) const {
+    const int u = min(unit, units - 1);
+    const int key = u << lg_unit;
+    int64_t page = table[key >> lg_page];
+    page = page < 0 ? 0 : (page > max_page ? max_page : page);
+    return static_cast<uint32_t>(((page << lg_page) + (key & ((1 << lg_page) - 1))) >> 4);
+  }
+  __device__ __forceinline__ void start(int unit) {
+    w0 = unit;
+    cur = fetch(w0 + lane_id());
+    nxt = fetch(w0 + kWave + lane_id());
+  }
+  // to be called before units from `unit` on are asked for
+  __device__ __forceinline__ void advance(int unit) {
+    if (unit - w0 >= kWave) {
+      w0 += kWave;
+      cur = nxt;
+      nxt = fetch(w0 + kWave + lane_id());
+    }
+  }
+  // first row of a unit at most 127 past w0: the same unit in every lane
+  __device__ __forceinline__ int64_t row(int unit) const {
+    const int i = unit - w0;
+    const uint32_t x = i < kWave ? __builtin_amdgcn_readlane(cur, i) : __builtin_amdgcn_readlane(nxt, i - kWave);
+    return static_cast<int64_t>(x) << 4;
+  }
+  // a key's row, each lane its own
+  __device__ __forceinline__ int64_t key_row(int key) const {
+    const int i = (key >> lg_unit) - w0;
+    const uint32_t a = __shfl(static_cast<int>(cur), i & 63), b = __shfl(static_cast<int>(nxt), i & 63);
+    return (static_cast<int64_t>(i < kWave ? a : b) << 4) + (key & ((1 << lg_unit) - 1));
+  }
+};
+
+// T: uint16_t = bf16 bits, uint8_t = E4M3 codes (o_scale multiplies O).
+template <typename T, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, msa_seqs sq, flash::Grid gr, int H_q,
+    int H_kv, float scale_log2, uint32_t q_flip, float o_scale, uint16_t* __restrict__ o, float* __restrict__ lse) {
+  constexpr int kThreads = WAVES * kWave;
+  constexpr int MT = kSub / 32;            // 32-key tiles of S^T
+  constexpr int KS = kDim / 16;            // k-steps of S^T = K Q^T
+  constexpr bool kDma = sizeof(T) == 2;
+  constexpr int NDMA = kSub / 4 / WAVES;   // DMA instructions per wave per sub-block and tensor
+  constexpr int NRAW = kSub * kDim / 16 / kThreads;   // E4M3: 16-byte pieces per thread and tensor
+  __shared__ __align__(16) Ring ring;
+  const int lane = lane_id();
+  const int wave = threadIdx.x / kWave;
+  const int n = lane & 31, h = lane >> 5;
+  const int G = H_q / H_kv;
+  const int qpw = 32 / G;                  // query rows per wave
+  const int qt = WAVES * qpw;              // query rows per CTA
+  const int jq = n / G, hh = n % G;
+  const int r = static_cast<int>(blockIdx.x % H_kv);
+  int s, tile;
+  flash::locate_tile(sq, gr, static_cast<int>(blockIdx.x / H_kv), qt, &s, &tile);
+  const SeqGeom g = seq_geom(sq, s);
+  const int t0 = tile * qt;
+  const int base_p = g.kv_len - g.q_rows;  // position of the sequence's first query row
+  int t_end = min(t0 + qt, g.q_rows);
+  t_end = static_cast<int>(min(static_cast<int64_t>(t_end), sq.total_q_rows - g.q_begin));
+  if (t_end <= t0) return;                                // uniform over the CTA
+  const int p_last = base_p + t_end - 1;
+  const int t = t0 + wave * qpw + jq;                     // this lane's query row in the sequence
+  const bool valid = n < qpw * G && t < t_end;
+  const int p = valid ? base_p + t : -1;
+  const bool live = t0 + wave * qpw < t_end;              // the wave has rows
+  // sub-blocks below nfree are visible to every row of the wave and need no mask
+  const int nfree = (base_p + min(t0 + wave * qpw, t_end - 1) + 1) / kSub;
+  const int64_t head_row = (static_cast<int64_t>(g.q_begin) + (valid ? t : t0)) * H_q + static_cast<int64_t>(r) * G + hh;
+  const int b_begin = 0, b_end = p_last < 0 ? 0 : p_last / kSub + 1;
+
+  Raw<T> rq[KS];
+  {
+    const T* qrow = q + head_row * kDim + 8 * h;
+#pragma unroll
+    for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
+  }
+
+  const int64_t stride = static_cast<int64_t>(H_kv) * kDim;
+  const char* kb = reinterpret_cast<const char*>(k + static_cast<int64_t>(r) * kDim);
+  const char* vb = reinterpret_cast<const char*>(v + static_cast<int64_t>(r) * kDim);
+  const uint32_t stride_b = static_cast<uint32_t>(stride * sizeof(T));
+  PageWindow pw;
+  pw.table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
+  pw.lg_page = 31 - __clz(sq.page_size);
+  pw.lg_unit = min(pw.lg_page, 6);
+  pw.max_page = (sq.total_kv_rows >> pw.lg_page) - 1;
+  pw.units = ((g.kv_len - 1) >> pw.lg_unit) + 1;
+  const int lg_sub = 6 - pw.lg_unit;       // log2 of units per sub-block
+
+  flash::LaneOffsets<NDMA> lo;
+  {
+    const int gq = lane >> 4, jj = lane & 15;
+#pragma unroll
+    for (int c = 0; c < NDMA; ++c) {
+      const int ra = 4 * (c * WAVES + wave) + gq;
+      lo.kg[c] = ra * stride_b + 16 * k_seg(ra, jj);        // the permutations are involutions
+      lo.vg[c] = ra * stride_b + 16 * v_seg(ra, jj);
+    }
+#pragma unroll
+    for (int st = 0; st < KS; ++st) lo.ks[st] = 2 * (n * kDim + 8 * k_seg(n, 2 * st + h));
+    const int rl = 4 * h + (jj >> 2);
+#pragma unroll
+    for (int td = 0; td < kDim / 32; ++td) {
+      const int col = 32 * td + 16 * (gq & 1) + 4 * (jj & 3);
+      lo.vs[td] = 2 * (rl * kDim + 8 * v_seg(rl, col >> 3) + (col & 7));
+    }
+  }
+  // First byte of the rows of a sub-block, as seen from row `first` of it (the
+  // unit that `first` lies in): base of offsets row * stride_b.
+  auto base_of = [&](const char* base, int sub, int first) -> const char* {
+    const int unit = (sub << lg_sub) + (first >> pw.lg_unit);
+    const int64_t row0 = pw.row(unit) - ((first >> pw.lg_unit) << pw.lg_unit);
+    return base + row0 * stride_b;
+  };
+  // One sub-block (K or V) into LDS by DMA: each wave instruction fills 4 rows
+  // (1 KiB); lane l takes row 4 piece + l / 16 and the logical segment that the
+  // row's permutation stores at physical segment l % 16.  In a sub-block running
+  // past kv_len the missing rows re-read the last key (finite values whose
+  // scores are masked).
+  auto dma = [&](const char* base, const uint32_t (&go)[NDMA], bool is_v, int sub, uint16_t* dst) {
+    const int key0 = sub * kSub;
+    if (key0 + kSub <= g.kv_len) {
+      const char* blk = base_of(base, sub, 0);
+#pragma unroll
+      for (int c = 0; c < NDMA; ++c) {
+        const int first = 4 * (c * WAVES + wave);
+        if (lg_sub != 0) blk = base_of(base, sub, __builtin_amdgcn_readfirstlane(first));
+        dma16(blk + go[c], dst + first * kDim);
+      }
+    } else {
+#pragma unroll 1
+      for (int c = 0; c < NDMA; ++c) {
+        const int ra = 4 * (c * WAVES + wave) + (lane >> 4);
+        const int64_t row = pw.key_row(min(key0 + ra, g.kv_len - 1));
+        const int seg = is_v ? v_seg(ra, lane & 15) : k_seg(ra, lane & 15);
+        dma16(base + row * stride_b + 16 * seg, dst + 4 * (c * WAVES + wave) * kDim);
+      }
+    }
+  };
+  // The same through registers for E4M3: whole 128-byte rows, 16 codes per
+  // lane; stored widened to bf16.
+  u32x4 rk[NRAW], rv[NRAW];
+  auto fetch = [&](const char* base, int sub, u32x4 (&dst)[NRAW]) {
+    const int key0 = sub * kSub;
+#pragma unroll
+    for (int i = 0; i < NRAW; ++i) {
+      const int c = threadIdx.x + kThreads * i;
+      const char* src;
+      if (key0 + kSub <= g.kv_len) {
+        src = base_of(base, sub, __builtin_amdgcn_readfirstlane(c >> 3)) + (c >> 3) * stride_b;
+      } else {
+        src = base + pw.key_row(min(key0 + (c >> 3), g.kv_len - 1)) * stride_b;
+      }
+      dst[i] = *reinterpret_cast<const u32x4*>(src + 16 * (c & 7));
+    }
+  };
+  auto store = [&](const u32x4 (&src)[NRAW], bool is_v, uint16_t* dst) {
+#pragma unroll
+    for (int i = 0; i < NRAW; ++i) {
+      const int c = threadIdx.x + kThreads * i;
+      const int ra = c >> 3;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int seg = 2 * (c & 7) + e;
+        *reinterpret_cast<u32x4*>(dst + ra * kDim + 8 * (is_v ? v_seg(ra, seg) : k_seg(ra, seg))) =
+            widen(u32x2{src[i][2 * e], src[i][2 * e + 1]});
+      }
+    }
+  };
+
+  bf16x8 bq[KS];
+  f32x16 acc_o[kDim / 32];
+#pragma unroll
+  for (int i = 0; i < kDim / 32; ++i) acc_o[i] = f32x16{};
+  float m_run = -INFINITY, l_run = 0.f;
+  // P of the pending sub-block in bf16, as the B operand of O^T = V^T P^T:
+  // k-step u covers keys 32(u/2) + 16(u%2) + {4h + e, 8 + 4h + e}, e = 0..3
+  bf16x8 bp[kSub / 16];
+  float alpha_pend = 0.f;                 // alpha of the sub-block whose P is in bp
+
+  // S^T = K Q^T on one sub-block: lane (n, h) gets keys 32i + 8(e/4) + 4h + e%4
+  // of row n.  16 MFMA slots, each fenced off from the next so that the
+  // compiler keeps the order; LDS operands are read kAhead slots ahead.
+  auto scores = [&](const uint16_t* kbuf, f32x16 (&acc_s)[MT]) {
+    const char* kbb = reinterpret_cast<const char*>(kbuf);
+    constexpr int NS = MT * KS;
+    auto kread = [&](int j) -> bf16x8 {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kbb + lo.ks[j % KS] + 2 * 32 * (j / KS) * kDim));
+    };
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc_s[i] = f32x16{};
+    bf16x8 kr[NS];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) kr[j] = kread(j);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      if (j + kAhead < NS) kr[j + kAhead] = kread(j + kAhead);
+      acc_s[j / KS] = mfma32x32x16(kr[j], bq[j % KS], acc_s[j / KS]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto mask = [&](f32x16 (&acc_s)[MT], int key0) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = key0 + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
+        acc_s[i][e] = key <= p ? acc_s[i][e] : -INFINITY;
+      }
+  };
+  // eight weights as a B operand; their sum in fp32, as they are
+  auto pack8 = [&](const f32x16& a, int e0, float& lsum) -> bf16x8 {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lsum += a[e0 + e];
+    uint4 w;
+    w.x = pack_bf16x2(a[e0 + 0], a[e0 + 1]);
+    w.y = pack_bf16x2(a[e0 + 2], a[e0 + 3]);
+    w.z = pack_bf16x2(a[e0 + 4], a[e0 + 5]);
+    w.w = pack_bf16x2(a[e0 + 6], a[e0 + 7]);
+    return __builtin_bit_cast(bf16x8, w);
+  };
+
+  // O is rescaled by the pending sub-block's alpha only when some row's maximum moved
+  auto rescale = [&]() {
+    if (__ballot(alpha_pend != 1.f)) {
+#pragma unroll
+      for (int i = 0; i < kDim / 32; ++i) acc_o[i] *= alpha_pend;
+    }
+  };
+  // V^T operand of k-step u, dim tile td, read down V's columns
+  auto read_vt = [&](const uint16_t* vbuf, int u, int td) -> bf16x8 {
+    const char* a0 = reinterpret_cast<const char*>(vbuf) + lo.vs[td] + 2 * (32 * (u >> 1) + 16 * (u & 1)) * kDim;
+    const uint2 x0 = lds_tr4(reinterpret_cast<const uint16_t*>(a0));
+    const uint2 x1 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + 2 * 8 * kDim));  // rows +8: same permutation
+    return __builtin_bit_cast(bf16x8, make_uint4(x0.x, x0.y, x1.x, x1.y));
+  };
+  // O^T += V^T P^T from one value sub-block in 16 fenced MFMA slots, beside(j)
+  // after the j-th
+  auto pv = [&](const uint16_t* vbuf, auto beside) {
+    constexpr int NO = (kSub / 16) * (kDim / 32);
+    auto vread = [&](int j) { return read_vt(vbuf, j / (kDim / 32), j % (kDim / 32)); };
+    bf16x8 vr[NO];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) vr[j] = vread(j);
+#pragma unroll
+    for (int j = 0; j < NO; ++j) {
+      if (j + kAhead < NO) vr[j + kAhead] = vread(j + kAhead);
+      acc_o[j % (kDim / 32)] = mfma32x32x16(vr[j], bp[j / (kDim / 32)], acc_o[j % (kDim / 32)]);
+      beside(j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // One sixteenth of a sub-block's softmax (raw scores; scale_log2 > 0 keeps
+  // their order): j = 0, 1 the maximum, 2 .. 13 the weights, 14, 15 their sum
+  // and the packing.
+  struct Soft {
+    float m0, m_new, alpha, neg, lsum;
+    bf16x8 bp[kSub / 16];
+  };
+  auto soft_step = [&](Soft& z, f32x16 (&acc_s)[MT], int j) __attribute__((always_inline)) {
+    if (j == 0) {
+      z.m0 = -INFINITY;
+      z.lsum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z.m0 = fmaxf(z.m0, acc_s[0][e]);
+    } else if (j == 1) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z.m0 = fmaxf(z.m0, acc_s[1][e]);
+      z.m0 = fmaxf(z.m0, xor32f(z.m0));
+      z.m_new = fmaxf(m_run, z.m0);
+      const float mm = z.m_new == -INFINITY ? 0.f : z.m_new;   // rows with nothing visible yet
+      z.alpha = exp2_hw((m_run - mm) * scale_log2);
+      z.neg = -mm * scale_log2;
+    } else if (j < 14) {
+#pragma unroll
+      for (int x = 0; x < 32; ++x) {
+        if (2 + (3 * x) / 8 != j) continue;
+        acc_s[x >> 4][x & 15] = exp2_hw(fmaf(acc_s[x >> 4][x & 15], scale_log2, z.neg));
+      }
+    } else {
+#pragma unroll
+      for (int u = 2 * (j - 14); u < 2 * (j - 14) + 2; ++u) z.bp[u] = pack8(acc_s[u >> 1], 8 * (u & 1), z.lsum);
+      if (j == 15) {
+        z.lsum += xor32f(z.lsum);
+        l_run = l_run * z.alpha + z.lsum;
+        m_run = z.m_new;
+      }
+    }
+  };
+  auto take = [&](const Soft& z) {
+#pragma unroll
+    for (int u = 0; u < kSub / 16; ++u) bp[u] = z.bp[u];
+    alpha_pend = z.alpha;
+  };
+
+  // iteration b: K_{b+1} is in k[(b+1)&1], V_b in v[b&1]; after the S^T slots
+  // each O^T slot carries one sixteenth of the next softmax, so the VALU works
+  // while the MFMA pipe drains.
+  auto step = [&](int b, auto masked_t) {
+    constexpr bool masked = decltype(masked_t)::value;
+    __builtin_amdgcn_s_waitcnt(0);        // this thread's copies of K_{b+1} and V_b have landed
+    __syncthreads();                      // everyone's have, and block b-1's readers are done
+    pw.advance((b + 1) << lg_sub);
+    if constexpr (kDma) {
+      if (b + 2 < b_end) dma(kb, lo.kg, false, b + 2, ring.k[b & 1]);
+      dma(vb, lo.vg, true, b + 1, ring.v[(b + 1) & 1]);
+    } else {
+      if (b + 2 < b_end) store(rk, false, ring.k[b & 1]);
+      store(rv, true, ring.v[(b + 1) & 1]);
+      if (b + 3 < b_end) fetch(kb, b + 3, rk);
+      if (b + 2 < b_end) fetch(vb, b + 2, rv);
+    }
+    if (!live) return;
+    rescale();
+    __builtin_amdgcn_sched_barrier(0);
+    f32x16 acc_s[MT];
+    scores(ring.k[(b + 1) & 1], acc_s);
+    Soft z;
+    pv(ring.v[b & 1], [&](int j) __attribute__((always_inline)) {
+      if (masked && j == 0) mask(acc_s, (b + 1) * kSub);
+      soft_step(z, acc_s, j);
+    });
+    take(z);
+  };
+
+  if (b_begin < b_end) {
+    pw.start(b_begin << lg_sub);
+    if constexpr (kDma) {
+      dma(kb, lo.kg, false, b_begin, ring.k[b_begin & 1]);
+      dma(vb, lo.vg, true, b_begin, ring.v[b_begin & 1]);
+      if (b_begin + 1 < b_end) dma(kb, lo.kg, false, b_begin + 1, ring.k[(b_begin + 1) & 1]);
+    } else {
+      u32x4 r0[NRAW], r1[NRAW], r2[NRAW];
+      fetch(kb, b_begin, r0);
+      fetch(vb, b_begin, r1);
+      if (b_begin + 1 < b_end) fetch(kb, b_begin + 1, r2);
+      if (b_begin + 2 < b_end) fetch(kb, b_begin + 2, rk);
+      if (b_begin + 1 < b_end) fetch(vb, b_begin + 1, rv);
+      store(r0, false, ring.k[b_begin & 1]);
+      store(r1, true, ring.v[b_begin & 1]);
+      if (b_begin + 1 < b_end) store(r2, false, ring.k[(b_begin + 1) & 1]);
+    }
+#pragma unroll
+    for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (live) {
+      f32x16 acc_s[MT];
+      scores(ring.k[b_begin & 1], acc_s);
+      if (b_begin >= nfree) mask(acc_s, b_begin * kSub);
+      Soft z;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) soft_step(z, acc_s, j);
+      take(z);
+    }
+    int b = b_begin;
+    for (; b + 1 < min(nfree, b_end); ++b) step(b, std::false_type{});
+    for (; b + 1 < b_end; ++b) step(b, std::true_type{});
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (live) {
+      rescale();
+      pv(ring.v[b & 1], [](int) {});
+    }
+  }
+  if (!valid) return;
+  const bool empty = !(l_run > 0.f);
+  const float inv_l = empty ? 0.f : o_scale / l_run;
+  // O^T tile td: lane (n, h) holds d = 32td + 8(e/4) + 4h + e%4 of row n
+  uint16_t* orow = o + head_row * kDim + 4 * h;
+#pragma unroll
+  for (int td = 0; td < kDim / 32; ++td)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      uint2 w;
+      w.x = pack_bf16x2(acc_o[td][4 * e4 + 0] * inv_l, acc_o[td][4 * e4 + 1] * inv_l);
+      w.y = pack_bf16x2(acc_o[td][4 * e4 + 2] * inv_l, acc_o[td][4 * e4 + 3] * inv_l);
+      *reinterpret_cast<uint2*>(orow + 32 * td + 8 * e4) = w;
+    }
+  if (h == 0) lse[head_row] = empty ? -INFINITY : (m_run * scale_log2 + __log2f(l_run)) * kLn_2;
+}
+
+// ---------------------------------------------------------------- host side
+int validate_paged(const msa_seqs* seqs, int H_q, int H_kv, int head_dim) {
+  int st = msa_host::validate_seqs(seqs);
+  if (st != MSA_OK) return st;
+  if (H_q < 1 || H_kv < 1 || head_dim < 1 || H_q % H_kv != 0) return MSA_ERR_INVALID;
+  if (!seqs->block_table) return MSA_ERR_UNSUPPORTED;   // a contiguous key side is msa_dense_attn's
+  if (!msa_host::is_pow2(seqs->page_size) || seqs->page_size < 16 || seqs->page_size > 8192) return MSA_ERR_INVALID;
+  if (head_dim != kDim) return MSA_ERR_UNSUPPORTED;
+  if (H_q / H_kv > 16 || H_kv > 64) return MSA_ERR_UNSUPPORTED;
+  if (seqs->total_q_rows * H_kv >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
+  if (seqs->total_kv_rows >= (int64_t(1) << 35)) return MSA_ERR_UNSUPPORTED;
+  return MSA_OK;
+}
+
+bool scale_ok(float x) { return x > 0.f && x < 3.0e38f; }   // finite and positive
+
+int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_scale, float k_scale, float v_scale,
+               const msa_seqs* seqs, int H_q, int H_kv, int head_dim, float softmax_scale, void* o, float* lse,
+               void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int st = validate_paged(seqs, H_q, H_kv, head_dim);
+  if (st != MSA_OK) return st;
+  if (fp8 && (!scale_ok(q_scale) || !scale_ok(k_scale) || !scale_ok(v_scale))) return MSA_ERR_INVALID;
+  if (seqs->total_q_rows == 0) return MSA_OK;
+  if (!q || !k || !v || !o || !lse) return MSA_ERR_INVALID;
+  const flash::LogitScale scale = flash::logit_scale(softmax_scale * q_scale * k_scale * kLog2E);
+  const int G = H_q / H_kv;
+  auto launch = [&](auto kernel, auto elem, int waves) -> int {
+    using T = decltype(elem);
+    int64_t tiles;
+    flash::Grid gr = flash::plan_grid(seqs, waves * (32 / G), seqs->max_q_rows, &tiles);
+    if (tiles * H_kv >= (int64_t(1) << 22)) return MSA_ERR_UNSUPPORTED;
+    msa_prof::launch("paged_attn_kernel", kernel, dim3(static_cast<unsigned>(tiles * H_kv)), dim3(waves * kWave), 0, stream,
+                     static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), *seqs, gr, H_q, H_kv,
+                     scale.log2, scale.q_flip, v_scale, static_cast<uint16_t*>(o), lse);
+    return msa_host::launch_status();
+  };
+  const int waves_needed = (seqs->max_q_rows + 32 / G - 1) / (32 / G);
+  auto pick = [&](auto elem) -> int {
+    using T = decltype(elem);
+    if (waves_needed <= 1) return launch(paged_attn_kernel<T, 1>, elem, 1);
+    if (waves_needed <= 2) return launch(paged_attn_kernel<T, 2>, elem, 2);
+    if (waves_needed <= 4) return launch(paged_attn_kernel<T, 4>, elem, 4);
+    return launch(paged_attn_kernel<T, 8>, elem, 8);
+  };
+  return fp8 ? pick(uint8_t{}) : pick(uint16_t{});
+}
+
+}  // namespace
+
+extern "C" size_t msa_dense_attn_paged_workspace_size(const msa_seqs* seqs, int num_q_heads, int num_kv_heads,
+                                                     int head_dim) {
+  if (validate_paged(seqs, num_q_heads, num_kv_heads, head_dim) != MSA_OK) return 0;
+  return 0;
+}
+
+extern "C" int msa_dense_attn_paged(const void* q, const void* k, const void* v, const msa_seqs* seqs, int num_q_heads,
+                                    int num_kv_heads, int head_dim, float softmax_scale, void* o, float* lse,
+                                    void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return paged_attn(q, k, v, false, 1.f, 1.f, 1.f, seqs, num_q_heads, num_kv_heads, head_dim, softmax_scale, o, lse,
+                    workspace, workspace_bytes, stream);
+}
+
+extern "C" int msa_dense_attn_paged_fp8(const void* q, const void* k, const void* v, float q_scale, float k_scale,
+                                        float v_scale, const msa_seqs* seqs, int num_q_heads, int num_kv_heads,
+                                        int head_dim, float softmax_scale, void* o, float* lse, void* workspace,
+                                        size_t workspace_bytes, hipStream_t stream) {
+  return paged_attn(q, k, v, true, q_scale, k_scale, v_scale, seqs, num_q_heads, num_kv_heads, head_dim, softmax_scale, o,
+                    lse, workspace, workspace_bytes, stream);
+}

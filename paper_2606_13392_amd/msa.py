@@ -26,6 +26,10 @@ EXPORTS = [
     "msa_sparse_attn_decode_workspace_size", "msa_sparse_attn_decode",
     "msa_sparse_attn_prefill_fp8", "msa_sparse_attn_decode_fp8",
     "msa_dense_attn_workspace_size", "msa_dense_attn",
+    "msa_dense_attn_paged_workspace_size", "msa_dense_attn_paged", "msa_dense_attn_paged_fp8",
+    "msa_qk_norm_rope", "msa_qk_norm_rope_fp8",
+    "msa_qk_norm_rope_backward_workspace_size", "msa_qk_norm_rope_backward",
+    "msa_kv_append", "msa_kv_append_fp8",
     "msa_sparse_attn_backward_workspace_size", "msa_sparse_attn_backward",
     "msa_sparse_kl_backward_workspace_size", "msa_sparse_kl_backward",
     "msa_profile_enable", "msa_profile_reset", "msa_profile_kernel_name", "msa_profile_read",
@@ -45,6 +49,15 @@ class MsaSeqsC(ctypes.Structure):
         ("block_table", ctypes.c_void_p),
         ("block_table_stride", ctypes.c_int32),
         ("page_size", ctypes.c_int32),
+    ]
+
+
+class MsaRopeC(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("inv_freq", ctypes.c_void_p),
     ]
 
 
@@ -84,6 +97,25 @@ def lib() -> ctypes.CDLL:
         L.msa_dense_attn_workspace_size.restype = Z
         L.msa_dense_attn.argtypes = [P, P, P, S, I, I, I, F, P, P, P, Z, P]
         L.msa_dense_attn.restype = I
+        L.msa_dense_attn_paged_workspace_size.argtypes = [S, I, I, I]
+        L.msa_dense_attn_paged_workspace_size.restype = Z
+        L.msa_dense_attn_paged.argtypes = [P, P, P, S, I, I, I, F, P, P, P, Z, P]
+        L.msa_dense_attn_paged.restype = I
+        L.msa_dense_attn_paged_fp8.argtypes = [P, P, P, F, F, F, S, I, I, I, F, P, P, P, Z, P]
+        L.msa_dense_attn_paged_fp8.restype = I
+        R, N = ctypes.POINTER(MsaRopeC), ctypes.c_int64
+        L.msa_qk_norm_rope.argtypes = [P, N, P, N, S, I, I, I, P, P, F, R, P, P, P]
+        L.msa_qk_norm_rope.restype = I
+        L.msa_qk_norm_rope_fp8.argtypes = [P, N, P, N, F, F, S, I, I, I, P, P, F, R, P, P, P]
+        L.msa_qk_norm_rope_fp8.restype = I
+        L.msa_qk_norm_rope_backward_workspace_size.argtypes = [S, I, I, I]
+        L.msa_qk_norm_rope_backward_workspace_size.restype = Z
+        L.msa_qk_norm_rope_backward.argtypes = [P, N, P, N, P, P, S, I, I, I, P, P, F, R, P, N, P, N, P, P, P, Z, P]
+        L.msa_qk_norm_rope_backward.restype = I
+        L.msa_kv_append.argtypes = [P, N, P, N, P, N, S, I, I, I, P, P, F, R, R, P, P, P, P]
+        L.msa_kv_append.restype = I
+        L.msa_kv_append_fp8.argtypes = [P, N, P, N, F, F, P, N, S, I, I, I, P, P, F, R, R, P, P, P, P]
+        L.msa_kv_append_fp8.restype = I
         L.msa_sparse_attn_backward_workspace_size.argtypes = [S, I, I, I, I, I]
         L.msa_sparse_attn_backward_workspace_size.restype = Z
         L.msa_sparse_attn_backward.argtypes = [P, P, P, P, P, P, P, S, I, I, I, I, I, F, P, P, P, P, Z, P]
@@ -113,6 +145,19 @@ def _check(status: int, what: str):
 def _stream() -> int:
     # the handle itself: building a torch.cuda.Stream object took 2.8 us of a call
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _call(name: str, device: torch.device, *args) -> None:
+    """The library's call ``name`` with the current stream of ``device`` as its last argument, whichever device is
+    current."""
+    fn, cur = getattr(lib(), name), torch.cuda.current_device()
+    if cur == device.index:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(cur))
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if st != MSA_OK:
+        _check(st, name)
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -364,6 +409,263 @@ def dense_attn(q, k, v, seqs: Seqs, softmax_scale=None, out=None, lse=None, work
                               _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream())
     _check(st, "msa_dense_attn")
     return out, lse
+
+
+# ---------------------------------------------------------------- dense attention on a paged cache
+def dense_attn_paged_workspace_size(seqs: Seqs, num_q_heads: int, num_kv_heads: int, head_dim: int = 128) -> int:
+    return int(lib().msa_dense_attn_paged_workspace_size(seqs.ref(), num_q_heads, num_kv_heads, head_dim))
+
+
+def _dense_paged(dtype, q, k, v, scales, seqs: Seqs, softmax_scale, out, lse, workspace):
+    Tq, H_q, d_h = q.shape
+    H_kv = k.shape[1]
+    dev = seqs.device
+    _need(q, "q", dtype, (seqs.total_q_rows, H_q, d_h), dev)
+    _need(k, "k", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
+    _need(v, "v", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
+    if out is None:
+        out = torch.empty((Tq, H_q, d_h), dtype=torch.bfloat16, device=dev)
+    else:
+        _need(out, "o", torch.bfloat16, (Tq, H_q, d_h), dev)
+    if lse is None:
+        lse = torch.empty((Tq, H_q), dtype=torch.float32, device=dev)
+    else:
+        _need(lse, "lse", torch.float32, (Tq, H_q), dev)
+    scale = 1.0 / math.sqrt(d_h) if softmax_scale is None else float(softmax_scale)
+    ws = _workspace(lib().msa_dense_attn_paged_workspace_size(seqs.ref(), H_q, H_kv, d_h), dev, workspace)
+    name, scales = ("msa_dense_attn_paged", ()) if scales is None else ("msa_dense_attn_paged_fp8", scales)
+    _call(name, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), *scales, seqs.ref(), H_q, H_kv, d_h, scale, out.data_ptr(),
+          lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    return out, lse
+
+
+def dense_attn_paged(q, k, v, seqs: Seqs, softmax_scale=None, out=None, lse=None, workspace=None):
+    """Dense causal attention of the new rows over a paged cache: (O bf16 [Tq, H_q, d], LSE fp32 [Tq, H_q])."""
+    return _dense_paged(torch.bfloat16, q, k, v, None, seqs, softmax_scale, out, lse, workspace)
+
+
+def dense_attn_paged_fp8(q, k, v, scales, seqs: Seqs, softmax_scale=None, out=None, lse=None, workspace=None):
+    """The same on e4m3 codes (uint8 tensors) with per-tensor scales (q, k, v)."""
+    qs, ks, vs = (float(x) for x in scales)
+    return _dense_paged(torch.uint8, q, k, v, (qs, ks, vs), seqs, softmax_scale, out, lse, workspace)
+
+
+# ---------------------------------------------------------------- norms, rotation, cache append
+class Rope:
+    """Rotation by position (struct msa_rope): ``inv_freq`` (radians per position
+    of each pair, float64 on the device; its length is half the rotated
+    dimensions), the pair layout and the factor of cosine and sine."""
+
+    def __init__(self, inv_freq: torch.Tensor, interleaved: bool = False, scale: float = 1.0):
+        if inv_freq.dim() != 1:
+            raise ValueError("inv_freq: expected a 1-d tensor")
+        _need(inv_freq, "inv_freq", torch.float64, tuple(inv_freq.shape), inv_freq.device)
+        self.inv_freq = inv_freq
+        self.c = MsaRopeC(2 * inv_freq.numel(), 1 if interleaved else 0, float(scale), inv_freq.data_ptr())
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     trained_len: int = 0, fast_turns: float = 32.0, slow_turns: float = 1.0):
+    """(inv_freq as float64 CPU tensor, factor of cosine and sine) of rotary positions.
+
+    ``scaling`` for contexts ``factor`` times as long as the trained ones:
+      none       base^(-2i / rot_dim)
+      linear     all divided by factor (positions interpolated)
+      ntk        base * factor^(rot_dim / (rot_dim - 2)): the slowest pair is slowed
+                 by factor, the fastest kept
+      by_parts   a pair that turns r times over ``trained_len`` positions is kept for
+                 r > ``fast_turns``, divided by factor for r < ``slow_turns``, and in
+                 between mixed linearly in r (YaRN, arXiv 2309.00071, Sec. 3.2);
+                 cosine and sine get 0.1 ln(factor) + 1 (Sec. 3.4)"""
+    if rot_dim < 8 or rot_dim % 8 != 0:
+        raise ValueError("rot_dim: expected a positive multiple of 8")
+    if not base > 1.0 or not factor >= 1.0 or not math.isfinite(base * factor):
+        raise ValueError("base must be above 1 and factor at least 1, both finite")
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    if scaling == "ntk":
+        return (base * factor ** (rot_dim / (rot_dim - 2))) ** (-2.0 * i / rot_dim), 1.0
+    f = base ** (-2.0 * i / rot_dim)
+    if scaling == "none":
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling != "by_parts":
+        raise ValueError(f"scaling: expected none, linear, ntk or by_parts, got {scaling!r}")
+    if trained_len < 1 or not fast_turns > slow_turns > 0:
+        raise ValueError("by_parts needs trained_len >= 1 and fast_turns > slow_turns > 0")
+    keep = ((trained_len * f / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns)).clamp(0.0, 1.0)
+    return f * keep + f / factor * (1.0 - keep), 0.1 * math.log(factor) + 1.0
+
+
+def _heads(t: torch.Tensor, name: str, rows: int, device):
+    """Heads of a [rows, heads, dim] bf16 tensor whose rows may be apart (columns of a wider one)."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
+    if t.dim() != 3 or t.shape[0] != rows:
+        raise ValueError(f"{name}: expected shape ({rows}, heads, dim), got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    _, h, d = t.shape
+    sr, sh, sd = t.stride()
+    if (sd != 1 and d != 1) or (sh != d and h != 1):
+        raise ValueError(f"{name}: a row's heads must be contiguous")
+    return h, (sr if rows > 1 else h * d)
+
+
+def _weight(w: Optional[torch.Tensor], name: str, dim: int, device):
+    if w is None:
+        return None
+    _need(w, name, torch.float32, (dim,), device)
+    return w.data_ptr()
+
+
+def _rope(rope: Optional[Rope], device):
+    if rope is None:
+        return None
+    if rope.inv_freq.device != device:
+        raise ValueError(f"rope: expected device {device}, got {rope.inv_freq.device}")
+    return ctypes.byref(rope.c)
+
+
+def _norm_rope(fp8, q, k, scales, seqs: Seqs, rope, q_weight, k_weight, eps, q_out, k_out):
+    T, dev = seqs.total_q_rows, seqs.device
+    H_q, q_stride = _heads(q, "q", T, dev)
+    d = q.shape[2]
+    H_kv, k_stride = 0, 0
+    if k is not None:
+        H_kv, k_stride = _heads(k, "k", T, dev)
+        if k.shape[2] != d:
+            raise ValueError(f"k: expected head size {d}, got {k.shape[2]}")
+    dtype = torch.uint8 if fp8 else torch.bfloat16
+    if q_out is None:
+        q_out = torch.empty((T, H_q, d), dtype=dtype, device=dev)
+    else:
+        _need(q_out, "q_out", dtype, (T, H_q, d), dev)
+    if k is not None and k_out is None:
+        k_out = torch.empty((T, H_kv, d), dtype=dtype, device=dev)
+    elif k_out is not None:
+        _need(k_out, "k_out", dtype, (T, H_kv, d), dev)
+    args = (seqs.ref(), H_q, H_kv, d, _weight(q_weight, "q_weight", d, dev), _weight(k_weight, "k_weight", d, dev),
+            float(eps), _rope(rope, dev), q_out.data_ptr(), _ptr(k_out))
+    if fp8:
+        qs, ks = scales
+        _call("msa_qk_norm_rope_fp8", dev, q.data_ptr(), q_stride, _ptr(k), k_stride, float(qs), float(ks), *args)
+    else:
+        _call("msa_qk_norm_rope", dev, q.data_ptr(), q_stride, _ptr(k), k_stride, *args)
+    return q_out, k_out
+
+
+def qk_norm_rope(q, k, seqs: Seqs, rope: Optional[Rope], q_weight=None, k_weight=None, eps: float = 1e-6,
+                 q_out=None, k_out=None):
+    """Norm of each head and rotation by position of the new rows' q [Tq, H_q, d] and k [Tq, H_kv, d] (bf16; rows
+    may be columns of a wider tensor; ``k`` may be None): (q_out, k_out), contiguous bf16."""
+    return _norm_rope(False, q, k, None, seqs, rope, q_weight, k_weight, eps, q_out, k_out)
+
+
+def qk_norm_rope_fp8(q, k, scales, seqs: Seqs, rope: Optional[Rope], q_weight=None, k_weight=None, eps: float = 1e-6,
+                     q_out=None, k_out=None):
+    """The same into e4m3 codes (uint8) with per-tensor scales (q, k)."""
+    return _norm_rope(True, q, k, scales, seqs, rope, q_weight, k_weight, eps, q_out, k_out)
+
+
+def qk_norm_rope_backward_workspace_size(seqs: Seqs, num_q_heads: int, num_kv_heads: int, head_dim: int) -> int:
+    return int(lib().msa_qk_norm_rope_backward_workspace_size(seqs.ref(), num_q_heads, num_kv_heads, head_dim))
+
+
+def qk_norm_rope_backward(q, k, d_q_out, d_k_out, seqs: Seqs, rope: Optional[Rope], q_weight=None, k_weight=None,
+                          eps: float = 1e-6, d_q=None, d_k=None, d_q_weight=None, d_k_weight=None, workspace=None):
+    """Gradients of qk_norm_rope: (d_q, d_k, d_q_weight, d_k_weight); a weight's is None where it is None.  ``q`` and
+    ``k`` are the forward's inputs (not read, and may be None, without weight); d_q and d_k may be columns of a wider
+    tensor."""
+    T, dev = seqs.total_q_rows, seqs.device
+
+    def side(x, g, w, d, dw, name):
+        if g is None:
+            return None, 0, 0, None, None, 0, None, None, None
+        h, stride = _heads(g, f"d_{name}_out", T, dev)
+        dim = g.shape[2]
+        if T > 1 and stride != h * dim:
+            raise ValueError(f"d_{name}_out: must be contiguous")
+        x_stride = 0
+        if w is not None:
+            if x is None:
+                raise ValueError(f"{name}: needed for the norm's gradient")
+            hx, x_stride = _heads(x, name, T, dev)
+            if x.shape[1:] != g.shape[1:]:
+                raise ValueError(f"{name}: expected {tuple(g.shape)}, got {tuple(x.shape)}")
+        d = torch.empty((T, h, dim), dtype=torch.bfloat16, device=dev) if d is None else d
+        hd, d_stride = _heads(d, f"d_{name}", T, dev)
+        if d.shape[1:] != g.shape[1:]:
+            raise ValueError(f"d_{name}: expected {tuple(g.shape)}, got {tuple(d.shape)}")
+        if w is not None:
+            dw = torch.empty(dim, dtype=torch.float32, device=dev) if dw is None else dw
+            _need(dw, f"d_{name}_weight", torch.float32, (dim,), dev)
+        elif dw is not None:
+            raise ValueError(f"d_{name}_weight: given without {name}_weight")
+        return (x if w is not None else None), x_stride, h, g, d, d_stride, _weight(w, f"{name}_weight", dim, dev), dw, dim
+
+    q, q_stride, H_q, gq, d_q, d_q_stride, qw, d_qw, dim = side(q, d_q_out, q_weight, d_q, d_q_weight, "q")
+    k, k_stride, H_kv, gk, d_k, d_k_stride, kw, d_kw, dim_k = side(k, d_k_out, k_weight, d_k, d_k_weight, "k")
+    if gq is None and gk is None:
+        raise ValueError("d_q_out or d_k_out is needed")
+    if gq is not None and gk is not None and dim != dim_k:
+        raise ValueError(f"d_k_out: expected head size {dim}, got {dim_k}")
+    dim = dim if gq is not None else dim_k
+    ws = workspace
+    if qw is not None or kw is not None:
+        ws = _workspace(lib().msa_qk_norm_rope_backward_workspace_size(seqs.ref(), H_q, H_kv, dim), dev, workspace)
+    _call("msa_qk_norm_rope_backward", dev, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(gq), _ptr(gk), seqs.ref(), H_q, H_kv,
+          dim, qw, kw, float(eps), _rope(rope, dev), _ptr(d_q), d_q_stride, _ptr(d_k), d_k_stride, _ptr(d_qw), _ptr(d_kw),
+          _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    return d_q, d_k, d_qw, d_kw
+
+
+def _append(fp8, k, v, scales, seqs: Seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
+            index_rope):
+    T, dev = seqs.total_q_rows, seqs.device
+    H_kv, k_stride = _heads(k, "k", T, dev)
+    H_v, v_stride = _heads(v, "v", T, dev)
+    d = k.shape[2]
+    if v.shape != k.shape:
+        raise ValueError(f"v: expected shape {tuple(k.shape)}, got {tuple(v.shape)}")
+    dtype = torch.uint8 if fp8 else torch.bfloat16
+    _need(k_cache, "k_cache", dtype, (seqs.total_kv_rows, H_kv, d), dev)
+    _need(v_cache, "v_cache", dtype, (seqs.total_kv_rows, H_kv, d), dev)
+    d_idx, i_stride, iw, ir = 0, 0, None, None
+    if (index_k is None) != (index_k_cache is None):
+        raise ValueError("index_k and index_k_cache go together")
+    if index_k is not None:
+        if index_k.dim() != 2:
+            raise ValueError(f"index_k: expected shape ({T}, d_idx), got {tuple(index_k.shape)}")
+        d_idx = index_k.shape[1]
+        _, i_stride = _heads(index_k.unsqueeze(1), "index_k", T, dev)
+        _need(index_k_cache, "index_k_cache", torch.bfloat16, (seqs.total_kv_rows, d_idx), dev)
+        iw = _weight(index_k_weight, "index_k_weight", d_idx, dev)
+        ir = _rope(index_rope, dev)
+    args = (_ptr(index_k), i_stride, seqs.ref(), H_kv, d, d_idx, _weight(k_weight, "k_weight", d, dev), iw, float(eps),
+            _rope(rope, dev), ir, k_cache.data_ptr(), v_cache.data_ptr(), _ptr(index_k_cache))
+    if fp8:
+        ks, vs = scales
+        _call("msa_kv_append_fp8", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, float(ks), float(vs), *args)
+    else:
+        _call("msa_kv_append", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, *args)
+
+
+def kv_append(k, v, seqs: Seqs, rope: Optional[Rope], k_cache, v_cache, k_weight=None, eps: float = 1e-6, index_k=None,
+              index_k_cache=None, index_k_weight=None, index_rope: Optional[Rope] = None) -> None:
+    """The new rows' k (norm, rotation), v and index_k (norm, rotation) into their cache rows, in place."""
+    _append(False, k, v, None, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
+            index_rope)
+
+
+def kv_append_fp8(k, v, scales, seqs: Seqs, rope: Optional[Rope], k_cache, v_cache, k_weight=None, eps: float = 1e-6,
+                  index_k=None, index_k_cache=None, index_k_weight=None, index_rope: Optional[Rope] = None) -> None:
+    """The same with e4m3 k and v caches (uint8) and per-tensor scales (k, v); index keys stay bf16."""
+    _append(True, k, v, scales, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
+            index_rope)
 
 
 # ---------------------------------------------------------------- kernel timing
