@@ -10,6 +10,16 @@
 // maximum and sum per row in registers, fp32).  The layout of a sub-block in
 // LDS and the transposing reads are those of flash_tile.h.
 //
+// Few tiles: the chip is then filled by a split of the keys.  The steps (64
+// keys of one tile) of a group's tiles, one sequence after the other, are
+// numbered through and dealt out evenly: CTA c of the group's gets steps
+// c * per .. (c + 1) * per - 1, whatever lengths the sequences have, so a batch
+// of ragged contexts ends everywhere at once.  Lengths are on the device, so
+// every CTA forms the numbering itself (a wave's prefix sum over up to 256
+// sequences).  Only a CTA's first and last tile can be shared with its
+// neighbours; those leave their part in fp32, and merge_kernel joins them by
+// the log-sum-exp rule in the order of the keys.
+//
 // Pages: 16 .. 8192 rows, a power of two.  Each lane holds the place of one
 // unit of min(page, 64) rows of the sequence, so 64 units' page ids arrive
 // with one load, a window ahead of their use, and a copy's scalar base comes
@@ -76,10 +86,99 @@ struct PageWindow {
   }
 };
 
+// How the steps are dealt out.
+struct Plan {
+  flash::Grid gr;                        // tiles of the unsplit grid
+  int ctas;                              // CTAs per group that share its steps; 0: a CTA per tile and group
+  int min_steps;                         // per CTA, where there are few
+  int qt;                                // query rows per tile
+};
+constexpr int kMaxSplitSeqs = 256;       // four sequences per lane of the prefix sum
+
+// A sequence with its lengths cut to the bounds that the host planned with.
+__device__ __forceinline__ SeqGeom bounded_geom(const msa_seqs& sq, int s) {
+  SeqGeom g = seq_geom(sq, s);
+  g.kv_len = min(g.kv_len, sq.max_kv_len);
+  g.q_rows = min(g.q_rows, sq.max_q_rows);
+  return g;
+}
+
+// The numbering of a group's steps, formed by a wave: a tile of a sequence has
+// as many as the sequence's last, at least one.
+struct Steps {
+  int cost[4];                           // steps of sequences 4 lane .. 4 lane + 3
+  int before;                            // steps of all sequences before them
+  int total, per;                        // of the group; of a CTA
+
+  static __device__ __forceinline__ int blocks(const SeqGeom& g) { return max(1, (g.kv_len + kSub - 1) / kSub); }
+  __device__ __forceinline__ Steps(const msa_seqs& sq, const Plan& pl) {
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = 4 * lane_id() + i;
+      cost[i] = 0;
+      if (s < sq.num_seqs) {
+        const SeqGeom g = bounded_geom(sq, s);
+        cost[i] = (max(g.q_rows, 0) + pl.qt - 1) / pl.qt * blocks(g);
+      }
+      sum += cost[i];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int x = __shfl_up(incl, d);
+      if (lane_id() >= d) incl += x;
+    }
+    before = incl - sum;
+    total = __builtin_amdgcn_readlane(incl, kWave - 1);
+    per = max(pl.min_steps, (total + pl.ctas - 1) / pl.ctas);
+  }
+  // first step of each sequence, and behind the last one
+  __device__ __forceinline__ void store(int (&first)[kMaxSplitSeqs + 1]) const {
+    int x = before;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      first[4 * lane_id() + i] = x;
+      x += cost[i];
+    }
+    if (lane_id() == kWave - 1) first[kMaxSplitSeqs] = x;
+  }
+  // sequence of step u < total (the same in every lane): the last that begins at or before it
+  __device__ __forceinline__ int seq_of(int u) const {
+    const int sum = cost[0] + cost[1] + cost[2] + cost[3];
+    const int j = __ffsll(static_cast<unsigned long long>(__ballot(u >= before && u < before + sum))) - 1;
+    int x = u - __builtin_amdgcn_readlane(before, j), i = 0;
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+      const int c = __builtin_amdgcn_readlane(cost[e], j);
+      if (i == e && x >= c) {
+        x -= c;
+        ++i;
+      }
+    }
+    return 4 * j + i;
+  }
+  // first step of sequence s
+  __device__ __forceinline__ int first(int s) const {
+    int x = __builtin_amdgcn_readlane(before, s >> 2);
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < (s & 3)) x += __builtin_amdgcn_readlane(cost[e], s >> 2);
+    return x;
+  }
+};
+
+// The part of a tile that a CTA leaves to merge_kernel: 0 where it does not
+// begin at the tile's first key, 1 where it does.  Each holds 32 * WAVES rows.
+struct Parts {
+  float* o;                              // [CTA][2][rows][128], normalised
+  float* lse;                            // [CTA][2][rows], base 2
+};
+
 // T: uint16_t = bf16 bits, uint8_t = E4M3 codes (o_scale multiplies O).
 template <typename T, int WAVES>
 __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_kernel(
-    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, msa_seqs sq, flash::Grid gr, int H_q,
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, msa_seqs sq, Plan pl, Parts parts, int H_q,
     int H_kv, float scale_log2, uint32_t q_flip, float o_scale, uint16_t* __restrict__ o, float* __restrict__ lse) {
   constexpr int kThreads = WAVES * kWave;
   constexpr int MT = kSub / 32;            // 32-key tiles of S^T
@@ -88,6 +187,7 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   constexpr int NDMA = kSub / 4 / WAVES;   // DMA instructions per wave per sub-block and tensor
   constexpr int NRAW = kSub * kDim / 16 / kThreads;   // E4M3: 16-byte pieces per thread and tensor
   __shared__ __align__(16) Ring ring;
+  __shared__ int first[kMaxSplitSeqs + 1];
   const int lane = lane_id();
   const int wave = threadIdx.x / kWave;
   const int n = lane & 31, h = lane >> 5;
@@ -96,43 +196,12 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   const int qt = WAVES * qpw;              // query rows per CTA
   const int jq = n / G, hh = n % G;
   const int r = static_cast<int>(blockIdx.x % H_kv);
-  int s, tile;
-  flash::locate_tile(sq, gr, static_cast<int>(blockIdx.x / H_kv), qt, &s, &tile);
-  const SeqGeom g = seq_geom(sq, s);
-  const int t0 = tile * qt;
-  const int base_p = g.kv_len - g.q_rows;  // position of the sequence's first query row
-  int t_end = min(t0 + qt, g.q_rows);
-  t_end = static_cast<int>(min(static_cast<int64_t>(t_end), sq.total_q_rows - g.q_begin));
-  if (t_end <= t0) return;                                // uniform over the CTA
-  const int p_last = base_p + t_end - 1;
-  const int t = t0 + wave * qpw + jq;                     // this lane's query row in the sequence
-  const bool valid = n < qpw * G && t < t_end;
-  const int p = valid ? base_p + t : -1;
-  const bool live = t0 + wave * qpw < t_end;              // the wave has rows
-  // sub-blocks below nfree are visible to every row of the wave and need no mask
-  const int nfree = (base_p + min(t0 + wave * qpw, t_end - 1) + 1) / kSub;
-  const int64_t head_row = (static_cast<int64_t>(g.q_begin) + (valid ? t : t0)) * H_q + static_cast<int64_t>(r) * G + hh;
-  const int b_begin = 0, b_end = p_last < 0 ? 0 : p_last / kSub + 1;
-
-  Raw<T> rq[KS];
-  {
-    const T* qrow = q + head_row * kDim + 8 * h;
-#pragma unroll
-    for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
-  }
+  const int cta = static_cast<int>(blockIdx.x / H_kv);
 
   const int64_t stride = static_cast<int64_t>(H_kv) * kDim;
   const char* kb = reinterpret_cast<const char*>(k + static_cast<int64_t>(r) * kDim);
   const char* vb = reinterpret_cast<const char*>(v + static_cast<int64_t>(r) * kDim);
   const uint32_t stride_b = static_cast<uint32_t>(stride * sizeof(T));
-  PageWindow pw;
-  pw.table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
-  pw.lg_page = 31 - __clz(sq.page_size);
-  pw.lg_unit = min(pw.lg_page, 6);
-  pw.max_page = (sq.total_kv_rows >> pw.lg_page) - 1;
-  pw.units = ((g.kv_len - 1) >> pw.lg_unit) + 1;
-  const int lg_sub = 6 - pw.lg_unit;       // log2 of units per sub-block
-
   flash::LaneOffsets<NDMA> lo;
   {
     const int gq = lane >> 4, jj = lane & 15;
@@ -151,6 +220,41 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
       lo.vs[td] = 2 * (rl * kDim + 8 * v_seg(rl, col >> 3) + (col & 7));
     }
   }
+  // Sub-blocks b_from .. b_to - 1 of one tile of sequence s (b_to past its
+  // last: to its end), into O and LSE or, if that is not all of them, a part.
+  auto run_tile = [&](int s, int tile, int b_from, int b_to) __attribute__((always_inline)) {
+  const SeqGeom g = bounded_geom(sq, s);
+  const int t0 = tile * qt;
+  const int base_p = g.kv_len - g.q_rows;  // position of the sequence's first query row
+  int t_end = min(t0 + qt, g.q_rows);
+  t_end = static_cast<int>(min(static_cast<int64_t>(t_end), sq.total_q_rows - g.q_begin));
+  if (t_end <= t0) return;                                // uniform over the CTA
+  const int p_last = base_p + t_end - 1;
+  const int t = t0 + wave * qpw + jq;                     // this lane's query row in the sequence
+  const bool valid = n < qpw * G && t < t_end;
+  const int p = valid ? base_p + t : -1;
+  const bool live = t0 + wave * qpw < t_end;              // the wave has rows
+  // sub-blocks below nfree are visible to every row of the wave and need no mask
+  const int nfree = (base_p + min(t0 + wave * qpw, t_end - 1) + 1) / kSub;
+  const int64_t head_row = (static_cast<int64_t>(g.q_begin) + (valid ? t : t0)) * H_q + static_cast<int64_t>(r) * G + hh;
+  const int b_all = p_last < 0 ? 0 : p_last / kSub + 1;
+  const int b_begin = b_from, b_end = min(b_to, b_all);
+  if (b_begin > 0 && b_begin >= b_end) return;            // the tile's rows see none of these keys
+
+  Raw<T> rq[KS];
+  {
+    const T* qrow = q + head_row * kDim + 8 * h;
+#pragma unroll
+    for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
+  }
+  PageWindow pw;
+  pw.table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
+  pw.lg_page = 31 - __clz(sq.page_size);
+  pw.lg_unit = min(pw.lg_page, 6);
+  pw.max_page = (sq.total_kv_rows >> pw.lg_page) - 1;
+  pw.units = ((g.kv_len - 1) >> pw.lg_unit) + 1;
+  const int lg_sub = 6 - pw.lg_unit;       // log2 of units per sub-block
+
   // First byte of the rows of a sub-block, as seen from row `first` of it (the
   // unit that `first` lies in): base of offsets row * stride_b.
   auto base_of = [&](const char* base, int sub, int first) -> const char* {
@@ -413,6 +517,19 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   if (!valid) return;
   const bool empty = !(l_run > 0.f);
   const float inv_l = empty ? 0.f : o_scale / l_run;
+  const float lse2 = empty ? -INFINITY : m_run * scale_log2 + __log2f(l_run);
+  if (b_begin > 0 || b_end < b_all) {
+    const int64_t row = (2 * static_cast<int64_t>(blockIdx.x) + (b_begin > 0 ? 0 : 1)) * (32 * WAVES) + 32 * wave + n;
+    float* dst = parts.o + row * kDim + 4 * h;
+#pragma unroll
+    for (int td = 0; td < kDim / 32; ++td)
+#pragma unroll
+      for (int e4 = 0; e4 < 4; ++e4)
+        *reinterpret_cast<f32x4*>(dst + 32 * td + 8 * e4) =
+            f32x4{acc_o[td][4 * e4], acc_o[td][4 * e4 + 1], acc_o[td][4 * e4 + 2], acc_o[td][4 * e4 + 3]} * inv_l;
+    if (h == 0) parts.lse[row] = lse2;
+    return;
+  }
   // O^T tile td: lane (n, h) holds d = 32td + 8(e/4) + 4h + e%4 of row n
   uint16_t* orow = o + head_row * kDim + 4 * h;
 #pragma unroll
@@ -424,7 +541,125 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
       w.y = pack_bf16x2(acc_o[td][4 * e4 + 2] * inv_l, acc_o[td][4 * e4 + 3] * inv_l);
       *reinterpret_cast<uint2*>(orow + 32 * td + 8 * e4) = w;
     }
-  if (h == 0) lse[head_row] = empty ? -INFINITY : (m_run * scale_log2 + __log2f(l_run)) * kLn_2;
+  if (h == 0) lse[head_row] = lse2 * kLn_2;
+  };
+
+  if (pl.ctas == 0) {
+    int s, tile;
+    flash::locate_tile(sq, pl.gr, cta, qt, &s, &tile);
+    run_tile(s, tile, 0, INT32_MAX);
+    return;
+  }
+  int u, u_end, s;
+  {
+    const Steps steps(sq, pl);
+    u = cta * steps.per;
+    u_end = min(steps.total, u + steps.per);
+    if (u >= u_end) return;
+    s = steps.seq_of(u);
+    if (threadIdx.x < kWave) steps.store(first);
+  }
+  __syncthreads();
+  while (u < u_end) {
+    while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
+    const int nb = Steps::blocks(bounded_geom(sq, s)), off = u - first[s];
+    const int tile = off / nb, b = off - tile * nb;
+    const int take = min(nb - b, u_end - u);
+    run_tile(s, tile, b, b + take == nb ? INT32_MAX : b + take);
+    __syncthreads();                      // the ring is free again
+    u += take;
+  }
+}
+
+// Joins the parts of the rows whose tile several CTAs had: a = max LSE_c,
+// LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c, in the order of
+// the keys.  A wave takes a (query row, group) and every gridDim.y-th of its
+// heads: lane l has dims 8 (l % 16) .. + 7 of parts l / 16, l / 16 + 4, ...
+__global__ __launch_bounds__(256) void merge_kernel(msa_seqs sq, Plan pl, Parts parts, int rows_per_tile, int H_q, int H_kv,
+                                                    uint16_t* __restrict__ o, float* __restrict__ lse) {
+  constexpr int kBatch = 4;
+  const int lane = lane_id();
+  const int64_t pair = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave;
+  const int64_t row = pair / H_kv;
+  const int r = static_cast<int>(pair % H_kv);
+  if (row >= sq.total_q_rows) return;
+  const int s = find_seq_wave(sq.q_offsets, sq.num_seqs, row);
+  const Steps steps(sq, pl);
+  const SeqGeom g = bounded_geom(sq, s);
+  const int t = static_cast<int>(row - g.q_begin);
+  if (t >= g.q_rows) return;
+  const int G = H_q / H_kv;
+  const int tile = t / pl.qt, in_tile = t - tile * pl.qt;
+  const int qpw = 32 / G;
+  const int p_last = g.kv_len - g.q_rows + min((tile + 1) * pl.qt, g.q_rows) - 1;
+  const int nb = Steps::blocks(g);
+  const int u0 = steps.first(s) + tile * nb;
+  const int visits = p_last < 0 ? 0 : p_last / kSub + 1;
+  const int c0 = u0 / steps.per, c1 = visits < 1 ? c0 : min((u0 + visits - 1) / steps.per, pl.ctas - 1);
+  if (c0 >= c1) return;                  // written by its one CTA
+  const int np = c1 - c0 + 1, d0 = 8 * (lane & 15), l4 = lane >> 4;
+  for (int hh = blockIdx.y; hh < G; hh += gridDim.y) {
+    const int slot = 32 * (in_tile / qpw) + (in_tile % qpw) * G + hh;
+    float a = -INFINITY, sum = 0.f;
+    float out[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int j0 = l4; j0 < np; j0 += 4 * kBatch) {
+      float l[kBatch];
+      f32x4 x[kBatch][2];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const int j = min(j0 + 4 * e, np - 1);
+        const int64_t cta = static_cast<int64_t>(c0 + j) * H_kv + r;
+        const int64_t at = (2 * cta + (j == 0 ? 1 : 0)) * rows_per_tile + slot;
+        l[e] = parts.lse[at];
+        const f32x4* src = reinterpret_cast<const f32x4*>(parts.o + at * kDim + d0);
+        x[e][0] = src[0];
+        x[e][1] = src[1];
+      }
+      float m = a;
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        l[e] = j0 + 4 * e < np ? l[e] : -INFINITY;
+        m = fmaxf(m, l[e]);
+      }
+      if (!(m > -INFINITY)) continue;
+      const float f = a > -INFINITY ? exp2f(a - m) : 0.f;
+      a = m;
+      sum *= f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out[i] *= f;
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        if (!(l[e] > -INFINITY)) continue;      // an empty part does not count
+        const float w = exp2f(l[e] - m);
+        sum += w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[i] = fmaf(w, x[e][i >> 2][i & 3], out[i]);
+      }
+    }
+    // the four lanes of a dim
+    float m = fmaxf(a, __shfl_xor(a, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float f = a > -INFINITY ? exp2f(a - m) : 0.f;
+    auto join = [&](float v) {
+      v *= f;
+      v += __shfl_xor(v, 16);
+      return v + __shfl_xor(v, 32);
+    };
+    sum = join(sum);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = join(out[i]);
+    if (l4 != 0) continue;
+    const bool any = m > -INFINITY;
+    const float inv = any ? 1.f / sum : 0.f;
+    const int64_t head_row = row * H_q + static_cast<int64_t>(r) * G + hh;
+    uint4 w;
+    w.x = pack_bf16x2(out[0] * inv, out[1] * inv);
+    w.y = pack_bf16x2(out[2] * inv, out[3] * inv);
+    w.z = pack_bf16x2(out[4] * inv, out[5] * inv);
+    w.w = pack_bf16x2(out[6] * inv, out[7] * inv);
+    *reinterpret_cast<uint4*>(o + head_row * kDim + d0) = w;
+    if (d0 == 0) lse[head_row] = any ? (m + __log2f(sum)) * kLn_2 : -INFINITY;
+  }
 }
 
 // ---------------------------------------------------------------- host side
@@ -441,6 +676,28 @@ int validate_paged(const msa_seqs* seqs, int H_q, int H_kv, int head_dim) {
   return MSA_OK;
 }
 
+// Waves for the longest sequence's rows, a CTA per tile and group where those
+// are several times what the chip holds at once (one CTA of 8 waves per CU, two
+// of fewer: registers and LDS), else as many CTAs as it holds.
+Plan plan_of(const msa_seqs* seqs, int H_q, int H_kv, int* waves, int64_t* ctas) {
+  const int qpw = 32 / (H_q / H_kv);
+  const int need = (seqs->max_q_rows + qpw - 1) / qpw;
+  *waves = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : 8;
+  Plan pl{};
+  pl.qt = *waves * qpw;
+  int64_t tiles;
+  pl.gr = flash::plan_grid(seqs, pl.qt, seqs->max_q_rows, &tiles);
+  *ctas = tiles * H_kv;
+  const int64_t held = *waves == 8 ? 256 : 512;
+  const int64_t blocks = (static_cast<int64_t>(seqs->max_kv_len) + kSub - 1) / kSub;
+  if (seqs->num_seqs > kMaxSplitSeqs || *ctas >= 4 * held || tiles * blocks >= (int64_t(1) << 30)) return pl;
+  pl.ctas = static_cast<int>(held / H_kv);
+  pl.min_steps = 4;
+  *ctas = static_cast<int64_t>(pl.ctas) * H_kv;
+  return pl;
+}
+size_t part_bytes(int64_t ctas, int waves) { return sizeof(float) * 2 * ctas * 32 * waves * (kDim + 1); }
+
 bool scale_ok(float x) { return x > 0.f && x < 3.0e38f; }   // finite and positive
 
 int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_scale, float k_scale, float v_scale,
@@ -452,26 +709,39 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
   if (seqs->total_q_rows == 0) return MSA_OK;
   if (!q || !k || !v || !o || !lse) return MSA_ERR_INVALID;
   const flash::LogitScale scale = flash::logit_scale(softmax_scale * q_scale * k_scale * kLog2E);
-  const int G = H_q / H_kv;
-  auto launch = [&](auto kernel, auto elem, int waves) -> int {
+  int waves;
+  int64_t ctas;
+  const Plan pl = plan_of(seqs, H_q, H_kv, &waves, &ctas);
+  if (ctas >= (int64_t(1) << 22)) return MSA_ERR_UNSUPPORTED;
+  Parts parts{};
+  if (pl.ctas > 0) {
+    if (!workspace || workspace_bytes < part_bytes(ctas, waves)) return MSA_ERR_WORKSPACE;
+    parts.o = static_cast<float*>(workspace);
+    parts.lse = parts.o + 2 * ctas * 32 * waves * kDim;
+  }
+  auto launch = [&](auto kernel, auto elem) {
     using T = decltype(elem);
-    int64_t tiles;
-    flash::Grid gr = flash::plan_grid(seqs, waves * (32 / G), seqs->max_q_rows, &tiles);
-    if (tiles * H_kv >= (int64_t(1) << 22)) return MSA_ERR_UNSUPPORTED;
-    msa_prof::launch("paged_attn_kernel", kernel, dim3(static_cast<unsigned>(tiles * H_kv)), dim3(waves * kWave), 0, stream,
-                     static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), *seqs, gr, H_q, H_kv,
-                     scale.log2, scale.q_flip, v_scale, static_cast<uint16_t*>(o), lse);
-    return msa_host::launch_status();
+    msa_prof::launch("paged_attn_kernel", kernel, dim3(static_cast<unsigned>(ctas)), dim3(waves * kWave), 0, stream,
+                     static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), *seqs, pl, parts, H_q,
+                     H_kv, scale.log2, scale.q_flip, v_scale, static_cast<uint16_t*>(o), lse);
   };
-  const int waves_needed = (seqs->max_q_rows + 32 / G - 1) / (32 / G);
-  auto pick = [&](auto elem) -> int {
+  auto pick = [&](auto elem) {
     using T = decltype(elem);
-    if (waves_needed <= 1) return launch(paged_attn_kernel<T, 1>, elem, 1);
-    if (waves_needed <= 2) return launch(paged_attn_kernel<T, 2>, elem, 2);
-    if (waves_needed <= 4) return launch(paged_attn_kernel<T, 4>, elem, 4);
-    return launch(paged_attn_kernel<T, 8>, elem, 8);
+    if (waves == 1) launch(paged_attn_kernel<T, 1>, elem);
+    else if (waves == 2) launch(paged_attn_kernel<T, 2>, elem);
+    else if (waves == 4) launch(paged_attn_kernel<T, 4>, elem);
+    else launch(paged_attn_kernel<T, 8>, elem);
   };
-  return fp8 ? pick(uint8_t{}) : pick(uint16_t{});
+  if (fp8) pick(uint8_t{});
+  else pick(uint16_t{});
+  if (pl.ctas > 0) {
+    // a wave per (row, group), or per head where those are few
+    const int64_t pairs = seqs->total_q_rows * H_kv;
+    const int by_head = pairs < 4096 ? H_q / H_kv : 1;
+    msa_prof::launch("paged_merge_kernel", merge_kernel, dim3(static_cast<unsigned>((pairs + 3) / 4), by_head), dim3(256), 0,
+                     stream, *seqs, pl, parts, 32 * waves, H_q, H_kv, static_cast<uint16_t*>(o), lse);
+  }
+  return msa_host::launch_status();
 }
 
 }  // namespace
@@ -479,7 +749,10 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
 extern "C" size_t msa_dense_attn_paged_workspace_size(const msa_seqs* seqs, int num_q_heads, int num_kv_heads,
                                                      int head_dim) {
   if (validate_paged(seqs, num_q_heads, num_kv_heads, head_dim) != MSA_OK) return 0;
-  return 0;
+  int waves;
+  int64_t ctas;
+  const Plan pl = plan_of(seqs, num_q_heads, num_kv_heads, &waves, &ctas);
+  return pl.ctas > 0 ? part_bytes(ctas, waves) : 0;
 }
 
 extern "C" int msa_dense_attn_paged(const void* q, const void* k, const void* v, const msa_seqs* seqs, int num_q_heads,
