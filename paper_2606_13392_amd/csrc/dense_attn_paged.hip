@@ -571,6 +571,284 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   }
 }
 
+// ---------------------------------------------------------------- few rows
+// A tile of at most 32 (query row, head) rows: one token of a sequence, or a
+// few draft rows.  Nothing but the keys' bytes costs then, and the time until
+// the first of them are there: the CTA's four waves take sub-blocks of the same
+// rows in turn, each through registers and LDS of its own (the next sub-block's
+// keys are requested as soon as this one's have left the registers, its values
+// likewise: up to 128 KiB under way per CU), and join their states in LDS.
+constexpr int kRowWaves = 4;
+constexpr int kRedStride = kDim + 4;     // fp32 row stride of the joined rows
+struct WaveBuf {
+  uint16_t k[kSub * kDim];
+  uint16_t v[kSub * kDim];
+};
+static_assert(sizeof(WaveBuf) >= 32 * kRedStride * sizeof(float), "joined rows do not fit");
+
+// Orders a wave's own LDS accesses (they complete in issue order; this keeps
+// the compiler from moving them across).
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, msa_seqs sq, Plan pl, Parts parts, int H_q,
+    int H_kv, float scale_log2, uint32_t q_flip, float o_scale, uint16_t* __restrict__ o, float* __restrict__ lse) {
+  constexpr int MT = kSub / 32, KS = kDim / 16;
+  constexpr int kLanes = kDim * sizeof(T) / 16;        // lanes per key row
+  constexpr int kRows = kWave / kLanes;                // key rows per load instruction
+  constexpr int NL = kSub / kRows;                     // load instructions per sub-block and tensor
+  __shared__ __align__(16) WaveBuf bufs[kRowWaves];
+  __shared__ float state[kRowWaves][2][32];
+  __shared__ int first[kMaxSplitSeqs + 1];
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  const int n = lane & 31, h = lane >> 5;
+  const int G = H_q / H_kv, qpw = 32 / G;
+  const int jq = n / G, hh = n % G;
+  const int r = static_cast<int>(blockIdx.x % H_kv);
+  const int cta = static_cast<int>(blockIdx.x / H_kv);
+  WaveBuf& buf = bufs[wave];
+  const char* kb = reinterpret_cast<const char*>(k + static_cast<int64_t>(r) * kDim);
+  const char* vb = reinterpret_cast<const char*>(v + static_cast<int64_t>(r) * kDim);
+  const uint32_t stride_b = static_cast<uint32_t>(H_kv * kDim * sizeof(T));
+  const int lrow = lane / kLanes, lseg = lane % kLanes;
+  const uint32_t lane_off = lrow * stride_b + 16 * lseg;
+
+  int u, u_end, s;
+  {
+    const Steps steps(sq, pl);
+    u = cta * steps.per;
+    u_end = min(steps.total, u + steps.per);
+    if (u >= u_end) return;
+    s = steps.seq_of(u);
+    if (threadIdx.x < kWave) steps.store(first);
+  }
+  __syncthreads();
+  while (u < u_end) {
+    while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
+    const SeqGeom g = bounded_geom(sq, s);
+    const int nb = Steps::blocks(g), off = u - first[s];
+    const int tile = off / nb, b_begin = off - tile * nb;
+    const int take = min(nb - b_begin, u_end - u);
+    u += take;
+    const int t0 = tile * qpw;
+    const int base_p = g.kv_len - g.q_rows;            // position of the sequence's first query row
+    int t_end = min(t0 + qpw, g.q_rows);
+    t_end = static_cast<int>(min(static_cast<int64_t>(t_end), sq.total_q_rows - g.q_begin));
+    if (t_end <= t0) continue;
+    const int p_last = base_p + t_end - 1;
+    const int b_all = p_last < 0 ? 0 : p_last / kSub + 1;
+    const int b_end = b_begin + take == nb ? b_all : min(b_begin + take, b_all);
+    if (b_begin > 0 && b_begin >= b_end) continue;     // the tile's rows see none of these keys
+    const bool valid = n < qpw * G && t0 + jq < t_end;
+    const int p = valid ? base_p + t0 + jq : -1;
+    const int nfree = (base_p + t0 + 1) / kSub;        // sub-blocks below it need no mask
+
+    bf16x8 bq[KS];
+    {
+      Raw<T> rq[KS];
+      const T* qrow = q + ((static_cast<int64_t>(g.q_begin) + (valid ? t0 + jq : t0)) * H_q + static_cast<int64_t>(r) * G + hh) * kDim + 8 * h;
+#pragma unroll
+      for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
+#pragma unroll
+      for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
+    }
+    PageWindow pw;
+    pw.table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
+    pw.lg_page = 31 - __clz(sq.page_size);
+    pw.lg_unit = min(pw.lg_page, 6);
+    pw.max_page = (sq.total_kv_rows >> pw.lg_page) - 1;
+    pw.units = ((g.kv_len - 1) >> pw.lg_unit) + 1;
+    const int lg_sub = 6 - pw.lg_unit;                 // log2 of units per sub-block
+
+    // whole rows of one sub-block, rows past the sequence's end its last one again
+    auto fetch = [&](const char* base, int sub, u32x4 (&dst)[NL]) {
+      const int key0 = sub * kSub;
+      if (key0 + kSub <= g.kv_len) {
+        if (lg_sub == 0) {
+          const char* blk = base + pw.row(sub) * stride_b;
+#pragma unroll
+          for (int c = 0; c < NL; ++c) dst[c] = *reinterpret_cast<const u32x4*>(blk + c * kRows * stride_b + lane_off);
+        } else {
+#pragma unroll
+          for (int c = 0; c < NL; ++c) {
+            const int in_unit = (c * kRows) & ((1 << pw.lg_unit) - 1);
+            const char* blk = base + (pw.row((sub << lg_sub) + ((c * kRows) >> pw.lg_unit)) + in_unit) * stride_b;
+            dst[c] = *reinterpret_cast<const u32x4*>(blk + lane_off);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < NL; ++c)
+          dst[c] = *reinterpret_cast<const u32x4*>(base + pw.key_row(min(key0 + c * kRows + lrow, g.kv_len - 1)) * stride_b + 16 * lseg);
+      }
+    };
+    auto store = [&](const u32x4 (&src)[NL], bool is_v, uint16_t* dst) {
+#pragma unroll
+      for (int c = 0; c < NL; ++c) {
+        const int ra = c * kRows + lrow;
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<u32x4*>(dst + ra * kDim + 8 * (is_v ? v_seg(ra, lseg) : k_seg(ra, lseg))) = src[c];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int seg = 2 * lseg + e;
+            *reinterpret_cast<u32x4*>(dst + ra * kDim + 8 * (is_v ? v_seg(ra, seg) : k_seg(ra, seg))) =
+                widen(u32x2{src[c][2 * e], src[c][2 * e + 1]});
+          }
+        }
+      }
+    };
+
+    f32x16 acc_o[kDim / 32];
+#pragma unroll
+    for (int i = 0; i < kDim / 32; ++i) acc_o[i] = f32x16{};
+    float m_run = -INFINITY, l_run = 0.f;
+    u32x4 rk[NL], rv[NL];
+    int b = b_begin + wave;
+    if (b < b_end) {
+      pw.start(b << lg_sub);
+      fetch(kb, b, rk);
+      fetch(vb, b, rv);
+    }
+    for (; b < b_end; b += kRowWaves) {
+      pw.advance((b + kRowWaves) << lg_sub);
+      wave_lds_order();
+      store(rk, false, buf.k);
+      if (b + kRowWaves < b_end) fetch(kb, b + kRowWaves, rk);
+      wave_lds_order();
+      // S^T = K Q^T: lane (n, h) gets keys 32i + 8(e/4) + 4h + e%4 of row n
+      f32x16 acc_s[MT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        acc_s[i] = f32x16{};
+#pragma unroll
+        for (int st = 0; st < KS; ++st)
+          acc_s[i] = mfma32x32x16(ld_bf16x8(buf.k + (32 * i + n) * kDim + 8 * k_seg(n, 2 * st + h)), bq[st], acc_s[i]);
+      }
+      if (b >= nfree) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = b * kSub + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
+            acc_s[i][e] = key <= p ? acc_s[i][e] : -INFINITY;
+          }
+      }
+      float bmax = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bmax = fmaxf(bmax, acc_s[i][e]);
+      bmax = fmaxf(bmax, xor32f(bmax));
+      const float m_new = fmaxf(m_run, bmax);
+      const float mm = m_new == -INFINITY ? 0.f : m_new;   // rows with nothing visible yet
+      const float alpha = exp2_hw((m_run - mm) * scale_log2), neg = -mm * scale_log2;
+      float lsum = 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          acc_s[i][e] = exp2_hw(fmaf(acc_s[i][e], scale_log2, neg));
+          lsum += acc_s[i][e];
+        }
+      lsum += xor32f(lsum);
+      l_run = l_run * alpha + lsum;
+      m_run = m_new;
+      if (__ballot(alpha != 1.f)) {
+#pragma unroll
+        for (int i = 0; i < kDim / 32; ++i) acc_o[i] *= alpha;
+      }
+      store(rv, true, buf.v);
+      if (b + kRowWaves < b_end) fetch(vb, b + kRowWaves, rv);
+      wave_lds_order();
+      // O^T += V^T P^T; P^T as the B operand: k-step w covers keys 32(w/2) + 16(w%2) + {4h + e, 8 + 4h + e}
+#pragma unroll
+      for (int w = 0; w < kSub / 16; ++w) {
+        const int i = w >> 1, e0 = 8 * (w & 1);
+        uint4 pw4;
+        pw4.x = pack_bf16x2(acc_s[i][e0 + 0], acc_s[i][e0 + 1]);
+        pw4.y = pack_bf16x2(acc_s[i][e0 + 2], acc_s[i][e0 + 3]);
+        pw4.z = pack_bf16x2(acc_s[i][e0 + 4], acc_s[i][e0 + 5]);
+        pw4.w = pack_bf16x2(acc_s[i][e0 + 6], acc_s[i][e0 + 7]);
+        const int row = 16 * w + 4 * h + ((lane & 15) >> 2);
+#pragma unroll
+        for (int td = 0; td < kDim / 32; ++td) {
+          const int col = 32 * td + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          const uint16_t* a0 = buf.v + row * kDim + 8 * v_seg(row, col >> 3) + (col & 7);
+          const uint2 x0 = lds_tr4(a0), x1 = lds_tr4(a0 + 8 * kDim);   // rows + 8: same permutation
+          acc_o[td] = mfma32x32x16(__builtin_bit_cast(bf16x8, make_uint4(x0.x, x0.y, x1.x, x1.y)),
+                                   __builtin_bit_cast(bf16x8, pw4), acc_o[td]);
+        }
+      }
+    }
+    // join: M = max m_w, L = sum l_w 2^(m_w - M), O = sum 2^(m_w - M) acc_w / L
+    if (h == 0) {
+      state[wave][0][n] = m_run;
+      state[wave][1][n] = l_run;
+    }
+    __syncthreads();
+    auto top = [&](int c) {
+      float m = state[0][0][c];
+#pragma unroll
+      for (int w = 1; w < kRowWaves; ++w) m = fmaxf(m, state[w][0][c]);
+      return m;
+    };
+    {
+      const float f = m_run > -INFINITY ? exp2_hw((m_run - top(n)) * scale_log2) : 0.f;
+      float* red = reinterpret_cast<float*>(&buf) + n * kRedStride + 4 * h;
+#pragma unroll
+      for (int td = 0; td < kDim / 32; ++td)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+          *reinterpret_cast<f32x4*>(red + 32 * td + 8 * e4) =
+              f32x4{acc_o[td][4 * e4], acc_o[td][4 * e4 + 1], acc_o[td][4 * e4 + 2], acc_o[td][4 * e4 + 3]} * f;
+    }
+    __syncthreads();
+    const int c = threadIdx.x >> 3, d0 = 16 * (threadIdx.x & 7);   // row c, dims d0 .. d0 + 15
+    if (c < (t_end - t0) * G) {
+      const float M = top(c);
+      float L = 0.f;
+      f32x4 x[4] = {};
+#pragma unroll
+      for (int w = 0; w < kRowWaves; ++w) {
+        const float mw = state[w][0][c];
+        L += mw > -INFINITY ? state[w][1][c] * exp2_hw((mw - M) * scale_log2) : 0.f;
+        const float* red = reinterpret_cast<const float*>(&bufs[w]) + c * kRedStride + d0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += *reinterpret_cast<const f32x4*>(red + 4 * i);
+      }
+      const bool empty = !(L > 0.f);
+      const float inv_l = empty ? 0.f : o_scale / L;
+      const float lse2 = empty ? -INFINITY : M * scale_log2 + __log2f(L);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] *= inv_l;
+      if (b_begin > 0 || b_end < b_all) {
+        const int64_t row = (2 * static_cast<int64_t>(blockIdx.x) + (b_begin > 0 ? 0 : 1)) * 32 + c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(parts.o + row * kDim + d0 + 4 * i) = x[i];
+        if (d0 == 0) parts.lse[row] = lse2;
+      } else {
+        const int64_t head_row = (static_cast<int64_t>(g.q_begin) + t0 + c / G) * H_q + static_cast<int64_t>(r) * G + c % G;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint4 w;
+          w.x = pack_bf16x2(x[2 * i][0], x[2 * i][1]);
+          w.y = pack_bf16x2(x[2 * i][2], x[2 * i][3]);
+          w.z = pack_bf16x2(x[2 * i + 1][0], x[2 * i + 1][1]);
+          w.w = pack_bf16x2(x[2 * i + 1][2], x[2 * i + 1][3]);
+          *reinterpret_cast<uint4*>(o + head_row * kDim + d0 + 8 * i) = w;
+        }
+        if (d0 == 0) lse[head_row] = lse2 * kLn_2;
+      }
+    }
+    __syncthreads();                      // the areas are free again
+  }
+}
+
 // Joins the parts of the rows whose tile several CTAs had: a = max LSE_c,
 // LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c, in the order of
 // the keys.  A wave takes a (query row, group) and every gridDim.y-th of its
@@ -688,7 +966,7 @@ Plan plan_of(const msa_seqs* seqs, int H_q, int H_kv, int* waves, int64_t* ctas)
   int64_t tiles;
   pl.gr = flash::plan_grid(seqs, pl.qt, seqs->max_q_rows, &tiles);
   *ctas = tiles * H_kv;
-  const int64_t held = *waves == 8 ? 256 : 512;
+  const int64_t held = *waves == 8 || *waves == 1 ? 256 : 512;
   const int64_t blocks = (static_cast<int64_t>(seqs->max_kv_len) + kSub - 1) / kSub;
   if (seqs->num_seqs > kMaxSplitSeqs || *ctas >= 4 * held || tiles * blocks >= (int64_t(1) << 30)) return pl;
   pl.ctas = static_cast<int>(held / H_kv);
@@ -719,15 +997,17 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
     parts.o = static_cast<float*>(workspace);
     parts.lse = parts.o + 2 * ctas * 32 * waves * kDim;
   }
-  auto launch = [&](auto kernel, auto elem) {
+  auto launch = [&](auto kernel, auto elem, int cta_waves = 0) {
     using T = decltype(elem);
-    msa_prof::launch("paged_attn_kernel", kernel, dim3(static_cast<unsigned>(ctas)), dim3(waves * kWave), 0, stream,
-                     static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), *seqs, pl, parts, H_q,
-                     H_kv, scale.log2, scale.q_flip, v_scale, static_cast<uint16_t*>(o), lse);
+    msa_prof::launch("paged_attn_kernel", kernel, dim3(static_cast<unsigned>(ctas)),
+                     dim3((cta_waves > 0 ? cta_waves : waves) * kWave), 0, stream, static_cast<const T*>(q),
+                     static_cast<const T*>(k), static_cast<const T*>(v), *seqs, pl, parts, H_q, H_kv, scale.log2,
+                     scale.q_flip, v_scale, static_cast<uint16_t*>(o), lse);
   };
   auto pick = [&](auto elem) {
     using T = decltype(elem);
-    if (waves == 1) launch(paged_attn_kernel<T, 1>, elem);
+    if (waves == 1 && pl.ctas > 0) launch(paged_rows_kernel<T>, elem, kRowWaves);
+    else if (waves == 1) launch(paged_attn_kernel<T, 1>, elem);
     else if (waves == 2) launch(paged_attn_kernel<T, 2>, elem);
     else if (waves == 4) launch(paged_attn_kernel<T, 4>, elem);
     else launch(paged_attn_kernel<T, 8>, elem);

@@ -404,26 +404,39 @@ __global__ __launch_bounds__(kThreads) void norm_rope_backward_kernel(Parts a, m
   }
 }
 
-// d w = sum of the CTAs' partials: a CTA of 256 threads takes 16 elements, 16
-// threads each, which are added in a fixed order.
-__global__ __launch_bounds__(256) void norm_grad_kernel(const float* __restrict__ dw_part, int ctas, int D, float* dq_w,
-                                                        float* dk_w) {
-  __shared__ float red[16][17];
+// d w = sum of the CTAs' partials: a CTA takes 16 elements, 64 threads each,
+// which are added in a fixed order.  (16 threads per element, whose 64 reads
+// waited for one another, took 20 us.)
+constexpr int kGradThreads = 1024;
+__global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(const float* __restrict__ dw_part, int ctas, int D,
+                                                                 float* dq_w, float* dk_w) {
+  constexpr int kRows = kGradThreads / 16, kBatch = 4;
+  __shared__ float red[kRows][17];
   const int i = blockIdx.y;
   float* out = i ? dk_w : dq_w;
+  if (!out) return;                      // uniform over the CTA
   const int e = threadIdx.x & 15, j = threadIdx.x >> 4;
   const int col = blockIdx.x * 16 + e;
   float sum = 0.f;
-  if (out)
-    for (int c = j; c < ctas; c += 16) sum += dw_part[(static_cast<int64_t>(c) * 2 + i) * D + col];
+  for (int c0 = j; c0 < ctas; c0 += kRows * kBatch) {
+    float x[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int c = c0 + u * kRows;
+      x[u] = dw_part[(static_cast<int64_t>(min(c, ctas - 1)) * 2 + i) * D + col];
+      x[u] = c < ctas ? x[u] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) sum += x[u];
+  }
   red[j][e] = sum;
   __syncthreads();
-  if (out && j == 0) {
-    float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += red[k][e];
-    out[col] = s;
+  for (int d = kRows / 2; d > 0; d /= 2) {
+    if (j < d) red[j][e] += red[j + d][e];
+    __syncthreads();
   }
+  if (j == 0) out[col] = red[0][e];
 }
 
 // ---------------------------------------------------------------- host side
@@ -478,11 +491,13 @@ int64_t iterations(const Parts& a, int nparts, int64_t rows) {
 }
 
 // Rows per CTA: enough for 16 iterations (the angles, the search for the rows'
-// sequences and the weights are shared by them) while at least 2048 CTAs, eight
-// per CU, are left.
-int rows_per_cta(const Parts& a, int nparts, int64_t total) {
+// sequences and the weights are shared by them) while there are more than
+// `ctas` CTAs.  Forward: 2048, eight per CU, which run at once (3929 rows of 64
+// + 4 heads into E4M3 24.7 us; with 1024 26.4, with 4096 26.0).
+constexpr int kCtas = 2048;
+int rows_per_cta(const Parts& a, int nparts, int64_t total, int ctas) {
   int rows = 1;
-  while (rows < kMaxRows && iterations(a, nparts, rows) < 16 && (total + 2 * rows - 1) / (2 * rows) >= 2048) rows *= 2;
+  while (rows < kMaxRows && iterations(a, nparts, rows) < 16 && (total + rows - 1) / rows > ctas) rows *= 2;
   return rows;
 }
 
@@ -490,7 +505,7 @@ size_t angle_bytes(const Parts& a) { return sizeof(float) * 2 * a.rows * (a.spec
 
 template <int NPARTS, bool CACHE>
 int launch_forward(const char* name, Parts a, const msa_seqs* seqs, hipStream_t stream) {
-  a.rows = rows_per_cta(a, NPARTS, seqs->total_q_rows);
+  a.rows = rows_per_cta(a, NPARTS, seqs->total_q_rows, kCtas);
   const int64_t tiles = (seqs->total_q_rows + a.rows - 1) / a.rows;
   if (tiles >= (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;   // a grid's limit
   // few rows: a row's iterations go to several CTAs, up to 1024 in all
@@ -652,7 +667,7 @@ extern "C" int msa_qk_norm_rope_backward(const void* q, int64_t q_stride, const 
     a.part[i] = part_of(in[i].x, in[i].stride, in[i].heads, head_dim, in[i].w, in[i].d, in[i].d_stride, spec);
     a.part[i].g = static_cast<const uint16_t*>(in[i].g);
   }
-  a.rows = rows_per_cta(a, 2, seqs->total_q_rows);
+  a.rows = rows_per_cta(a, 2, seqs->total_q_rows, kGradCtas);
   const int64_t ctas = grad_ctas(seqs, a);
   auto* part = static_cast<float*>(workspace);
   if (ctas > 0)
@@ -661,7 +676,7 @@ extern "C" int msa_qk_norm_rope_backward(const void* q, int64_t q_stride, const 
   float* dqw = num_q_heads > 0 ? d_q_weight : nullptr;
   float* dkw = num_kv_heads > 0 ? d_k_weight : nullptr;
   if (dqw || dkw)
-    msa_prof::launch("norm_grad_kernel", norm_grad_kernel, dim3(head_dim / 16, 2), dim3(256), 0, stream,
+    msa_prof::launch("norm_grad_kernel", norm_grad_kernel, dim3(head_dim / 16, 2), dim3(kGradThreads), 0, stream,
                      static_cast<const float*>(part), static_cast<int>(ctas), head_dim, dqw, dkw);
   return msa_host::launch_status();
 }

@@ -150,7 +150,7 @@ def _stream() -> int:
 def _call(name: str, device: torch.device, *args) -> None:
     """The library's call ``name`` with the current stream of ``device`` as its last argument, whichever device is
     current."""
-    fn, cur = getattr(lib(), name), torch.cuda.current_device()
+    fn, cur = getattr(_lib or lib(), name), torch._C._cuda_getDevice()
     if cur == device.index:
         st = fn(*args, torch._C._cuda_getCurrentRawStream(cur))
     else:
@@ -462,9 +462,10 @@ class Rope:
         _need(inv_freq, "inv_freq", torch.float64, tuple(inv_freq.shape), inv_freq.device)
         self.inv_freq = inv_freq
         self.c = MsaRopeC(2 * inv_freq.numel(), 1 if interleaved else 0, float(scale), inv_freq.data_ptr())
+        self._ref = ctypes.byref(self.c)
 
     def ref(self):
-        return ctypes.byref(self.c)
+        return self._ref
 
 
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -501,18 +502,19 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
 
 
 def _heads(t: torch.Tensor, name: str, rows: int, device):
-    """Heads of a [rows, heads, dim] bf16 tensor whose rows may be apart (columns of a wider one)."""
+    """(heads, row stride) of a [rows, heads, dim] bf16 tensor whose rows may be apart (columns of a wider one)."""
+    shape = t.shape
+    if t.dtype == torch.bfloat16 and len(shape) == 3 and shape[0] == rows and t.device == device:
+        stride = t.stride()
+        _, h, d = shape
+        if (stride[2] == 1 or d == 1) and (stride[1] == d or h == 1):
+            return h, (stride[0] if rows > 1 else h * d)
+        raise ValueError(f"{name}: a row's heads must be contiguous")
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
-    if t.dim() != 3 or t.shape[0] != rows:
-        raise ValueError(f"{name}: expected shape ({rows}, heads, dim), got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name}: expected device {device}, got {t.device}")
-    _, h, d = t.shape
-    sr, sh, sd = t.stride()
-    if (sd != 1 and d != 1) or (sh != d and h != 1):
-        raise ValueError(f"{name}: a row's heads must be contiguous")
-    return h, (sr if rows > 1 else h * d)
+    raise ValueError(f"{name}: expected shape ({rows}, heads, dim), got {tuple(shape)}")
 
 
 def _weight(w: Optional[torch.Tensor], name: str, dim: int, device):
@@ -527,7 +529,7 @@ def _rope(rope: Optional[Rope], device):
         return None
     if rope.inv_freq.device != device:
         raise ValueError(f"rope: expected device {device}, got {rope.inv_freq.device}")
-    return ctypes.byref(rope.c)
+    return rope.ref()
 
 
 def _norm_rope(fp8, q, k, scales, seqs: Seqs, rope, q_weight, k_weight, eps, q_out, k_out):
@@ -541,20 +543,21 @@ def _norm_rope(fp8, q, k, scales, seqs: Seqs, rope, q_weight, k_weight, eps, q_o
             raise ValueError(f"k: expected head size {d}, got {k.shape[2]}")
     dtype = torch.uint8 if fp8 else torch.bfloat16
     if q_out is None:
-        q_out = torch.empty((T, H_q, d), dtype=dtype, device=dev)
+        q_out = torch.empty(T, H_q, d, dtype=dtype, device=dev)
     else:
         _need(q_out, "q_out", dtype, (T, H_q, d), dev)
-    if k is not None and k_out is None:
-        k_out = torch.empty((T, H_kv, d), dtype=dtype, device=dev)
-    elif k_out is not None:
+    if k_out is not None:
         _need(k_out, "k_out", dtype, (T, H_kv, d), dev)
-    args = (seqs.ref(), H_q, H_kv, d, _weight(q_weight, "q_weight", d, dev), _weight(k_weight, "k_weight", d, dev),
-            float(eps), _rope(rope, dev), q_out.data_ptr(), _ptr(k_out))
+    elif k is not None:
+        k_out = torch.empty(T, H_kv, d, dtype=dtype, device=dev)
+    shared = (seqs.ref(), H_q, H_kv, d, _weight(q_weight, "q_weight", d, dev), _weight(k_weight, "k_weight", d, dev), float(eps),
+              _rope(rope, dev), q_out.data_ptr(), None if k_out is None else k_out.data_ptr())
+    k_ptr = None if k is None else k.data_ptr()
     if fp8:
-        qs, ks = scales
-        _call("msa_qk_norm_rope_fp8", dev, q.data_ptr(), q_stride, _ptr(k), k_stride, float(qs), float(ks), *args)
+        q_scale, k_scale = scales
+        _call("msa_qk_norm_rope_fp8", dev, q.data_ptr(), q_stride, k_ptr, k_stride, float(q_scale), float(k_scale), *shared)
     else:
-        _call("msa_qk_norm_rope", dev, q.data_ptr(), q_stride, _ptr(k), k_stride, *args)
+        _call("msa_qk_norm_rope", dev, q.data_ptr(), q_stride, k_ptr, k_stride, *shared)
     return q_out, k_out
 
 
@@ -641,17 +644,23 @@ def _append(fp8, k, v, scales, seqs: Seqs, rope, k_cache, v_cache, k_weight, eps
         if index_k.dim() != 2:
             raise ValueError(f"index_k: expected shape ({T}, d_idx), got {tuple(index_k.shape)}")
         d_idx = index_k.shape[1]
-        _, i_stride = _heads(index_k.unsqueeze(1), "index_k", T, dev)
+        if index_k.dtype != torch.bfloat16:
+            raise TypeError(f"index_k: expected torch.bfloat16, got {index_k.dtype}")
+        if index_k.shape[0] != T or index_k.device != dev:
+            raise ValueError(f"index_k: expected {T} rows on {dev}, got {index_k.shape[0]} on {index_k.device}")
+        if index_k.stride(1) != 1 and d_idx != 1:
+            raise ValueError("index_k: a row must be contiguous")
+        i_stride = index_k.stride(0) if T > 1 else d_idx
         _need(index_k_cache, "index_k_cache", torch.bfloat16, (seqs.total_kv_rows, d_idx), dev)
         iw = _weight(index_k_weight, "index_k_weight", d_idx, dev)
         ir = _rope(index_rope, dev)
-    args = (_ptr(index_k), i_stride, seqs.ref(), H_kv, d, d_idx, _weight(k_weight, "k_weight", d, dev), iw, float(eps),
-            _rope(rope, dev), ir, k_cache.data_ptr(), v_cache.data_ptr(), _ptr(index_k_cache))
+    shared = (_ptr(index_k), i_stride, seqs.ref(), H_kv, d, d_idx, _weight(k_weight, "k_weight", d, dev), iw, float(eps),
+              _rope(rope, dev), ir, k_cache.data_ptr(), v_cache.data_ptr(), _ptr(index_k_cache))
     if fp8:
-        ks, vs = scales
-        _call("msa_kv_append_fp8", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, float(ks), float(vs), *args)
+        k_scale, v_scale = scales
+        _call("msa_kv_append_fp8", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, float(k_scale), float(v_scale), *shared)
     else:
-        _call("msa_kv_append", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, *args)
+        _call("msa_kv_append", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, *shared)
 
 
 def kv_append(k, v, seqs: Seqs, rope: Optional[Rope], k_cache, v_cache, k_weight=None, eps: float = 1e-6, index_k=None,
