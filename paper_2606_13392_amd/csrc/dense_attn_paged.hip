@@ -3,7 +3,7 @@
 // one token per sequence; bf16 or E4M3.
 //
 // A CTA owns one KV group and a tile of consecutive query rows of one sequence
-// (each of its 1, 2, 4 or 8 waves holds 32 (query row, head) rows) and streams
+// (each of its 2, 4 or 8 waves holds 32 (query row, head) rows) and streams
 // the sequence's keys, 64 at a time, through a double-buffered LDS ring one
 // sub-block ahead: S^T = K Q^T and O^T += V^T P^T on MFMA 32x32x16, the online
 // softmax of one sub-block between the O MFMAs of the one before (running
@@ -22,14 +22,20 @@
 //
 // Pages: 16 .. 8192 rows, a power of two.  Each lane holds the place of one
 // unit of min(page, 64) rows of the sequence, so 64 units' page ids arrive
-// with one load, a window ahead of their use, and a copy's scalar base comes
-// from a lane read.  Rows past the end of the sequence are never read.
+// with one load, a window ahead of their use, and a sub-block's place comes
+// from a lane read (pages of 64 rows and more) or a lane exchange (smaller
+// ones).  Rows past the end of the sequence are never read: they repeat its
+// last one, whose value is finite, at weight zero.
+//
+// E4M3 codes are widened to bf16, which is exact, on their way into LDS.  The
+// 8-bit MFMA (32x32x64, twice the bf16 rate) on the codes themselves drops
+// product bits some 2^-13 below the largest: LSE was off by up to 1.0e-4 on
+// sequences of 5 - 34 keys (bf16: 1e-6).
 #include "flash_tile.h"
 
 namespace {
 
 using namespace msa;
-using flash::add_bf16_pair;
 using flash::dma16;
 using flash::kAhead;
 using flash::kDim;
@@ -43,46 +49,52 @@ using flash::v_seg;
 using flash::xor32f;
 
 // Places of a sequence's key rows in the pool, in units of min(page, 64) rows:
-// a window of 64 units and the one behind it, one unit per lane.
+// a window of 64 units, one per lane, and the one behind it.  SMALL: pages of
+// fewer than 64 rows.
+template <bool SMALL>
 struct PageWindow {
   const int32_t* table;                  // the sequence's block-table row
   int lg_unit, lg_page;
   int units;                             // units of the sequence
-  int64_t max_page;
+  int max_page;
   int w0;                                // first unit of `cur`
-  uint32_t cur, nxt;                     // first row of the lane's unit / 16
+  int cur, nxt;                          // first row of the lane's unit
 
-  __device__ __forceinline__ uint32_t fetch(int unit) const {
-    const int u = min(unit, units - 1);
-    const int key = u << lg_unit;
-    int64_t page = table[key >> lg_page];
-    page = page < 0 ? 0 : (page > max_page ? max_page : page);
-    return static_cast<uint32_t>(((page << lg_page) + (key & ((1 << lg_page) - 1))) >> 4);
+  __device__ __forceinline__ PageWindow(const msa_seqs& sq, int s, int kv_len) {
+    table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
+    lg_page = 31 - __clz(sq.page_size);
+    lg_unit = SMALL ? lg_page : 6;
+    max_page = static_cast<int>(sq.total_kv_rows >> lg_page) - 1;
+    units = ((kv_len - 1) >> lg_unit) + 1;
   }
-  __device__ __forceinline__ void start(int unit) {
-    w0 = unit;
+  __device__ __forceinline__ int fetch(int unit) const {
+    const int key = min(unit, units - 1) << lg_unit;
+    const int page = min(max(table[key >> lg_page], 0), max_page);
+    return (page << lg_page) + (key & ((1 << lg_page) - 1));
+  }
+  // sub-blocks from `sub` on; the sequence is not empty
+  __device__ __forceinline__ void start(int sub) {
+    w0 = sub << (6 - lg_unit);
     cur = fetch(w0 + lane_id());
     nxt = fetch(w0 + kWave + lane_id());
   }
-  // to be called before units from `unit` on are asked for
-  __device__ __forceinline__ void advance(int unit) {
-    if (unit - w0 >= kWave) {
+  // Sub-block `sub`, at most 64 units past the last one asked for.  The place
+  // of its row `row`: SMALL a row of the pool, each lane its own; else that of
+  // the sub-block's first row, the same in every lane.
+  __device__ __forceinline__ void advance(int sub) {
+    if ((sub << (6 - lg_unit)) - w0 >= kWave) {
       w0 += kWave;
       cur = nxt;
       nxt = fetch(w0 + kWave + lane_id());
     }
   }
-  // first row of a unit at most 127 past w0: the same unit in every lane
-  __device__ __forceinline__ int64_t row(int unit) const {
-    const int i = unit - w0;
-    const uint32_t x = i < kWave ? __builtin_amdgcn_readlane(cur, i) : __builtin_amdgcn_readlane(nxt, i - kWave);
-    return static_cast<int64_t>(x) << 4;
-  }
-  // a key's row, each lane its own
-  __device__ __forceinline__ int64_t key_row(int key) const {
-    const int i = (key >> lg_unit) - w0;
-    const uint32_t a = __shfl(static_cast<int>(cur), i & 63), b = __shfl(static_cast<int>(nxt), i & 63);
-    return (static_cast<int64_t>(i < kWave ? a : b) << 4) + (key & ((1 << lg_unit) - 1));
+  __device__ __forceinline__ int place(int sub, int row) const {
+    if constexpr (SMALL) {
+      const int key = sub * kSub + row;
+      return __shfl(cur, (key >> lg_unit) - w0) + (key & ((1 << lg_unit) - 1));
+    } else {
+      return __builtin_amdgcn_readlane(cur, sub - w0);
+    }
   }
 };
 
@@ -175,17 +187,42 @@ struct Parts {
   float* lse;                            // [CTA][2][rows], base 2
 };
 
+// Sub-block `sub` of a sequence's keys, as N of a thread's pieces see it.
+template <bool SMALL, int N>
+struct Rows {
+  int at[SMALL ? N : 1];                 // SMALL: the pieces' rows in the pool; else the first row
+  int last;                              // last row of the sub-block that the sequence has
+
+  // row_of(c): the row of piece c
+  template <typename F>
+  __device__ __forceinline__ void find(PageWindow<SMALL>& pw, int sub, int kv_len, F row_of) {
+    pw.advance(sub);
+    last = kv_len - 1 - sub * kSub;
+    if constexpr (SMALL) {
+#pragma unroll
+      for (int c = 0; c < N; ++c) at[c] = pw.place(sub, min(row_of(c), last));
+    } else {
+      at[0] = pw.place(sub, 0);
+    }
+  }
+  __device__ __forceinline__ const char* ptr(const char* base, uint32_t stride_b, int c, int row) const {
+    if constexpr (SMALL) return base + static_cast<int64_t>(at[c]) * stride_b;
+    else return base + static_cast<int64_t>(at[0]) * stride_b + static_cast<uint32_t>(min(row, last)) * stride_b;
+  }
+};
+
 // T: uint16_t = bf16 bits, uint8_t = E4M3 codes (o_scale multiplies O).
-template <typename T, int WAVES>
+template <typename T, int WAVES, bool SMALL>
 __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, msa_seqs sq, Plan pl, Parts parts, int H_q,
     int H_kv, float scale_log2, uint32_t q_flip, float o_scale, uint16_t* __restrict__ o, float* __restrict__ lse) {
   constexpr int kThreads = WAVES * kWave;
+  constexpr bool kCodes = sizeof(T) == 1;
   constexpr int MT = kSub / 32;            // 32-key tiles of S^T
-  constexpr int KS = kDim / 16;            // k-steps of S^T = K Q^T
-  constexpr bool kDma = sizeof(T) == 2;
-  constexpr int NDMA = kSub / 4 / WAVES;   // DMA instructions per wave per sub-block and tensor
-  constexpr int NRAW = kSub * kDim / 16 / kThreads;   // E4M3: 16-byte pieces per thread and tensor
+  constexpr int KS = kDim / 16;            // bf16: k-steps of S^T = K Q^T
+  constexpr int kSegs = kDim * sizeof(T) / 16;        // 16-byte segments of a key row
+  constexpr int N = kSub * kSegs / kThreads;          // pieces of 16 bytes per thread, sub-block and tensor
+  constexpr int kPieceRows = kWave / kSegs;           // rows of a wave's piece
   __shared__ __align__(16) Ring ring;
   __shared__ int first[kMaxSplitSeqs + 1];
   const int lane = lane_id();
@@ -197,377 +234,350 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   const int jq = n / G, hh = n % G;
   const int r = static_cast<int>(blockIdx.x % H_kv);
   const int cta = static_cast<int>(blockIdx.x / H_kv);
-
-  const int64_t stride = static_cast<int64_t>(H_kv) * kDim;
   const char* kb = reinterpret_cast<const char*>(k + static_cast<int64_t>(r) * kDim);
   const char* vb = reinterpret_cast<const char*>(v + static_cast<int64_t>(r) * kDim);
-  const uint32_t stride_b = static_cast<uint32_t>(stride * sizeof(T));
-  flash::LaneOffsets<NDMA> lo;
+  const uint32_t stride_b = static_cast<uint32_t>(H_kv * kDim * sizeof(T));
+
+  // A thread's pieces: row piece_row(c) and a 16-byte segment.  By DMA lane l's
+  // piece lands at 16 l of its wave's, so it takes the segment that the row's
+  // permutation stores there (the permutations are involutions).
+  auto piece_row = [&](int c) { return kPieceRows * (c * WAVES + wave) + lane / kSegs; };
+  uint32_t kseg[N], vseg[N];
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    const int ra = piece_row(c), sg = lane % kSegs;
+    kseg[c] = 16 * (kCodes ? sg : k_seg(ra, sg));
+    vseg[c] = 16 * (kCodes ? sg : v_seg(ra, sg));
+  }
+  // MFMA operand reads, relative to a ring buffer
+  uint32_t ks_at[KS], vs_at[kDim / 32];
+#pragma unroll
+  for (int st = 0; st < KS; ++st) ks_at[st] = 2 * (n * kDim + 8 * k_seg(n, 2 * st + h));
   {
+    // V^T operand: in each 16-lane group, lane j addresses row k0 + j/4, dims
+    // n0 + 4(j%4) .. +3 of V and receives rows k0 .. k0+3 of dim n0 + j
     const int gq = lane >> 4, jj = lane & 15;
-#pragma unroll
-    for (int c = 0; c < NDMA; ++c) {
-      const int ra = 4 * (c * WAVES + wave) + gq;
-      lo.kg[c] = ra * stride_b + 16 * k_seg(ra, jj);        // the permutations are involutions
-      lo.vg[c] = ra * stride_b + 16 * v_seg(ra, jj);
-    }
-#pragma unroll
-    for (int st = 0; st < KS; ++st) lo.ks[st] = 2 * (n * kDim + 8 * k_seg(n, 2 * st + h));
     const int rl = 4 * h + (jj >> 2);
 #pragma unroll
     for (int td = 0; td < kDim / 32; ++td) {
       const int col = 32 * td + 16 * (gq & 1) + 4 * (jj & 3);
-      lo.vs[td] = 2 * (rl * kDim + 8 * v_seg(rl, col >> 3) + (col & 7));
+      vs_at[td] = 2 * (rl * kDim + 8 * v_seg(rl, col >> 3) + (col & 7));
     }
   }
-  // Sub-blocks b_from .. b_to - 1 of one tile of sequence s (b_to past its
-  // last: to its end), into O and LSE or, if that is not all of them, a part.
-  auto run_tile = [&](int s, int tile, int b_from, int b_to) __attribute__((always_inline)) {
-  const SeqGeom g = bounded_geom(sq, s);
-  const int t0 = tile * qt;
-  const int base_p = g.kv_len - g.q_rows;  // position of the sequence's first query row
-  int t_end = min(t0 + qt, g.q_rows);
-  t_end = static_cast<int>(min(static_cast<int64_t>(t_end), sq.total_q_rows - g.q_begin));
-  if (t_end <= t0) return;                                // uniform over the CTA
-  const int p_last = base_p + t_end - 1;
-  const int t = t0 + wave * qpw + jq;                     // this lane's query row in the sequence
-  const bool valid = n < qpw * G && t < t_end;
-  const int p = valid ? base_p + t : -1;
-  const bool live = t0 + wave * qpw < t_end;              // the wave has rows
-  // sub-blocks below nfree are visible to every row of the wave and need no mask
-  const int nfree = (base_p + min(t0 + wave * qpw, t_end - 1) + 1) / kSub;
-  const int64_t head_row = (static_cast<int64_t>(g.q_begin) + (valid ? t : t0)) * H_q + static_cast<int64_t>(r) * G + hh;
-  const int b_all = p_last < 0 ? 0 : p_last / kSub + 1;
-  const int b_begin = b_from, b_end = min(b_to, b_all);
-  if (b_begin > 0 && b_begin >= b_end) return;            // the tile's rows see none of these keys
 
-  Raw<T> rq[KS];
-  {
-    const T* qrow = q + head_row * kDim + 8 * h;
-#pragma unroll
-    for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
-  }
-  PageWindow pw;
-  pw.table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
-  pw.lg_page = 31 - __clz(sq.page_size);
-  pw.lg_unit = min(pw.lg_page, 6);
-  pw.max_page = (sq.total_kv_rows >> pw.lg_page) - 1;
-  pw.units = ((g.kv_len - 1) >> pw.lg_unit) + 1;
-  const int lg_sub = 6 - pw.lg_unit;       // log2 of units per sub-block
-
-  // First byte of the rows of a sub-block, as seen from row `first` of it (the
-  // unit that `first` lies in): base of offsets row * stride_b.
-  auto base_of = [&](const char* base, int sub, int first) -> const char* {
-    const int unit = (sub << lg_sub) + (first >> pw.lg_unit);
-    const int64_t row0 = pw.row(unit) - ((first >> pw.lg_unit) << pw.lg_unit);
-    return base + row0 * stride_b;
-  };
-  // One sub-block (K or V) into LDS by DMA: each wave instruction fills 4 rows
-  // (1 KiB); lane l takes row 4 piece + l / 16 and the logical segment that the
-  // row's permutation stores at physical segment l % 16.  In a sub-block running
-  // past kv_len the missing rows re-read the last key (finite values whose
-  // scores are masked).
-  auto dma = [&](const char* base, const uint32_t (&go)[NDMA], bool is_v, int sub, uint16_t* dst) {
-    const int key0 = sub * kSub;
-    if (key0 + kSub <= g.kv_len) {
-      const char* blk = base_of(base, sub, 0);
-#pragma unroll
-      for (int c = 0; c < NDMA; ++c) {
-        const int first = 4 * (c * WAVES + wave);
-        if (lg_sub != 0) blk = base_of(base, sub, __builtin_amdgcn_readfirstlane(first));
-        dma16(blk + go[c], dst + first * kDim);
-      }
-    } else {
-#pragma unroll 1
-      for (int c = 0; c < NDMA; ++c) {
-        const int ra = 4 * (c * WAVES + wave) + (lane >> 4);
-        const int64_t row = pw.key_row(min(key0 + ra, g.kv_len - 1));
-        const int seg = is_v ? v_seg(ra, lane & 15) : k_seg(ra, lane & 15);
-        dma16(base + row * stride_b + 16 * seg, dst + 4 * (c * WAVES + wave) * kDim);
-      }
-    }
-  };
-  // The same through registers for E4M3: whole 128-byte rows, 16 codes per
-  // lane; stored widened to bf16.
-  u32x4 rk[NRAW], rv[NRAW];
-  auto fetch = [&](const char* base, int sub, u32x4 (&dst)[NRAW]) {
-    const int key0 = sub * kSub;
-#pragma unroll
-    for (int i = 0; i < NRAW; ++i) {
-      const int c = threadIdx.x + kThreads * i;
-      const char* src;
-      if (key0 + kSub <= g.kv_len) {
-        src = base_of(base, sub, __builtin_amdgcn_readfirstlane(c >> 3)) + (c >> 3) * stride_b;
-      } else {
-        src = base + pw.key_row(min(key0 + (c >> 3), g.kv_len - 1)) * stride_b;
-      }
-      dst[i] = *reinterpret_cast<const u32x4*>(src + 16 * (c & 7));
-    }
-  };
-  auto store = [&](const u32x4 (&src)[NRAW], bool is_v, uint16_t* dst) {
-#pragma unroll
-    for (int i = 0; i < NRAW; ++i) {
-      const int c = threadIdx.x + kThreads * i;
-      const int ra = c >> 3;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int seg = 2 * (c & 7) + e;
-        *reinterpret_cast<u32x4*>(dst + ra * kDim + 8 * (is_v ? v_seg(ra, seg) : k_seg(ra, seg))) =
-            widen(u32x2{src[i][2 * e], src[i][2 * e + 1]});
-      }
-    }
-  };
-
-  bf16x8 bq[KS];
-  f32x16 acc_o[kDim / 32];
-#pragma unroll
-  for (int i = 0; i < kDim / 32; ++i) acc_o[i] = f32x16{};
-  float m_run = -INFINITY, l_run = 0.f;
-  // P of the pending sub-block in bf16, as the B operand of O^T = V^T P^T:
-  // k-step u covers keys 32(u/2) + 16(u%2) + {4h + e, 8 + 4h + e}, e = 0..3
-  bf16x8 bp[kSub / 16];
-  float alpha_pend = 0.f;                 // alpha of the sub-block whose P is in bp
-
-  // S^T = K Q^T on one sub-block: lane (n, h) gets keys 32i + 8(e/4) + 4h + e%4
-  // of row n.  16 MFMA slots, each fenced off from the next so that the
-  // compiler keeps the order; LDS operands are read kAhead slots ahead.
-  auto scores = [&](const uint16_t* kbuf, f32x16 (&acc_s)[MT]) {
-    const char* kbb = reinterpret_cast<const char*>(kbuf);
-    constexpr int NS = MT * KS;
-    auto kread = [&](int j) -> bf16x8 {
-      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kbb + lo.ks[j % KS] + 2 * 32 * (j / KS) * kDim));
-    };
-#pragma unroll
-    for (int i = 0; i < MT; ++i) acc_s[i] = f32x16{};
-    bf16x8 kr[NS];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) kr[j] = kread(j);
-#pragma unroll
-    for (int j = 0; j < NS; ++j) {
-      if (j + kAhead < NS) kr[j + kAhead] = kread(j + kAhead);
-      acc_s[j / KS] = mfma32x32x16(kr[j], bq[j % KS], acc_s[j / KS]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  auto mask = [&](f32x16 (&acc_s)[MT], int key0) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = key0 + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
-        acc_s[i][e] = key <= p ? acc_s[i][e] : -INFINITY;
-      }
-  };
-  // eight weights as a B operand; their sum in fp32, as they are
-  auto pack8 = [&](const f32x16& a, int e0, float& lsum) -> bf16x8 {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) lsum += a[e0 + e];
-    uint4 w;
-    w.x = pack_bf16x2(a[e0 + 0], a[e0 + 1]);
-    w.y = pack_bf16x2(a[e0 + 2], a[e0 + 3]);
-    w.z = pack_bf16x2(a[e0 + 4], a[e0 + 5]);
-    w.w = pack_bf16x2(a[e0 + 6], a[e0 + 7]);
-    return __builtin_bit_cast(bf16x8, w);
-  };
-
-  // O is rescaled by the pending sub-block's alpha only when some row's maximum moved
-  auto rescale = [&]() {
-    if (__ballot(alpha_pend != 1.f)) {
-#pragma unroll
-      for (int i = 0; i < kDim / 32; ++i) acc_o[i] *= alpha_pend;
-    }
-  };
-  // V^T operand of k-step u, dim tile td, read down V's columns
-  auto read_vt = [&](const uint16_t* vbuf, int u, int td) -> bf16x8 {
-    const char* a0 = reinterpret_cast<const char*>(vbuf) + lo.vs[td] + 2 * (32 * (u >> 1) + 16 * (u & 1)) * kDim;
-    const uint2 x0 = lds_tr4(reinterpret_cast<const uint16_t*>(a0));
-    const uint2 x1 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + 2 * 8 * kDim));  // rows +8: same permutation
-    return __builtin_bit_cast(bf16x8, make_uint4(x0.x, x0.y, x1.x, x1.y));
-  };
-  // O^T += V^T P^T from one value sub-block in 16 fenced MFMA slots, beside(j)
-  // after the j-th
-  auto pv = [&](const uint16_t* vbuf, auto beside) {
-    constexpr int NO = (kSub / 16) * (kDim / 32);
-    auto vread = [&](int j) { return read_vt(vbuf, j / (kDim / 32), j % (kDim / 32)); };
-    bf16x8 vr[NO];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) vr[j] = vread(j);
-#pragma unroll
-    for (int j = 0; j < NO; ++j) {
-      if (j + kAhead < NO) vr[j + kAhead] = vread(j + kAhead);
-      acc_o[j % (kDim / 32)] = mfma32x32x16(vr[j], bp[j / (kDim / 32)], acc_o[j % (kDim / 32)]);
-      beside(j);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-
-  // One sixteenth of a sub-block's softmax (raw scores; scale_log2 > 0 keeps
-  // their order): j = 0, 1 the maximum, 2 .. 13 the weights, 14, 15 their sum
-  // and the packing.
-  struct Soft {
-    float m0, m_new, alpha, neg, lsum;
-    bf16x8 bp[kSub / 16];
-  };
-  auto soft_step = [&](Soft& z, f32x16 (&acc_s)[MT], int j) __attribute__((always_inline)) {
-    if (j == 0) {
-      z.m0 = -INFINITY;
-      z.lsum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) z.m0 = fmaxf(z.m0, acc_s[0][e]);
-    } else if (j == 1) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) z.m0 = fmaxf(z.m0, acc_s[1][e]);
-      z.m0 = fmaxf(z.m0, xor32f(z.m0));
-      z.m_new = fmaxf(m_run, z.m0);
-      const float mm = z.m_new == -INFINITY ? 0.f : z.m_new;   // rows with nothing visible yet
-      z.alpha = exp2_hw((m_run - mm) * scale_log2);
-      z.neg = -mm * scale_log2;
-    } else if (j < 14) {
-#pragma unroll
-      for (int x = 0; x < 32; ++x) {
-        if (2 + (3 * x) / 8 != j) continue;
-        acc_s[x >> 4][x & 15] = exp2_hw(fmaf(acc_s[x >> 4][x & 15], scale_log2, z.neg));
-      }
-    } else {
-#pragma unroll
-      for (int u = 2 * (j - 14); u < 2 * (j - 14) + 2; ++u) z.bp[u] = pack8(acc_s[u >> 1], 8 * (u & 1), z.lsum);
-      if (j == 15) {
-        z.lsum += xor32f(z.lsum);
-        l_run = l_run * z.alpha + z.lsum;
-        m_run = z.m_new;
-      }
-    }
-  };
-  auto take = [&](const Soft& z) {
-#pragma unroll
-    for (int u = 0; u < kSub / 16; ++u) bp[u] = z.bp[u];
-    alpha_pend = z.alpha;
-  };
-
-  // iteration b: K_{b+1} is in k[(b+1)&1], V_b in v[b&1]; after the S^T slots
-  // each O^T slot carries one sixteenth of the next softmax, so the VALU works
-  // while the MFMA pipe drains.
-  auto step = [&](int b, auto masked_t) {
-    constexpr bool masked = decltype(masked_t)::value;
-    __builtin_amdgcn_s_waitcnt(0);        // this thread's copies of K_{b+1} and V_b have landed
-    __syncthreads();                      // everyone's have, and block b-1's readers are done
-    pw.advance((b + 1) << lg_sub);
-    if constexpr (kDma) {
-      if (b + 2 < b_end) dma(kb, lo.kg, false, b + 2, ring.k[b & 1]);
-      dma(vb, lo.vg, true, b + 1, ring.v[(b + 1) & 1]);
-    } else {
-      if (b + 2 < b_end) store(rk, false, ring.k[b & 1]);
-      store(rv, true, ring.v[(b + 1) & 1]);
-      if (b + 3 < b_end) fetch(kb, b + 3, rk);
-      if (b + 2 < b_end) fetch(vb, b + 2, rv);
-    }
-    if (!live) return;
-    rescale();
-    __builtin_amdgcn_sched_barrier(0);
-    f32x16 acc_s[MT];
-    scores(ring.k[(b + 1) & 1], acc_s);
-    Soft z;
-    pv(ring.v[b & 1], [&](int j) __attribute__((always_inline)) {
-      if (masked && j == 0) mask(acc_s, (b + 1) * kSub);
-      soft_step(z, acc_s, j);
-    });
-    take(z);
-  };
-
-  if (b_begin < b_end) {
-    pw.start(b_begin << lg_sub);
-    if constexpr (kDma) {
-      dma(kb, lo.kg, false, b_begin, ring.k[b_begin & 1]);
-      dma(vb, lo.vg, true, b_begin, ring.v[b_begin & 1]);
-      if (b_begin + 1 < b_end) dma(kb, lo.kg, false, b_begin + 1, ring.k[(b_begin + 1) & 1]);
-    } else {
-      u32x4 r0[NRAW], r1[NRAW], r2[NRAW];
-      fetch(kb, b_begin, r0);
-      fetch(vb, b_begin, r1);
-      if (b_begin + 1 < b_end) fetch(kb, b_begin + 1, r2);
-      if (b_begin + 2 < b_end) fetch(kb, b_begin + 2, rk);
-      if (b_begin + 1 < b_end) fetch(vb, b_begin + 1, rv);
-      store(r0, false, ring.k[b_begin & 1]);
-      store(r1, true, ring.v[b_begin & 1]);
-      if (b_begin + 1 < b_end) store(r2, false, ring.k[(b_begin + 1) & 1]);
-    }
-#pragma unroll
-    for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (live) {
-      f32x16 acc_s[MT];
-      scores(ring.k[b_begin & 1], acc_s);
-      if (b_begin >= nfree) mask(acc_s, b_begin * kSub);
-      Soft z;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) soft_step(z, acc_s, j);
-      take(z);
-    }
-    int b = b_begin;
-    for (; b + 1 < min(nfree, b_end); ++b) step(b, std::false_type{});
-    for (; b + 1 < b_end; ++b) step(b, std::true_type{});
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (live) {
-      rescale();
-      pv(ring.v[b & 1], [](int) {});
-    }
-  }
-  if (!valid) return;
-  const bool empty = !(l_run > 0.f);
-  const float inv_l = empty ? 0.f : o_scale / l_run;
-  const float lse2 = empty ? -INFINITY : m_run * scale_log2 + __log2f(l_run);
-  if (b_begin > 0 || b_end < b_all) {
-    const int64_t row = (2 * static_cast<int64_t>(blockIdx.x) + (b_begin > 0 ? 0 : 1)) * (32 * WAVES) + 32 * wave + n;
-    float* dst = parts.o + row * kDim + 4 * h;
-#pragma unroll
-    for (int td = 0; td < kDim / 32; ++td)
-#pragma unroll
-      for (int e4 = 0; e4 < 4; ++e4)
-        *reinterpret_cast<f32x4*>(dst + 32 * td + 8 * e4) =
-            f32x4{acc_o[td][4 * e4], acc_o[td][4 * e4 + 1], acc_o[td][4 * e4 + 2], acc_o[td][4 * e4 + 3]} * inv_l;
-    if (h == 0) parts.lse[row] = lse2;
-    return;
-  }
-  // O^T tile td: lane (n, h) holds d = 32td + 8(e/4) + 4h + e%4 of row n
-  uint16_t* orow = o + head_row * kDim + 4 * h;
-#pragma unroll
-  for (int td = 0; td < kDim / 32; ++td)
-#pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) {
-      uint2 w;
-      w.x = pack_bf16x2(acc_o[td][4 * e4 + 0] * inv_l, acc_o[td][4 * e4 + 1] * inv_l);
-      w.y = pack_bf16x2(acc_o[td][4 * e4 + 2] * inv_l, acc_o[td][4 * e4 + 3] * inv_l);
-      *reinterpret_cast<uint2*>(orow + 32 * td + 8 * e4) = w;
-    }
-  if (h == 0) lse[head_row] = lse2 * kLn_2;
-  };
-
-  if (pl.ctas == 0) {
-    int s, tile;
-    flash::locate_tile(sq, pl.gr, cta, qt, &s, &tile);
-    run_tile(s, tile, 0, INT32_MAX);
-    return;
-  }
-  int u, u_end, s;
-  {
+  int u = 0, u_end = 1, s = 0;
+  if (pl.ctas > 0) {
     const Steps steps(sq, pl);
     u = cta * steps.per;
     u_end = min(steps.total, u + steps.per);
     if (u >= u_end) return;
     s = steps.seq_of(u);
     if (threadIdx.x < kWave) steps.store(first);
+    __syncthreads();
   }
-  __syncthreads();
+#pragma unroll 1
   while (u < u_end) {
-    while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
-    const int nb = Steps::blocks(bounded_geom(sq, s)), off = u - first[s];
-    const int tile = off / nb, b = off - tile * nb;
-    const int take = min(nb - b, u_end - u);
-    run_tile(s, tile, b, b + take == nb ? INT32_MAX : b + take);
-    __syncthreads();                      // the ring is free again
-    u += take;
+    int tile, b_begin = 0, b_to = INT32_MAX;           // sub-blocks of this tile: to its last
+    if (pl.ctas > 0) {
+      while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
+      const int nb = Steps::blocks(bounded_geom(sq, s)), off = u - first[s];
+      tile = off / nb;
+      b_begin = off - tile * nb;
+      const int take = min(nb - b_begin, u_end - u);
+      if (b_begin + take < nb) b_to = b_begin + take;
+      u += take;
+    } else {
+      flash::locate_tile(sq, pl.gr, cta, qt, &s, &tile);
+      u = u_end;
+    }
+    const SeqGeom g = bounded_geom(sq, s);
+    const int t0 = tile * qt;
+    const int base_p = g.kv_len - g.q_rows;  // position of the sequence's first query row
+    int t_end = min(t0 + qt, g.q_rows);
+    t_end = static_cast<int>(min(static_cast<int64_t>(t_end), sq.total_q_rows - g.q_begin));
+    if (t_end <= t0) continue;                              // uniform over the CTA
+    const int p_last = base_p + t_end - 1;
+    const int t = t0 + wave * qpw + jq;                     // this lane's query row in the sequence
+    const bool valid = n < qpw * G && t < t_end;
+    const int p = valid ? base_p + t : -1;
+    const bool live = t0 + wave * qpw < t_end;              // the wave has rows
+    // sub-blocks below nfree are visible to every row of the wave and need no mask
+    const int nfree = (base_p + min(t0 + wave * qpw, t_end - 1) + 1) / kSub;
+    const int64_t head_row = (static_cast<int64_t>(g.q_begin) + (valid ? t : t0)) * H_q + static_cast<int64_t>(r) * G + hh;
+    const int b_all = p_last < 0 ? 0 : p_last / kSub + 1;
+    const int b_end = min(b_to, b_all);
+    if (b_begin > 0 && b_begin >= b_end) continue;          // the tile's rows see none of these keys
+
+    f32x16 acc_o[kDim / 32];
+#pragma unroll
+    for (int i = 0; i < kDim / 32; ++i) acc_o[i] = f32x16{};
+    float m_run = -INFINITY, l_run = 0.f;
+    // P of the pending sub-block in bf16, as the B operand of O^T = V^T P^T:
+    // k-step u covers keys 32(u/2) + 16(u%2) + {4h + e, 8 + 4h + e}, e = 0..3
+    bf16x8 bp[kSub / 16];
+    float alpha_pend = 0.f;                 // alpha of the sub-block whose P is in bp
+
+    if (b_begin < b_end) {
+      PageWindow<SMALL> pw(sq, s, g.kv_len);
+      pw.start(b_begin);
+      // the query rows, as the B operand of S^T
+      bf16x8 bq[KS];
+      {
+        const T* qrow = q + head_row * kDim + 8 * h;
+        Raw<T> rq[KS];
+#pragma unroll
+        for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
+#pragma unroll
+        for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
+      }
+
+      // bf16 goes into LDS by DMA (copy); codes through registers (get, put)
+      auto copy = [&](const char* base, const Rows<SMALL, N>& at, const uint32_t (&seg)[N], uint16_t* dst) {
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+          dma16(at.ptr(base, stride_b, c, piece_row(c)) + seg[c], dst + kPieceRows * (c * WAVES + wave) * kDim);
+      };
+      u32x4 rk[N], rv[N];
+      auto get = [&](const char* base, const Rows<SMALL, N>& at, u32x4 (&raw)[N]) {
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+          raw[c] = *reinterpret_cast<const u32x4*>(at.ptr(base, stride_b, c, piece_row(c)) + 16 * (lane % kSegs));
+      };
+      auto put = [&](const u32x4 (&raw)[N], bool is_v, uint16_t* dst) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          const int ra = piece_row(c);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int sg = 2 * (lane % kSegs) + e;
+            *reinterpret_cast<u32x4*>(dst + ra * kDim + 8 * (is_v ? v_seg(ra, sg) : k_seg(ra, sg))) =
+                widen(u32x2{raw[c][2 * e], raw[c][2 * e + 1]});
+          }
+        }
+      };
+      Rows<SMALL, N> at_k, at_v;              // K is one sub-block ahead of V
+      auto next_rows = [&](int sub) {
+        at_v = at_k;
+        if (sub < b_end) at_k.find(pw, sub, g.kv_len, piece_row);
+      };
+
+      // S^T = K Q^T on one sub-block: lane (n, h) gets keys 32i + 8(e/4) + 4h + e%4
+      // of row n.  16 MFMA slots, each fenced off from the next so that the
+      // compiler keeps the order; LDS operands are read kAhead slots ahead.
+      auto scores = [&](const uint16_t* kbuf, f32x16 (&acc_s)[MT]) {
+        const char* kbb = reinterpret_cast<const char*>(kbuf);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc_s[i] = f32x16{};
+        constexpr int NS = MT * KS;
+        auto kread = [&](int j) -> bf16x8 {
+          return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kbb + ks_at[j % KS] + 2 * 32 * (j / KS) * kDim));
+        };
+        bf16x8 kr[NS];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) kr[j] = kread(j);
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          if (j + kAhead < NS) kr[j + kAhead] = kread(j + kAhead);
+          acc_s[j / KS] = mfma32x32x16(kr[j], bq[j % KS], acc_s[j / KS]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      auto mask = [&](f32x16 (&acc_s)[MT], int key0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = key0 + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
+            acc_s[i][e] = key <= p ? acc_s[i][e] : -INFINITY;
+          }
+      };
+      // eight weights as a B operand; their sum in fp32, as they are
+      auto pack8 = [&](const f32x16& a, int e0, float& lsum) -> bf16x8 {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) lsum += a[e0 + e];
+        uint4 w;
+        w.x = pack_bf16x2(a[e0 + 0], a[e0 + 1]);
+        w.y = pack_bf16x2(a[e0 + 2], a[e0 + 3]);
+        w.z = pack_bf16x2(a[e0 + 4], a[e0 + 5]);
+        w.w = pack_bf16x2(a[e0 + 6], a[e0 + 7]);
+        return __builtin_bit_cast(bf16x8, w);
+      };
+      // O is rescaled by the pending sub-block's alpha only when some row's maximum moved
+      auto rescale = [&]() {
+        if (__ballot(alpha_pend != 1.f)) {
+#pragma unroll
+          for (int i = 0; i < kDim / 32; ++i) acc_o[i] *= alpha_pend;
+        }
+      };
+      // V^T operand of k-step w, dim tile td, read down V's columns
+      auto read_vt = [&](const uint16_t* vbuf, int w, int td) -> bf16x8 {
+        const char* a0 = reinterpret_cast<const char*>(vbuf) + vs_at[td] + 2 * 16 * w * kDim;
+        const uint2 x0 = lds_tr4(reinterpret_cast<const uint16_t*>(a0));
+        const uint2 x1 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + 2 * 8 * kDim));  // rows +8: same permutation
+        return __builtin_bit_cast(bf16x8, make_uint4(x0.x, x0.y, x1.x, x1.y));
+      };
+      // O^T += V^T P^T from one value sub-block in 16 fenced MFMA slots, beside(j)
+      // after the j-th
+      auto pv = [&](const uint16_t* vbuf, auto beside) {
+        constexpr int NO = (kSub / 16) * (kDim / 32);
+        auto vread = [&](int j) { return read_vt(vbuf, j / (kDim / 32), j % (kDim / 32)); };
+        bf16x8 vr[NO];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) vr[j] = vread(j);
+#pragma unroll
+        for (int j = 0; j < NO; ++j) {
+          if (j + kAhead < NO) vr[j + kAhead] = vread(j + kAhead);
+          acc_o[j % (kDim / 32)] = mfma32x32x16(vr[j], bp[j / (kDim / 32)], acc_o[j % (kDim / 32)]);
+          beside(j);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      // One sixteenth of a sub-block's softmax (raw scores; scale_log2 > 0 keeps
+      // their order): j = 0, 1 the maximum, 2 .. 13 the weights, 14, 15 their sum
+      // and the packing.
+      struct Soft {
+        float m0, m_new, alpha, neg, lsum;
+        bf16x8 bp[kSub / 16];
+      };
+      auto soft_step = [&](Soft& z, f32x16 (&acc_s)[MT], int j) __attribute__((always_inline)) {
+        if (j == 0) {
+          z.m0 = -INFINITY;
+          z.lsum = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z.m0 = fmaxf(z.m0, acc_s[0][e]);
+        } else if (j == 1) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z.m0 = fmaxf(z.m0, acc_s[1][e]);
+          z.m0 = fmaxf(z.m0, xor32f(z.m0));
+          z.m_new = fmaxf(m_run, z.m0);
+          const float mm = z.m_new == -INFINITY ? 0.f : z.m_new;   // rows with nothing visible yet
+          z.alpha = exp2_hw((m_run - mm) * scale_log2);
+          z.neg = -mm * scale_log2;
+        } else if (j < 14) {
+#pragma unroll
+          for (int x = 0; x < 32; ++x) {
+            if (2 + (3 * x) / 8 != j) continue;
+            acc_s[x >> 4][x & 15] = exp2_hw(fmaf(acc_s[x >> 4][x & 15], scale_log2, z.neg));
+          }
+        } else {
+#pragma unroll
+          for (int w = 2 * (j - 14); w < 2 * (j - 14) + 2; ++w) z.bp[w] = pack8(acc_s[w >> 1], 8 * (w & 1), z.lsum);
+          if (j == 15) {
+            z.lsum += xor32f(z.lsum);
+            l_run = l_run * z.alpha + z.lsum;
+            m_run = z.m_new;
+          }
+        }
+      };
+      auto take = [&](const Soft& z) {
+#pragma unroll
+        for (int w = 0; w < kSub / 16; ++w) bp[w] = z.bp[w];
+        alpha_pend = z.alpha;
+      };
+
+      // iteration b: K_{b+1} is in k[(b+1)&1], V_b in v[b&1]; after the S^T slots
+      // each O^T slot carries one sixteenth of the next softmax, so the VALU works
+      // while the MFMA pipe drains.
+      auto step = [&](int b, auto masked_t) {
+        constexpr bool masked = decltype(masked_t)::value;
+        __builtin_amdgcn_s_waitcnt(0);        // this thread's copies of K_{b+1} and V_b have landed
+        __syncthreads();                      // everyone's have, and block b-1's readers are done
+        if constexpr (kCodes) {
+          if (b + 2 < b_end) put(rk, false, ring.k[b & 1]);
+          put(rv, true, ring.v[(b + 1) & 1]);
+          next_rows(b + 3);
+          if (b + 3 < b_end) get(kb, at_k, rk);
+          if (b + 2 < b_end) get(vb, at_v, rv);
+        } else {
+          next_rows(b + 2);
+          if (b + 2 < b_end) copy(kb, at_k, kseg, ring.k[b & 1]);
+          copy(vb, at_v, vseg, ring.v[(b + 1) & 1]);
+        }
+        if (!live) return;
+        rescale();
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 acc_s[MT];
+        scores(ring.k[(b + 1) & 1], acc_s);
+        Soft z;
+        pv(ring.v[b & 1], [&](int j) __attribute__((always_inline)) {
+          if (masked && j == 0) mask(acc_s, (b + 1) * kSub);
+          soft_step(z, acc_s, j);
+        });
+        take(z);
+      };
+
+      // K and V of the first sub-block, K of the second; codes of the sub-blocks
+      // after them wait in registers
+      at_k.find(pw, b_begin, g.kv_len, piece_row);
+      if constexpr (kCodes) {
+        get(kb, at_k, rk);
+        get(vb, at_k, rv);
+        put(rk, false, ring.k[b_begin & 1]);
+        put(rv, true, ring.v[b_begin & 1]);
+        next_rows(b_begin + 1);
+        if (b_begin + 1 < b_end) {
+          get(kb, at_k, rk);
+          get(vb, at_k, rv);
+          put(rk, false, ring.k[(b_begin + 1) & 1]);
+        }
+        next_rows(b_begin + 2);
+        if (b_begin + 2 < b_end) get(kb, at_k, rk);
+      } else {
+        copy(kb, at_k, kseg, ring.k[b_begin & 1]);
+        copy(vb, at_k, vseg, ring.v[b_begin & 1]);
+        next_rows(b_begin + 1);
+        if (b_begin + 1 < b_end) copy(kb, at_k, kseg, ring.k[(b_begin + 1) & 1]);
+      }
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (live) {
+        f32x16 acc_s[MT];
+        scores(ring.k[b_begin & 1], acc_s);
+        if (b_begin >= nfree) mask(acc_s, b_begin * kSub);
+        Soft z;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) soft_step(z, acc_s, j);
+        take(z);
+      }
+      int b = b_begin;
+      for (; b + 1 < min(nfree, b_end); ++b) step(b, std::false_type{});
+      for (; b + 1 < b_end; ++b) step(b, std::true_type{});
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (live) {
+        rescale();
+        pv(ring.v[b & 1], [](int) {});
+      }
+      __syncthreads();                        // the ring is free again
+    }
+    if (!valid) continue;
+    const bool empty = !(l_run > 0.f);
+    const float inv_l = empty ? 0.f : o_scale / l_run;
+    const float lse2 = empty ? -INFINITY : m_run * scale_log2 + __log2f(l_run);
+    // O^T tile td: lane (n, h) holds d = 32td + 8(e/4) + 4h + e%4 of row n
+    if (b_begin > 0 || b_end < b_all) {
+      const int64_t row = (2 * static_cast<int64_t>(blockIdx.x) + (b_begin > 0 ? 0 : 1)) * (32 * WAVES) + 32 * wave + n;
+      float* dst = parts.o + row * kDim + 4 * h;
+#pragma unroll
+      for (int td = 0; td < kDim / 32; ++td)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+          *reinterpret_cast<f32x4*>(dst + 32 * td + 8 * e4) =
+              f32x4{acc_o[td][4 * e4], acc_o[td][4 * e4 + 1], acc_o[td][4 * e4 + 2], acc_o[td][4 * e4 + 3]} * inv_l;
+      if (h == 0) parts.lse[row] = lse2;
+    } else {
+      uint16_t* orow = o + head_row * kDim + 4 * h;
+#pragma unroll
+      for (int td = 0; td < kDim / 32; ++td)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          uint2 w;
+          w.x = pack_bf16x2(acc_o[td][4 * e4 + 0] * inv_l, acc_o[td][4 * e4 + 1] * inv_l);
+          w.y = pack_bf16x2(acc_o[td][4 * e4 + 2] * inv_l, acc_o[td][4 * e4 + 3] * inv_l);
+          *reinterpret_cast<uint2*>(orow + 32 * td + 8 * e4) = w;
+        }
+      if (h == 0) lse[head_row] = lse2 * kLn_2;
+    }
   }
 }
 
@@ -593,7 +603,7 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-template <typename T>
+template <typename T, bool SMALL>
 __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, msa_seqs sq, Plan pl, Parts parts, int H_q,
     int H_kv, float scale_log2, uint32_t q_flip, float o_scale, uint16_t* __restrict__ o, float* __restrict__ lse) {
@@ -615,25 +625,35 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
   const char* vb = reinterpret_cast<const char*>(v + static_cast<int64_t>(r) * kDim);
   const uint32_t stride_b = static_cast<uint32_t>(H_kv * kDim * sizeof(T));
   const int lrow = lane / kLanes, lseg = lane % kLanes;
-  const uint32_t lane_off = lrow * stride_b + 16 * lseg;
 
-  int u, u_end, s;
-  {
+  auto piece_row = [&](int c) { return c * kRows + lrow; };
+
+  int u = 0, u_end = 1, s = 0;
+  if (pl.ctas > 0) {
     const Steps steps(sq, pl);
     u = cta * steps.per;
     u_end = min(steps.total, u + steps.per);
     if (u >= u_end) return;
     s = steps.seq_of(u);
     if (threadIdx.x < kWave) steps.store(first);
+    __syncthreads();
   }
-  __syncthreads();
+#pragma unroll 1
   while (u < u_end) {
-    while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
+    int tile, b_begin = 0, b_to = INT32_MAX;           // sub-blocks of this tile: to its last
+    if (pl.ctas > 0) {
+      while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
+      const int nb = Steps::blocks(bounded_geom(sq, s)), off = u - first[s];
+      tile = off / nb;
+      b_begin = off - tile * nb;
+      const int take = min(nb - b_begin, u_end - u);
+      if (b_begin + take < nb) b_to = b_begin + take;
+      u += take;
+    } else {
+      flash::locate_tile(sq, pl.gr, cta, qpw, &s, &tile);
+      u = u_end;
+    }
     const SeqGeom g = bounded_geom(sq, s);
-    const int nb = Steps::blocks(g), off = u - first[s];
-    const int tile = off / nb, b_begin = off - tile * nb;
-    const int take = min(nb - b_begin, u_end - u);
-    u += take;
     const int t0 = tile * qpw;
     const int base_p = g.kv_len - g.q_rows;            // position of the sequence's first query row
     int t_end = min(t0 + qpw, g.q_rows);
@@ -641,7 +661,7 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     if (t_end <= t0) continue;
     const int p_last = base_p + t_end - 1;
     const int b_all = p_last < 0 ? 0 : p_last / kSub + 1;
-    const int b_end = b_begin + take == nb ? b_all : min(b_begin + take, b_all);
+    const int b_end = min(b_to, b_all);
     if (b_begin > 0 && b_begin >= b_end) continue;     // the tile's rows see none of these keys
     const bool valid = n < qpw * G && t0 + jq < t_end;
     const int p = valid ? base_p + t0 + jq : -1;
@@ -656,35 +676,11 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
 #pragma unroll
       for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
     }
-    PageWindow pw;
-    pw.table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
-    pw.lg_page = 31 - __clz(sq.page_size);
-    pw.lg_unit = min(pw.lg_page, 6);
-    pw.max_page = (sq.total_kv_rows >> pw.lg_page) - 1;
-    pw.units = ((g.kv_len - 1) >> pw.lg_unit) + 1;
-    const int lg_sub = 6 - pw.lg_unit;                 // log2 of units per sub-block
-
-    // whole rows of one sub-block, rows past the sequence's end its last one again
-    auto fetch = [&](const char* base, int sub, u32x4 (&dst)[NL]) {
-      const int key0 = sub * kSub;
-      if (key0 + kSub <= g.kv_len) {
-        if (lg_sub == 0) {
-          const char* blk = base + pw.row(sub) * stride_b;
+    PageWindow<SMALL> pw(sq, s, g.kv_len);
+    auto fetch = [&](const char* base, const Rows<SMALL, NL>& at, u32x4 (&dst)[NL]) {
 #pragma unroll
-          for (int c = 0; c < NL; ++c) dst[c] = *reinterpret_cast<const u32x4*>(blk + c * kRows * stride_b + lane_off);
-        } else {
-#pragma unroll
-          for (int c = 0; c < NL; ++c) {
-            const int in_unit = (c * kRows) & ((1 << pw.lg_unit) - 1);
-            const char* blk = base + (pw.row((sub << lg_sub) + ((c * kRows) >> pw.lg_unit)) + in_unit) * stride_b;
-            dst[c] = *reinterpret_cast<const u32x4*>(blk + lane_off);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < NL; ++c)
-          dst[c] = *reinterpret_cast<const u32x4*>(base + pw.key_row(min(key0 + c * kRows + lrow, g.kv_len - 1)) * stride_b + 16 * lseg);
-      }
+      for (int c = 0; c < NL; ++c)
+        dst[c] = *reinterpret_cast<const u32x4*>(at.ptr(base, stride_b, c, piece_row(c)) + 16 * lseg);
     };
     auto store = [&](const u32x4 (&src)[NL], bool is_v, uint16_t* dst) {
 #pragma unroll
@@ -708,17 +704,25 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     for (int i = 0; i < kDim / 32; ++i) acc_o[i] = f32x16{};
     float m_run = -INFINITY, l_run = 0.f;
     u32x4 rk[NL], rv[NL];
-    int b = b_begin + wave;
-    if (b < b_end) {
-      pw.start(b << lg_sub);
-      fetch(kb, b, rk);
-      fetch(vb, b, rv);
-    }
-    for (; b < b_end; b += kRowWaves) {
-      pw.advance((b + kRowWaves) << lg_sub);
+    Rows<SMALL, NL> at;
+    if (b_begin + wave < b_end) pw.start(b_begin + wave);
+    // The first pass only requests: each load stands once in the code, which is
+    // read from memory anew by every launch (with the first loads apart and
+    // paths of their own for whole sub-blocks, 30 KB instead of XXX, a call of
+    // one token on 8K keys took YYY us instead of ZZZ).
+#pragma unroll 1
+    for (int b = b_begin + wave - kRowWaves; b < b_end; b += kRowWaves) {
+      const bool now = b >= b_begin, more = b + kRowWaves < b_end;
       wave_lds_order();
-      store(rk, false, buf.k);
-      if (b + kRowWaves < b_end) fetch(kb, b + kRowWaves, rk);
+      if (now) store(rk, false, buf.k);
+      if (more) {
+        at.find(pw, b + kRowWaves, g.kv_len, piece_row);
+        fetch(kb, at, rk);
+      }
+      if (!now) {
+        if (more) fetch(vb, at, rv);
+        continue;
+      }
       wave_lds_order();
       // S^T = K Q^T: lane (n, h) gets keys 32i + 8(e/4) + 4h + e%4 of row n
       f32x16 acc_s[MT];
@@ -763,7 +767,7 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
         for (int i = 0; i < kDim / 32; ++i) acc_o[i] *= alpha;
       }
       store(rv, true, buf.v);
-      if (b + kRowWaves < b_end) fetch(vb, b + kRowWaves, rv);
+      if (more) fetch(vb, at, rv);
       wave_lds_order();
       // O^T += V^T P^T; P^T as the B operand: k-step w covers keys 32(w/2) + 16(w%2) + {4h + e, 8 + 4h + e}
 #pragma unroll
@@ -850,12 +854,15 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
 }
 
 // Joins the parts of the rows whose tile several CTAs had: a = max LSE_c,
-// LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c, in the order of
-// the keys.  A wave takes a (query row, group) and every gridDim.y-th of its
-// heads: lane l has dims 8 (l % 16) .. + 7 of parts l / 16, l / 16 + 4, ...
+// LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c, in an order that
+// the lengths fix.  A wave takes a (query row, group), its heads in turn: each
+// of its four lane groups (16 lanes x 8 dims) has every fourth part of one head,
+// or with HEADS = 4 all parts of a head of its own (tiles of many rows, which
+// few CTAs share).
+template <int HEADS>
 __global__ __launch_bounds__(256) void merge_kernel(msa_seqs sq, Plan pl, Parts parts, int rows_per_tile, int H_q, int H_kv,
                                                     uint16_t* __restrict__ o, float* __restrict__ lse) {
-  constexpr int kBatch = 4;
+  constexpr int kShare = 4 / HEADS;      // lane groups per head
   const int lane = lane_id();
   const int64_t pair = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave;
   const int64_t row = pair / H_kv;
@@ -870,73 +877,61 @@ __global__ __launch_bounds__(256) void merge_kernel(msa_seqs sq, Plan pl, Parts 
   const int tile = t / pl.qt, in_tile = t - tile * pl.qt;
   const int qpw = 32 / G;
   const int p_last = g.kv_len - g.q_rows + min((tile + 1) * pl.qt, g.q_rows) - 1;
-  const int nb = Steps::blocks(g);
-  const int u0 = steps.first(s) + tile * nb;
+  const int u0 = steps.first(s) + tile * Steps::blocks(g);
   const int visits = p_last < 0 ? 0 : p_last / kSub + 1;
   const int c0 = u0 / steps.per, c1 = visits < 1 ? c0 : min((u0 + visits - 1) / steps.per, pl.ctas - 1);
   if (c0 >= c1) return;                  // written by its one CTA
-  const int np = c1 - c0 + 1, d0 = 8 * (lane & 15), l4 = lane >> 4;
-  for (int hh = blockIdx.y; hh < G; hh += gridDim.y) {
+  const int np = c1 - c0 + 1, l16 = lane & 15, l4 = lane >> 4;
+#pragma unroll 1
+  for (int h0 = blockIdx.y * HEADS; h0 < G; h0 += gridDim.y * HEADS) {
+    const int hh = min(h0 + (HEADS == 4 ? l4 : 0), G - 1);
     const int slot = 32 * (in_tile / qpw) + (in_tile % qpw) * G + hh;
-    float a = -INFINITY, sum = 0.f;
-    float out[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int j0 = l4; j0 < np; j0 += 4 * kBatch) {
-      float l[kBatch];
-      f32x4 x[kBatch][2];
+    auto part_row = [&](int j) {         // of the CTA's two parts: the tile's beginning, or not
+      return (2 * (static_cast<int64_t>(c0 + j) * H_kv + r) + (j == 0 ? 1 : 0)) * rows_per_tile + slot;
+    };
+    float a = -INFINITY;
+    for (int j = l16; j < np; j += 16) a = fmaxf(a, parts.lse[part_row(j)]);
+    auto each = [&](auto f) {            // over the 16 lanes of a group
+      a = f(a, __uint_as_float(xor_lane_u32<1>(__float_as_uint(a))));
+      a = f(a, __uint_as_float(xor_lane_u32<2>(__float_as_uint(a))));
+      a = f(a, __uint_as_float(xor_lane_u32<4>(__float_as_uint(a))));
+      a = f(a, __uint_as_float(xor_lane_u32<8>(__float_as_uint(a))));
+    };
+    each([](float x, float y) { return fmaxf(x, y); });
+    const float top = a > -INFINITY ? a : 0.f;   // every part empty: all weights are zero
+    float sum = 0.f;
+    f32x4 x0{}, x1{};
+#pragma unroll 4
+    for (int j = HEADS == 4 ? 0 : l4; j < np; j += kShare) {
+      const int64_t at = part_row(j);
+      const float w = exp2_hw(parts.lse[at] - top);
+      const f32x4* src = reinterpret_cast<const f32x4*>(parts.o + at * kDim + 8 * l16);
+      sum += w;
+      x0 += src[0] * w;
+      x1 += src[1] * w;
+    }
+    if constexpr (HEADS == 1) {
+      auto join = [](float v) {
+        v += __uint_as_float(xor_lane_u32<16>(__float_as_uint(v)));
+        return v + __uint_as_float(xor_lane_u32<32>(__float_as_uint(v)));
+      };
+      sum = join(sum);
 #pragma unroll
-      for (int e = 0; e < kBatch; ++e) {
-        const int j = min(j0 + 4 * e, np - 1);
-        const int64_t cta = static_cast<int64_t>(c0 + j) * H_kv + r;
-        const int64_t at = (2 * cta + (j == 0 ? 1 : 0)) * rows_per_tile + slot;
-        l[e] = parts.lse[at];
-        const f32x4* src = reinterpret_cast<const f32x4*>(parts.o + at * kDim + d0);
-        x[e][0] = src[0];
-        x[e][1] = src[1];
-      }
-      float m = a;
-#pragma unroll
-      for (int e = 0; e < kBatch; ++e) {
-        l[e] = j0 + 4 * e < np ? l[e] : -INFINITY;
-        m = fmaxf(m, l[e]);
-      }
-      if (!(m > -INFINITY)) continue;
-      const float f = a > -INFINITY ? exp2f(a - m) : 0.f;
-      a = m;
-      sum *= f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) out[i] *= f;
-#pragma unroll
-      for (int e = 0; e < kBatch; ++e) {
-        if (!(l[e] > -INFINITY)) continue;      // an empty part does not count
-        const float w = exp2f(l[e] - m);
-        sum += w;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = fmaf(w, x[e][i >> 2][i & 3], out[i]);
+      for (int i = 0; i < 4; ++i) {
+        x0[i] = join(x0[i]);
+        x1[i] = join(x1[i]);
       }
     }
-    // the four lanes of a dim
-    float m = fmaxf(a, __shfl_xor(a, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const float f = a > -INFINITY ? exp2f(a - m) : 0.f;
-    auto join = [&](float v) {
-      v *= f;
-      v += __shfl_xor(v, 16);
-      return v + __shfl_xor(v, 32);
-    };
-    sum = join(sum);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) out[i] = join(out[i]);
-    if (l4 != 0) continue;
-    const bool any = m > -INFINITY;
-    const float inv = any ? 1.f / sum : 0.f;
+    if (HEADS == 4 ? h0 + l4 >= G : l4 != 0) continue;
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
     const int64_t head_row = row * H_q + static_cast<int64_t>(r) * G + hh;
     uint4 w;
-    w.x = pack_bf16x2(out[0] * inv, out[1] * inv);
-    w.y = pack_bf16x2(out[2] * inv, out[3] * inv);
-    w.z = pack_bf16x2(out[4] * inv, out[5] * inv);
-    w.w = pack_bf16x2(out[6] * inv, out[7] * inv);
-    *reinterpret_cast<uint4*>(o + head_row * kDim + d0) = w;
-    if (d0 == 0) lse[head_row] = any ? (m + __log2f(sum)) * kLn_2 : -INFINITY;
+    w.x = pack_bf16x2(x0[0] * inv, x0[1] * inv);
+    w.y = pack_bf16x2(x0[2] * inv, x0[3] * inv);
+    w.z = pack_bf16x2(x1[0] * inv, x1[1] * inv);
+    w.w = pack_bf16x2(x1[2] * inv, x1[3] * inv);
+    *reinterpret_cast<uint4*>(o + head_row * kDim + 8 * l16) = w;
+    if (l16 == 0) lse[head_row] = sum > 0.f ? (top + __log2f(sum)) * kLn_2 : -INFINITY;
   }
 }
 
@@ -950,7 +945,7 @@ int validate_paged(const msa_seqs* seqs, int H_q, int H_kv, int head_dim) {
   if (head_dim != kDim) return MSA_ERR_UNSUPPORTED;
   if (H_q / H_kv > 16 || H_kv > 64) return MSA_ERR_UNSUPPORTED;
   if (seqs->total_q_rows * H_kv >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
-  if (seqs->total_kv_rows >= (int64_t(1) << 35)) return MSA_ERR_UNSUPPORTED;
+  if (seqs->total_kv_rows >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
   return MSA_OK;
 }
 
@@ -987,6 +982,7 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
   if (seqs->total_q_rows == 0) return MSA_OK;
   if (!q || !k || !v || !o || !lse) return MSA_ERR_INVALID;
   const flash::LogitScale scale = flash::logit_scale(softmax_scale * q_scale * k_scale * kLog2E);
+  const int G = H_q / H_kv;
   int waves;
   int64_t ctas;
   const Plan pl = plan_of(seqs, H_q, H_kv, &waves, &ctas);
@@ -997,29 +993,33 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
     parts.o = static_cast<float*>(workspace);
     parts.lse = parts.o + 2 * ctas * 32 * waves * kDim;
   }
-  auto launch = [&](auto kernel, auto elem, int cta_waves = 0) {
+  auto launch = [&](const char* name, auto kernel, auto elem, int cta_waves) {
     using T = decltype(elem);
-    msa_prof::launch("paged_attn_kernel", kernel, dim3(static_cast<unsigned>(ctas)),
-                     dim3((cta_waves > 0 ? cta_waves : waves) * kWave), 0, stream, static_cast<const T*>(q),
-                     static_cast<const T*>(k), static_cast<const T*>(v), *seqs, pl, parts, H_q, H_kv, scale.log2,
-                     scale.q_flip, v_scale, static_cast<uint16_t*>(o), lse);
+    msa_prof::launch(name, kernel, dim3(static_cast<unsigned>(ctas)), dim3(cta_waves * kWave), 0, stream,
+                     static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v), *seqs, pl, parts, H_q, H_kv,
+                     scale.log2, scale.q_flip, v_scale, static_cast<uint16_t*>(o), lse);
   };
-  auto pick = [&](auto elem) {
+  auto pick = [&](auto elem, auto small) {
     using T = decltype(elem);
-    if (waves == 1 && pl.ctas > 0) launch(paged_rows_kernel<T>, elem, kRowWaves);
-    else if (waves == 1) launch(paged_attn_kernel<T, 1>, elem);
-    else if (waves == 2) launch(paged_attn_kernel<T, 2>, elem);
-    else if (waves == 4) launch(paged_attn_kernel<T, 4>, elem);
-    else launch(paged_attn_kernel<T, 8>, elem);
+    constexpr bool SMALL = decltype(small)::value;
+    if (waves == 1) launch("paged_rows_kernel", paged_rows_kernel<T, SMALL>, elem, kRowWaves);
+    else if (waves == 2) launch("paged_attn_kernel", paged_attn_kernel<T, 2, SMALL>, elem, 2);
+    else if (waves == 4) launch("paged_attn_kernel", paged_attn_kernel<T, 4, SMALL>, elem, 4);
+    else launch("paged_attn_kernel", paged_attn_kernel<T, 8, SMALL>, elem, 8);
   };
-  if (fp8) pick(uint8_t{});
-  else pick(uint16_t{});
+  const bool small = seqs->page_size < kSub;
+  if (fp8 && small) pick(uint8_t{}, std::true_type{});
+  else if (fp8) pick(uint8_t{}, std::false_type{});
+  else if (small) pick(uint16_t{}, std::true_type{});
+  else pick(uint16_t{}, std::false_type{});
   if (pl.ctas > 0) {
-    // a wave per (row, group), or per head where those are few
+    // a wave per (row, group); where those are few one per head of them
     const int64_t pairs = seqs->total_q_rows * H_kv;
-    const int by_head = pairs < 4096 ? H_q / H_kv : 1;
-    msa_prof::launch("paged_merge_kernel", merge_kernel, dim3(static_cast<unsigned>((pairs + 3) / 4), by_head), dim3(256), 0,
-                     stream, *seqs, pl, parts, 32 * waves, H_q, H_kv, static_cast<uint16_t*>(o), lse);
+    const bool many = waves >= 4;
+    const int by_head = pairs >= 4096 ? 1 : many ? (G + 3) / 4 : G;
+    msa_prof::launch("paged_merge_kernel", many ? merge_kernel<4> : merge_kernel<1>,
+                     dim3(static_cast<unsigned>((pairs + 3) / 4), by_head), dim3(256), 0, stream, *seqs, pl, parts, 32 * waves,
+                     H_q, H_kv, static_cast<uint16_t*>(o), lse);
   }
   return msa_host::launch_status();
 }

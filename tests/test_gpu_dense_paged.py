@@ -45,6 +45,10 @@ CASES = [
     ("mixed", [1, 300, 1, 0, 40, 1], [2000, 900, 64, 128, 41, 3333], 16, 2, 64, 0),
     ("chunk_on_long", [64], [12000], 8, 1, 1024, 0),
     ("chunks_on_long", [130, 20], [5000, 9000], 8, 1, 32, 0),
+    ("300_sequences", [1, 2] * 150, [1 + 7 * i % 400 + 2 for i in range(300)], 8, 2, 64, 0),
+    ("300_prompts_small_pages", [5 + i % 30 for i in range(300)], [5 + i % 30 for i in range(300)], 8, 2, 16, 0),
+    ("many_tiles", [700, 900, 1, 500], [700, 1000, 40, 500], 64, 64, 64, 0),
+    ("many_few_row_tiles", [1] * 90, [1 + 5 * i for i in range(90)], 64, 64, 32, 0),
 ]
 
 
@@ -111,12 +115,17 @@ def test_dense_paged(case, fp8):
     assert torch.equal(o2[:n], o[:n]) and torch.equal(l2[:n], lse[:n])
 
 
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("q_rows", [[3, 8], [3, 40]], ids=["few_rows", "tiles"])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 0.9])
-def test_softmax_scales(scale):
-    case = ("scales", [3, 40], [70, 130], 4, 2, 64, 0)
-    x, d, seqs, lay, _ = _make(case, False)
-    o, l = msa.dense_attn_paged(*d, seqs, softmax_scale=scale)
-    o_ref, l_ref = _reference(case, x, lay, False, None, scale)
+def test_softmax_scales(scale, q_rows, fp8):
+    case = ("scales", q_rows, [70, 130], 4, 2, 64, 0)
+    x, d, seqs, lay, _ = _make(case, fp8)
+    if fp8:
+        o, l = msa.dense_attn_paged_fp8(*d, SCALES, seqs, softmax_scale=scale)
+    else:
+        o, l = msa.dense_attn_paged(*d, seqs, softmax_scale=scale)
+    o_ref, l_ref = _reference(case, x, lay, fp8, None, scale)
     check_outputs(o.float().cpu().numpy(), l.cpu().numpy(), o_ref, l_ref, "scale")
 
 

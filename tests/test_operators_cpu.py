@@ -131,7 +131,7 @@ PAGED_BAD = [
     (dict(seqs=_seqs()), UNS),                             # contiguous
     (dict(seqs=_paged(page_size=96)), INV), (dict(seqs=_paged(page_size=8, block_table_stride=20)), INV),
     (dict(seqs=_paged(page_size=16384, total_kv_rows=1 << 20)), INV), (dict(seqs=_paged(block_table_stride=1)), INV),
-    (dict(seqs=_paged(total_kv_rows=1 << 35)), UNS), (dict(d=64), UNS), (dict(H=6, K=4), INV), (dict(H=34, K=2), UNS),
+    (dict(seqs=_paged(total_kv_rows=1 << 31)), UNS), (dict(d=64), UNS), (dict(H=6, K=4), INV), (dict(H=34, K=2), UNS),
     (dict(H=65, K=65), UNS), (dict(q=None), INV), (dict(k=None), INV), (dict(v=None), INV), (dict(o=None), INV),
     (dict(lse=None), INV),
 ]
