@@ -36,7 +36,6 @@
 namespace {
 
 using namespace msa;
-using flash::dma16;
 using flash::kAhead;
 using flash::kDim;
 using flash::kLn_2;
@@ -47,6 +46,23 @@ using flash::lds_tr4;
 using flash::Ring;
 using flash::v_seg;
 using flash::xor32f;
+
+// global_load_lds: lane l's 16 bytes land at dst + 16 l (dst wave-uniform).  From
+// inline assembly: the compiler cannot tell the ring's buffers apart and would
+// wait for the copies just issued before the first read of the sub-block that
+// has landed (2 x 2048 rows on 16K keys 2035 us instead of 1977); every step
+// waits for them itself before its barrier.  M0 holds the LDS address, one wait
+// state ahead of the copy.
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<size_t>((__attribute__((address_space(3))) const void*)(p)));
+}
+__device__ __forceinline__ void copy16(const char* base, uint32_t offset, uint32_t lds) {   // base, lds wave-uniform
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(offset), "s"(base), "s"(lds) : "m0", "memory");
+}
+__device__ __forceinline__ void copy16(const char* src, uint32_t lds) {                      // src each lane its own
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(src), "s"(lds) : "m0", "memory");
+}
 
 // Places of a sequence's key rows in the pool, in units of min(page, 64) rows:
 // a window of 64 units, one per lane, and the one behind it.  SMALL: pages of
@@ -205,9 +221,17 @@ struct Rows {
       at[0] = pw.place(sub, 0);
     }
   }
-  __device__ __forceinline__ const char* ptr(const char* base, uint32_t stride_b, int c, int row) const {
-    if constexpr (SMALL) return base + static_cast<int64_t>(at[c]) * stride_b;
-    else return base + static_cast<int64_t>(at[0]) * stride_b + static_cast<uint32_t>(min(row, last)) * stride_b;
+  // Piece c is 16 bytes at byte `seg` of row `row`: uniform base and lane offset
+  // (whole sub-blocks: `off` = row * stride_b + seg, formed once).
+  __device__ __forceinline__ const char* from(const char* base, uint32_t stride_b) const {
+    return base + static_cast<int64_t>(at[0]) * stride_b;
+  }
+  __device__ __forceinline__ uint32_t offset(uint32_t off, uint32_t stride_b, int row, uint32_t seg) const {
+    return last >= kSub - 1 ? off : static_cast<uint32_t>(min(row, last)) * stride_b + seg;
+  }
+  __device__ __forceinline__ const char* ptr(const char* base, uint32_t stride_b, int c, int row, uint32_t seg) const {
+    if constexpr (SMALL) return base + static_cast<int64_t>(at[c]) * stride_b + seg;
+    else return from(base, stride_b) + offset(row * stride_b + seg, stride_b, row, seg);
   }
 };
 
@@ -226,7 +250,7 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   __shared__ __align__(16) Ring ring;
   __shared__ int first[kMaxSplitSeqs + 1];
   const int lane = lane_id();
-  const int wave = threadIdx.x / kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int n = lane & 31, h = lane >> 5;
   const int G = H_q / H_kv;
   const int qpw = 32 / G;                  // query rows per wave
@@ -242,13 +266,17 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   // piece lands at 16 l of its wave's, so it takes the segment that the row's
   // permutation stores there (the permutations are involutions).
   auto piece_row = [&](int c) { return kPieceRows * (c * WAVES + wave) + lane / kSegs; };
-  uint32_t kseg[N], vseg[N];
+  auto piece_seg = [&](int c, bool is_v) -> uint32_t {
+    const int ra = piece_row(c), sg = lane % kSegs;
+    return 16 * (kCodes ? sg : is_v ? v_seg(ra, sg) : k_seg(ra, sg));
+  };
+  uint32_t koff[N], voff[N];               // in whole sub-blocks of large pages
 #pragma unroll
   for (int c = 0; c < N; ++c) {
-    const int ra = piece_row(c), sg = lane % kSegs;
-    kseg[c] = 16 * (kCodes ? sg : k_seg(ra, sg));
-    vseg[c] = 16 * (kCodes ? sg : v_seg(ra, sg));
+    koff[c] = piece_row(c) * stride_b + piece_seg(c, false);
+    voff[c] = piece_row(c) * stride_b + piece_seg(c, true);
   }
+  const uint32_t lds_k = lds_address(ring.k[0]), lds_v = lds_address(ring.v[0]);
   // MFMA operand reads, relative to a ring buffer
   uint32_t ks_at[KS], vs_at[kDim / 32];
 #pragma unroll
@@ -332,16 +360,22 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
       }
 
       // bf16 goes into LDS by DMA (copy); codes through registers (get, put)
-      auto copy = [&](const char* base, const Rows<SMALL, N>& at, const uint32_t (&seg)[N], uint16_t* dst) {
+      auto copy = [&](const char* base, const Rows<SMALL, N>& at, bool is_v, int buf) {
+        const uint32_t lds = (is_v ? lds_v : lds_k) + buf * 2 * kSub * kDim + 1024 * wave;
 #pragma unroll
-        for (int c = 0; c < N; ++c)
-          dma16(at.ptr(base, stride_b, c, piece_row(c)) + seg[c], dst + kPieceRows * (c * WAVES + wave) * kDim);
+        for (int c = 0; c < N; ++c) {
+          if constexpr (SMALL)
+            copy16(at.ptr(base, stride_b, c, 0, piece_seg(c, is_v)), lds + 1024 * WAVES * c);
+          else
+            copy16(at.from(base, stride_b), at.offset(is_v ? voff[c] : koff[c], stride_b, piece_row(c), piece_seg(c, is_v)),
+                   lds + 1024 * WAVES * c);
+        }
       };
       u32x4 rk[N], rv[N];
       auto get = [&](const char* base, const Rows<SMALL, N>& at, u32x4 (&raw)[N]) {
 #pragma unroll
         for (int c = 0; c < N; ++c)
-          raw[c] = *reinterpret_cast<const u32x4*>(at.ptr(base, stride_b, c, piece_row(c)) + 16 * (lane % kSegs));
+          raw[c] = *reinterpret_cast<const u32x4*>(at.ptr(base, stride_b, c, piece_row(c), 16 * (lane % kSegs)));
       };
       auto put = [&](const u32x4 (&raw)[N], bool is_v, uint16_t* dst) {
 #pragma unroll
@@ -364,7 +398,7 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
       // S^T = K Q^T on one sub-block: lane (n, h) gets keys 32i + 8(e/4) + 4h + e%4
       // of row n.  16 MFMA slots, each fenced off from the next so that the
       // compiler keeps the order; LDS operands are read kAhead slots ahead.
-      auto scores = [&](const uint16_t* kbuf, f32x16 (&acc_s)[MT]) {
+      auto scores = [&](const uint16_t* kbuf, f32x16 (&acc_s)[MT], auto beside) {
         const char* kbb = reinterpret_cast<const char*>(kbuf);
 #pragma unroll
         for (int i = 0; i < MT; ++i) acc_s[i] = f32x16{};
@@ -379,6 +413,7 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
         for (int j = 0; j < NS; ++j) {
           if (j + kAhead < NS) kr[j + kAhead] = kread(j + kAhead);
           acc_s[j / KS] = mfma32x32x16(kr[j], bq[j % KS], acc_s[j / KS]);
+          beside(j);
           __builtin_amdgcn_sched_barrier(0);
         }
       };
@@ -482,22 +517,38 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
         constexpr bool masked = decltype(masked_t)::value;
         __builtin_amdgcn_s_waitcnt(0);        // this thread's copies of K_{b+1} and V_b have landed
         __syncthreads();                      // everyone's have, and block b-1's readers are done
-        if constexpr (kCodes) {
-          if (b + 2 < b_end) put(rk, false, ring.k[b & 1]);
-          put(rv, true, ring.v[(b + 1) & 1]);
-          next_rows(b + 3);
-          if (b + 3 < b_end) get(kb, at_k, rk);
-          if (b + 2 < b_end) get(vb, at_v, rv);
-        } else {
-          next_rows(b + 2);
-          if (b + 2 < b_end) copy(kb, at_k, kseg, ring.k[b & 1]);
-          copy(vb, at_v, vseg, ring.v[(b + 1) & 1]);
+        // the next copies go out beside the first S^T slots: in front of them (some
+        // sixty scalar and address instructions) they held up all eight waves
+        auto move_k = [&]() __attribute__((always_inline)) {
+          if constexpr (kCodes) {
+            if (b + 2 < b_end) put(rk, false, ring.k[b & 1]);
+            next_rows(b + 3);
+            if (b + 3 < b_end) get(kb, at_k, rk);
+          } else {
+            next_rows(b + 2);
+            if (b + 2 < b_end) copy(kb, at_k, false, b & 1);
+          }
+        };
+        auto move_v = [&]() __attribute__((always_inline)) {
+          if constexpr (kCodes) {
+            put(rv, true, ring.v[(b + 1) & 1]);
+            if (b + 2 < b_end) get(vb, at_v, rv);
+          } else {
+            copy(vb, at_v, true, (b + 1) & 1);
+          }
+        };
+        if (!live) {
+          move_k();
+          move_v();
+          return;
         }
-        if (!live) return;
         rescale();
         __builtin_amdgcn_sched_barrier(0);
         f32x16 acc_s[MT];
-        scores(ring.k[(b + 1) & 1], acc_s);
+        scores(ring.k[(b + 1) & 1], acc_s, [&](int j) __attribute__((always_inline)) {
+          if (j == 1) move_k();
+          if (j == 4) move_v();
+        });
         Soft z;
         pv(ring.v[b & 1], [&](int j) __attribute__((always_inline)) {
           if (masked && j == 0) mask(acc_s, (b + 1) * kSub);
@@ -523,16 +574,16 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
         next_rows(b_begin + 2);
         if (b_begin + 2 < b_end) get(kb, at_k, rk);
       } else {
-        copy(kb, at_k, kseg, ring.k[b_begin & 1]);
-        copy(vb, at_k, vseg, ring.v[b_begin & 1]);
+        copy(kb, at_k, false, b_begin & 1);
+        copy(vb, at_k, true, b_begin & 1);
         next_rows(b_begin + 1);
-        if (b_begin + 1 < b_end) copy(kb, at_k, kseg, ring.k[(b_begin + 1) & 1]);
+        if (b_begin + 1 < b_end) copy(kb, at_k, false, (b_begin + 1) & 1);
       }
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       if (live) {
         f32x16 acc_s[MT];
-        scores(ring.k[b_begin & 1], acc_s);
+        scores(ring.k[b_begin & 1], acc_s, [](int) {});
         if (b_begin >= nfree) mask(acc_s, b_begin * kSub);
         Soft z;
 #pragma unroll
@@ -680,7 +731,7 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     auto fetch = [&](const char* base, const Rows<SMALL, NL>& at, u32x4 (&dst)[NL]) {
 #pragma unroll
       for (int c = 0; c < NL; ++c)
-        dst[c] = *reinterpret_cast<const u32x4*>(at.ptr(base, stride_b, c, piece_row(c)) + 16 * lseg);
+        dst[c] = *reinterpret_cast<const u32x4*>(at.ptr(base, stride_b, c, piece_row(c), 16 * lseg));
     };
     auto store = [&](const u32x4 (&src)[NL], bool is_v, uint16_t* dst) {
 #pragma unroll
