@@ -1000,9 +1000,19 @@ int validate_paged(const msa_seqs* seqs, int H_q, int H_kv, int head_dim) {
   return MSA_OK;
 }
 
-// Waves for the longest sequence's rows, a CTA per tile and group where those
-// are several times what the chip holds at once (one CTA of 8 waves per CU, two
-// of fewer: registers and LDS), else as many CTAs as it holds.
+// Waves for the longest sequence's rows, and whether the keys are split.
+//
+// The chip holds one CTA of 8 waves, one of the few-row kernel, or two of 2 or 4
+// waves per CU.  Unsplit, a call lasts as many steps as the longest sequence has
+// sub-blocks, once per round of CTAs; split, its share of all steps and some ten
+// more for the parts and their merge.  The lengths are on the device: several
+// sequences are taken to have three quarters of the longest's on average.
+// Measured, us split / whole (64 heads on 8): one token of one sequence on 512
+// keys 13.6 / 11.2, 1024 13.7 / 17.0; 32 sequences 1024 31.8 / 26.8, 4096 102.8 /
+// 97.4 (all of them equally long; of 4K - 60K 421 against what the longest takes,
+// over 600); 512 rows on 1024 keys 37.1 / 35.1, 2048 52.7 / 59.7; 64 rows 512 22.1
+// / 21.5, 1024 24.9 / 33.8.
+constexpr int kFewRowsGain = 11, kTileGain = 9;      // steps that a split has to save
 Plan plan_of(const msa_seqs* seqs, int H_q, int H_kv, int* waves, int64_t* ctas) {
   const int qpw = 32 / (H_q / H_kv);
   const int need = (seqs->max_q_rows + qpw - 1) / qpw;
@@ -1015,6 +1025,11 @@ Plan plan_of(const msa_seqs* seqs, int H_q, int H_kv, int* waves, int64_t* ctas)
   const int64_t held = *waves == 8 || *waves == 1 ? 256 : 512;
   const int64_t blocks = (static_cast<int64_t>(seqs->max_kv_len) + kSub - 1) / kSub;
   if (seqs->num_seqs > kMaxSplitSeqs || *ctas >= 4 * held || tiles * blocks >= (int64_t(1) << 30)) return pl;
+  const int64_t per_seq = (seqs->max_q_rows + pl.qt - 1) / pl.qt;
+  const int64_t work = std::min<int64_t>(tiles, seqs->num_seqs * per_seq) * H_kv;    // CTAs with rows, at most
+  const int64_t rounds = (work + held - 1) / held;
+  const int64_t mean4 = seqs->num_seqs > 1 ? 3 : 4;
+  if (blocks * (4 * rounds * held - mean4 * work) <= 4 * held * (*waves == 1 ? kFewRowsGain : kTileGain)) return pl;
   pl.ctas = static_cast<int>(held / H_kv);
   pl.min_steps = 4;
   *ctas = static_cast<int64_t>(pl.ctas) * H_kv;

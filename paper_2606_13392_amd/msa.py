@@ -412,6 +412,10 @@ def dense_attn(q, k, v, seqs: Seqs, softmax_scale=None, out=None, lse=None, work
 
 
 # ---------------------------------------------------------------- dense attention on a paged cache
+def _ws_args(ws: Optional[torch.Tensor]):
+    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+
+
 def dense_attn_paged_workspace_size(seqs: Seqs, num_q_heads: int, num_kv_heads: int, head_dim: int = 128) -> int:
     return int(lib().msa_dense_attn_paged_workspace_size(seqs.ref(), num_q_heads, num_kv_heads, head_dim))
 
@@ -424,18 +428,20 @@ def _dense_paged(dtype, q, k, v, scales, seqs: Seqs, softmax_scale, out, lse, wo
     _need(k, "k", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
     _need(v, "v", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
     if out is None:
-        out = torch.empty((Tq, H_q, d_h), dtype=torch.bfloat16, device=dev)
+        out = torch.empty(Tq, H_q, d_h, dtype=torch.bfloat16, device=dev)
     else:
         _need(out, "o", torch.bfloat16, (Tq, H_q, d_h), dev)
     if lse is None:
-        lse = torch.empty((Tq, H_q), dtype=torch.float32, device=dev)
+        lse = torch.empty(Tq, H_q, dtype=torch.float32, device=dev)
     else:
         _need(lse, "lse", torch.float32, (Tq, H_q), dev)
     scale = 1.0 / math.sqrt(d_h) if softmax_scale is None else float(softmax_scale)
-    ws = _workspace(lib().msa_dense_attn_paged_workspace_size(seqs.ref(), H_q, H_kv, d_h), dev, workspace)
+    ref = seqs.ref()
+    if workspace is None:
+        workspace = _workspace(lib().msa_dense_attn_paged_workspace_size(ref, H_q, H_kv, d_h), dev, None)
     name, scales = ("msa_dense_attn_paged", ()) if scales is None else ("msa_dense_attn_paged_fp8", scales)
-    _call(name, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), *scales, seqs.ref(), H_q, H_kv, d_h, scale, out.data_ptr(),
-          lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    _call(name, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), *scales, ref, H_q, H_kv, d_h, scale, out.data_ptr(),
+          lse.data_ptr(), *_ws_args(workspace))
     return out, lse
 
 
@@ -578,52 +584,58 @@ def qk_norm_rope_backward_workspace_size(seqs: Seqs, num_q_heads: int, num_kv_he
     return int(lib().msa_qk_norm_rope_backward_workspace_size(seqs.ref(), num_q_heads, num_kv_heads, head_dim))
 
 
+def _grad_side(name, seqs: Seqs, x, g, w, d, dw):
+    """(input, its row stride, heads, gradient, its row stride, weight, its gradient) of q or k; no heads where the
+    tensor's upstream gradient is None."""
+    if g is None:
+        return None, 0, 0, None, 0, None, None
+    T, dev = seqs.total_q_rows, seqs.device
+    h, stride = _heads(g, f"d_{name}_out", T, dev)
+    dim = g.shape[2]
+    if stride != h * dim:
+        raise ValueError(f"d_{name}_out: must be contiguous")
+    x_ptr, x_stride, w_ptr = None, 0, None
+    if w is not None:
+        if x is None:
+            raise ValueError(f"{name}: needed for the norm's gradient")
+        hx, x_stride = _heads(x, name, T, dev)
+        if hx != h or x.shape[2] != dim:
+            raise ValueError(f"{name}: expected shape {tuple(g.shape)}, got {tuple(x.shape)}")
+        x_ptr, w_ptr = x.data_ptr(), _weight(w, f"{name}_weight", dim, dev)
+        if dw is None:
+            dw = torch.empty(dim, dtype=torch.float32, device=dev)
+        else:
+            _need(dw, f"d_{name}_weight", torch.float32, (dim,), dev)
+    elif dw is not None:
+        raise ValueError(f"d_{name}_weight: given without {name}_weight")
+    if d is None:
+        return x_ptr, x_stride, h, torch.empty(T, h, dim, dtype=torch.bfloat16, device=dev), h * dim, w_ptr, dw
+    hd, d_stride = _heads(d, f"d_{name}", T, dev)
+    if hd != h or d.shape[2] != dim:
+        raise ValueError(f"d_{name}: expected shape {tuple(g.shape)}, got {tuple(d.shape)}")
+    return x_ptr, x_stride, h, d, d_stride, w_ptr, dw
+
+
 def qk_norm_rope_backward(q, k, d_q_out, d_k_out, seqs: Seqs, rope: Optional[Rope], q_weight=None, k_weight=None,
                           eps: float = 1e-6, d_q=None, d_k=None, d_q_weight=None, d_k_weight=None, workspace=None):
     """Gradients of qk_norm_rope: (d_q, d_k, d_q_weight, d_k_weight); a weight's is None where it is None.  ``q`` and
     ``k`` are the forward's inputs (not read, and may be None, without weight); d_q and d_k may be columns of a wider
     tensor."""
-    T, dev = seqs.total_q_rows, seqs.device
-
-    def side(x, g, w, d, dw, name):
-        if g is None:
-            return None, 0, 0, None, None, 0, None, None, None
-        h, stride = _heads(g, f"d_{name}_out", T, dev)
-        dim = g.shape[2]
-        if T > 1 and stride != h * dim:
-            raise ValueError(f"d_{name}_out: must be contiguous")
-        x_stride = 0
-        if w is not None:
-            if x is None:
-                raise ValueError(f"{name}: needed for the norm's gradient")
-            hx, x_stride = _heads(x, name, T, dev)
-            if x.shape[1:] != g.shape[1:]:
-                raise ValueError(f"{name}: expected {tuple(g.shape)}, got {tuple(x.shape)}")
-        d = torch.empty((T, h, dim), dtype=torch.bfloat16, device=dev) if d is None else d
-        hd, d_stride = _heads(d, f"d_{name}", T, dev)
-        if d.shape[1:] != g.shape[1:]:
-            raise ValueError(f"d_{name}: expected {tuple(g.shape)}, got {tuple(d.shape)}")
-        if w is not None:
-            dw = torch.empty(dim, dtype=torch.float32, device=dev) if dw is None else dw
-            _need(dw, f"d_{name}_weight", torch.float32, (dim,), dev)
-        elif dw is not None:
-            raise ValueError(f"d_{name}_weight: given without {name}_weight")
-        return (x if w is not None else None), x_stride, h, g, d, d_stride, _weight(w, f"{name}_weight", dim, dev), dw, dim
-
-    q, q_stride, H_q, gq, d_q, d_q_stride, qw, d_qw, dim = side(q, d_q_out, q_weight, d_q, d_q_weight, "q")
-    k, k_stride, H_kv, gk, d_k, d_k_stride, kw, d_kw, dim_k = side(k, d_k_out, k_weight, d_k, d_k_weight, "k")
-    if gq is None and gk is None:
+    if d_q_out is None and d_k_out is None:
         raise ValueError("d_q_out or d_k_out is needed")
-    if gq is not None and gk is not None and dim != dim_k:
-        raise ValueError(f"d_k_out: expected head size {dim}, got {dim_k}")
-    dim = dim if gq is not None else dim_k
-    ws = workspace
-    if qw is not None or kw is not None:
-        ws = _workspace(lib().msa_qk_norm_rope_backward_workspace_size(seqs.ref(), H_q, H_kv, dim), dev, workspace)
-    _call("msa_qk_norm_rope_backward", dev, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(gq), _ptr(gk), seqs.ref(), H_q, H_kv,
-          dim, qw, kw, float(eps), _rope(rope, dev), _ptr(d_q), d_q_stride, _ptr(d_k), d_k_stride, _ptr(d_qw), _ptr(d_kw),
-          _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
-    return d_q, d_k, d_qw, d_kw
+    dev = seqs.device
+    q_in, q_stride, H_q, d_q, dq_stride, qw, d_q_weight = _grad_side("q", seqs, q, d_q_out, q_weight, d_q, d_q_weight)
+    k_in, k_stride, H_kv, d_k, dk_stride, kw, d_k_weight = _grad_side("k", seqs, k, d_k_out, k_weight, d_k, d_k_weight)
+    dim = (d_k_out if d_q_out is None else d_q_out).shape[2]
+    if d_k_out is not None and d_k_out.shape[2] != dim:
+        raise ValueError(f"d_k_out: expected head size {dim}, got {d_k_out.shape[2]}")
+    ref = seqs.ref()
+    if workspace is None and (qw is not None or kw is not None):
+        workspace = _workspace(lib().msa_qk_norm_rope_backward_workspace_size(ref, H_q, H_kv, dim), dev, None)
+    _call("msa_qk_norm_rope_backward", dev, q_in, q_stride, k_in, k_stride, _ptr(d_q_out), _ptr(d_k_out), ref, H_q, H_kv, dim,
+          qw, kw, float(eps), _rope(rope, dev), _ptr(d_q), dq_stride, _ptr(d_k), dk_stride, _ptr(d_q_weight), _ptr(d_k_weight),
+          *_ws_args(workspace))
+    return d_q, d_k, d_q_weight, d_k_weight
 
 
 def _append(fp8, k, v, scales, seqs: Seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
