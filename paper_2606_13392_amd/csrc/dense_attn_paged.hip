@@ -757,10 +757,8 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     u32x4 rk[NL], rv[NL];
     Rows<SMALL, NL> at;
     if (b_begin + wave < b_end) pw.start(b_begin + wave);
-    // The first pass only requests: each load stands once in the code, which is
-    // read from memory anew by every launch (with the first loads apart and
-    // paths of their own for whole sub-blocks, 30 KB instead of XXX, a call of
-    // one token on 8K keys took YYY us instead of ZZZ).
+    // the first pass only requests: each load stands once in the code (16 KB
+    // instead of 30, which every launch reads anew)
 #pragma unroll 1
     for (int b = b_begin + wave - kRowWaves; b < b_end; b += kRowWaves) {
       const bool now = b >= b_begin, more = b + kRowWaves < b_end;

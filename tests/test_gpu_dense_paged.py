@@ -185,6 +185,36 @@ def test_captured_with_lengths_that_grow(case):
         check_outputs(got[0].float().cpu().numpy()[rows], got[1].cpu().numpy()[rows], o_ref, l_ref, name)
 
 
+@pytest.mark.parametrize("page", [16, 64])
+def test_pool_past_4_gib(page):
+    """Pages whose bytes lie past 2^32 (and whose elements lie past 2^31): appended there, read from there."""
+    H, rows = 8, 2200000 // page * page                    # 4.5 GB each for k and v
+    free, _ = torch.cuda.mem_get_info()
+    if free < 12 << 30:
+        pytest.skip("needs 12 GB")
+    kv_lens, q_rows = [200, 90], [200, 1]
+    rng = np.random.default_rng(8)
+    need = [-(-n // page) for n in kv_lens]
+    last = rows // page - 1
+    table = np.zeros((2, max(need)), dtype=np.int32)
+    table[0, :need[0]] = last - rng.permutation(need[0])
+    table[1, :need[1]] = last - need[0] - rng.permutation(need[1])
+    pools = [torch.empty((rows, H, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    tab = torch.from_numpy(table).cuda()
+    x = [synth.bf16_bits_from_f32(rng.standard_normal((sum(kv_lens), H, D)).astype(np.float32)) for _ in range(2)]
+    whole = padded_seqs(kv_lens, kv_lens, total_kv=rows, table=tab, page=page)
+    msa.kv_append(to_dev(x[0]), to_dev(x[1]), whole, None, *pools)
+    q = synth.bf16_bits_from_f32(rng.standard_normal((sum(q_rows), 2 * H, D)).astype(np.float32))
+    seqs = padded_seqs(q_rows, kv_lens, total_kv=rows, table=tab, page=page)
+    o, l = msa.dense_attn_paged(to_dev(q), *pools, seqs)
+    one = padded_seqs([1, 1], kv_lens, total_kv=rows, table=tab, page=page)
+    o1, l1 = msa.dense_attn_paged(to_dev(q[[199, 200]]), *pools, one)
+    pick = [0, 63, 64, 130, 199, 200]
+    o_ref, l_ref = O.dense_causal_attention(q, *x, O.Layout(q_rows, kv_lens, [0, 200]), rows=pick)
+    check_outputs(o[pick].float().cpu().numpy(), l[pick].cpu().numpy(), o_ref, l_ref, "tiles")
+    check_outputs(o1.float().cpu().numpy(), l1.cpu().numpy(), o_ref[4:], l_ref[4:], "few rows")
+
+
 def test_pages_outside_the_pool_stay_inside_it():
     """Bad page ids are clamped: the call ends and writes finite rows (what they are is unspecified)."""
     table = torch.tensor([[5, -3, 1 << 30, 0]], dtype=torch.int32, device="cuda")
