@@ -319,7 +319,7 @@ int msa_dense_attn(const void* q, const void* k, const void* v, const msa_seqs* 
  * the lengths on the device: a result is bit-reproducible for equal inputs.
  *
  * Supported: head_dim == 128; 1 <= num_q_heads / num_kv_heads <= 16;
- * num_kv_heads <= 64; total_kv_rows < 2^31.
+ * num_kv_heads <= 64; total_kv_rows < 2^31; q, k, v and o 16-byte aligned.
  * ------------------------------------------------------------------------ */
 size_t msa_dense_attn_paged_workspace_size(const msa_seqs* seqs, int num_q_heads, int num_kv_heads,
                                            int head_dim);

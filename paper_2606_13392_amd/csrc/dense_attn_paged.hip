@@ -31,6 +31,8 @@
 // 8-bit MFMA (32x32x64, twice the bf16 rate) on the codes themselves drops
 // product bits some 2^-13 below the largest: LSE was off by up to 1.0e-4 on
 // sequences of 5 - 34 keys (bf16: 1e-6).
+#include <initializer_list>
+
 #include "flash_tile.h"
 
 namespace {
@@ -135,6 +137,7 @@ __device__ __forceinline__ SeqGeom bounded_geom(const msa_seqs& sq, int s) {
 // as many as the sequence's last, at least one.
 struct Steps {
   int cost[4];                           // steps of sequences 4 lane .. 4 lane + 3
+  int q_begin[4], q_rows[4], kv_len[4];  // their geometry (paged: kv_start is unused)
   int before;                            // steps of all sequences before them
   int total, per;                        // of the group; of a CTA
 
@@ -145,8 +148,13 @@ struct Steps {
     for (int i = 0; i < 4; ++i) {
       const int s = 4 * lane_id() + i;
       cost[i] = 0;
+      q_begin[i] = INT32_MAX;
+      q_rows[i] = kv_len[i] = 0;
       if (s < sq.num_seqs) {
         const SeqGeom g = bounded_geom(sq, s);
+        q_begin[i] = g.q_begin;
+        q_rows[i] = g.q_rows;
+        kv_len[i] = g.kv_len;
         cost[i] = (max(g.q_rows, 0) + pl.qt - 1) / pl.qt * blocks(g);
       }
       sum += cost[i];
@@ -185,6 +193,24 @@ struct Steps {
       }
     }
     return 4 * j + i;
+  }
+  // sequence of a query row: the last that begins at or before it
+  __device__ __forceinline__ int seq_of_row(int64_t row) const {
+    int n = -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) n += __popcll(__ballot(q_begin[e] <= row));
+    return n;
+  }
+  __device__ __forceinline__ SeqGeom geom(int s) const {
+    SeqGeom g{};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if ((s & 3) == e) {
+        g.q_begin = __builtin_amdgcn_readlane(q_begin[e], s >> 2);
+        g.q_rows = __builtin_amdgcn_readlane(q_rows[e], s >> 2);
+        g.kv_len = __builtin_amdgcn_readlane(kv_len[e], s >> 2);
+      }
+    return g;
   }
   // first step of sequence s
   __device__ __forceinline__ int first(int s) const {
@@ -294,12 +320,14 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   }
 
   int u = 0, u_end = 1, s = 0;
+  SeqGeom g{};
   if (pl.ctas > 0) {
     const Steps steps(sq, pl);
     u = cta * steps.per;
     u_end = min(steps.total, u + steps.per);
     if (u >= u_end) return;
     s = steps.seq_of(u);
+    g = steps.geom(s);
     if (threadIdx.x < kWave) steps.store(first);
     __syncthreads();
   }
@@ -307,8 +335,12 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
   while (u < u_end) {
     int tile, b_begin = 0, b_to = INT32_MAX;           // sub-blocks of this tile: to its last
     if (pl.ctas > 0) {
-      while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
-      const int nb = Steps::blocks(bounded_geom(sq, s)), off = u - first[s];
+      if (s + 1 < sq.num_seqs && first[s + 1] <= u) {
+        do ++s;
+        while (s + 1 < sq.num_seqs && first[s + 1] <= u);
+        g = bounded_geom(sq, s);
+      }
+      const int nb = Steps::blocks(g), off = u - first[s];
       tile = off / nb;
       b_begin = off - tile * nb;
       const int take = min(nb - b_begin, u_end - u);
@@ -316,9 +348,9 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
       u += take;
     } else {
       flash::locate_tile(sq, pl.gr, cta, qt, &s, &tile);
+      g = bounded_geom(sq, s);
       u = u_end;
     }
-    const SeqGeom g = bounded_geom(sq, s);
     const int t0 = tile * qt;
     const int base_p = g.kv_len - g.q_rows;  // position of the sequence's first query row
     int t_end = min(t0 + qt, g.q_rows);
@@ -348,17 +380,7 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
     if (b_begin < b_end) {
       PageWindow<SMALL> pw(sq, s, g.kv_len);
       pw.start(b_begin);
-      // the query rows, as the B operand of S^T
-      bf16x8 bq[KS];
-      {
-        const T* qrow = q + head_row * kDim + 8 * h;
-        Raw<T> rq[KS];
-#pragma unroll
-        for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
-#pragma unroll
-        for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
-      }
-
+      bf16x8 bq[KS];                          // the query rows, as the B operand of S^T
       // bf16 goes into LDS by DMA (copy); codes through registers (get, put)
       auto copy = [&](const char* base, const Rows<SMALL, N>& at, bool is_v, int buf) {
         const uint32_t lds = (is_v ? lds_v : lds_k) + buf * 2 * kSub * kDim + 1024 * wave;
@@ -579,6 +601,14 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
         next_rows(b_begin + 1);
         if (b_begin + 1 < b_end) copy(kb, at_k, false, (b_begin + 1) & 1);
       }
+      {
+        const T* qrow = q + head_row * kDim + 8 * h;
+        Raw<T> rq[KS];
+#pragma unroll
+        for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
+#pragma unroll
+        for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
+      }
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       if (live) {
@@ -680,12 +710,14 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
   auto piece_row = [&](int c) { return c * kRows + lrow; };
 
   int u = 0, u_end = 1, s = 0;
+  SeqGeom g{};
   if (pl.ctas > 0) {
     const Steps steps(sq, pl);
     u = cta * steps.per;
     u_end = min(steps.total, u + steps.per);
     if (u >= u_end) return;
     s = steps.seq_of(u);
+    g = steps.geom(s);
     if (threadIdx.x < kWave) steps.store(first);
     __syncthreads();
   }
@@ -693,8 +725,12 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
   while (u < u_end) {
     int tile, b_begin = 0, b_to = INT32_MAX;           // sub-blocks of this tile: to its last
     if (pl.ctas > 0) {
-      while (s + 1 < sq.num_seqs && first[s + 1] <= u) ++s;
-      const int nb = Steps::blocks(bounded_geom(sq, s)), off = u - first[s];
+      if (s + 1 < sq.num_seqs && first[s + 1] <= u) {
+        do ++s;
+        while (s + 1 < sq.num_seqs && first[s + 1] <= u);
+        g = bounded_geom(sq, s);
+      }
+      const int nb = Steps::blocks(g), off = u - first[s];
       tile = off / nb;
       b_begin = off - tile * nb;
       const int take = min(nb - b_begin, u_end - u);
@@ -702,9 +738,9 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
       u += take;
     } else {
       flash::locate_tile(sq, pl.gr, cta, qpw, &s, &tile);
+      g = bounded_geom(sq, s);
       u = u_end;
     }
-    const SeqGeom g = bounded_geom(sq, s);
     const int t0 = tile * qpw;
     const int base_p = g.kv_len - g.q_rows;            // position of the sequence's first query row
     int t_end = min(t0 + qpw, g.q_rows);
@@ -718,15 +754,6 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     const int p = valid ? base_p + t0 + jq : -1;
     const int nfree = (base_p + t0 + 1) / kSub;        // sub-blocks below it need no mask
 
-    bf16x8 bq[KS];
-    {
-      Raw<T> rq[KS];
-      const T* qrow = q + ((static_cast<int64_t>(g.q_begin) + (valid ? t0 + jq : t0)) * H_q + static_cast<int64_t>(r) * G + hh) * kDim + 8 * h;
-#pragma unroll
-      for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
-#pragma unroll
-      for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip);
-    }
     PageWindow<SMALL> pw(sq, s, g.kv_len);
     auto fetch = [&](const char* base, const Rows<SMALL, NL>& at, u32x4 (&dst)[NL]) {
 #pragma unroll
@@ -757,6 +784,14 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     u32x4 rk[NL], rv[NL];
     Rows<SMALL, NL> at;
     if (b_begin + wave < b_end) pw.start(b_begin + wave);
+    // the query rows stay as they are loaded: turned into operands here, they
+    // would be waited for before the first key is asked for
+    Raw<T> rq[KS];
+    {
+      const T* qrow = q + ((static_cast<int64_t>(g.q_begin) + (valid ? t0 + jq : t0)) * H_q + static_cast<int64_t>(r) * G + hh) * kDim + 8 * h;
+#pragma unroll
+      for (int st = 0; st < KS; ++st) rq[st] = valid ? load_raw(qrow + 16 * st) : Raw<T>{};
+    }
     // the first pass only requests: each load stands once in the code (16 KB
     // instead of 30, which every launch reads anew)
 #pragma unroll 1
@@ -780,7 +815,8 @@ __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
         acc_s[i] = f32x16{};
 #pragma unroll
         for (int st = 0; st < KS; ++st)
-          acc_s[i] = mfma32x32x16(ld_bf16x8(buf.k + (32 * i + n) * kDim + 8 * k_seg(n, 2 * st + h)), bq[st], acc_s[i]);
+          acc_s[i] = mfma32x32x16(ld_bf16x8(buf.k + (32 * i + n) * kDim + 8 * k_seg(n, 2 * st + h)),
+                                  __builtin_bit_cast(bf16x8, widen(rq[st]) ^ q_flip), acc_s[i]);
       }
       if (b >= nfree) {
 #pragma unroll
@@ -917,9 +953,9 @@ __global__ __launch_bounds__(256) void merge_kernel(msa_seqs sq, Plan pl, Parts 
   const int64_t row = pair / H_kv;
   const int r = static_cast<int>(pair % H_kv);
   if (row >= sq.total_q_rows) return;
-  const int s = find_seq_wave(sq.q_offsets, sq.num_seqs, row);
   const Steps steps(sq, pl);
-  const SeqGeom g = bounded_geom(sq, s);
+  const int s = steps.seq_of_row(row);
+  const SeqGeom g = steps.geom(s);
   const int t = static_cast<int>(row - g.q_begin);
   if (t >= g.q_rows) return;
   const int G = H_q / H_kv;
@@ -938,29 +974,48 @@ __global__ __launch_bounds__(256) void merge_kernel(msa_seqs sq, Plan pl, Parts 
     auto part_row = [&](int j) {         // of the CTA's two parts: the tile's beginning, or not
       return (2 * (static_cast<int64_t>(c0 + j) * H_kv + r) + (j == 0 ? 1 : 0)) * rows_per_tile + slot;
     };
-    float a = -INFINITY;
-    for (int j = l16; j < np; j += 16) a = fmaxf(a, parts.lse[part_row(j)]);
-    auto each = [&](auto f) {            // over the 16 lanes of a group
-      a = f(a, __uint_as_float(xor_lane_u32<1>(__float_as_uint(a))));
-      a = f(a, __uint_as_float(xor_lane_u32<2>(__float_as_uint(a))));
-      a = f(a, __uint_as_float(xor_lane_u32<4>(__float_as_uint(a))));
-      a = f(a, __uint_as_float(xor_lane_u32<8>(__float_as_uint(a))));
-    };
-    each([](float x, float y) { return fmaxf(x, y); });
-    const float top = a > -INFINITY ? a : 0.f;   // every part empty: all weights are zero
-    float sum = 0.f;
+    // parts in batches whose loads are under way together
+    constexpr int kBatch = HEADS == 4 ? 4 : 8;
+    float top = -INFINITY, sum = 0.f;
     f32x4 x0{}, x1{};
-#pragma unroll 4
-    for (int j = HEADS == 4 ? 0 : l4; j < np; j += kShare) {
-      const int64_t at = part_row(j);
-      const float w = exp2_hw(parts.lse[at] - top);
-      const f32x4* src = reinterpret_cast<const f32x4*>(parts.o + at * kDim + 8 * l16);
-      sum += w;
-      x0 += src[0] * w;
-      x1 += src[1] * w;
+    for (int j0 = HEADS == 4 ? 0 : l4; j0 < np; j0 += kShare * kBatch) {
+      float l[kBatch];
+      f32x4 y[kBatch][2];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const int64_t at = part_row(min(j0 + kShare * e, np - 1));
+        l[e] = parts.lse[at];
+        const f32x4* src = reinterpret_cast<const f32x4*>(parts.o + at * kDim + 8 * l16);
+        y[e][0] = src[0];
+        y[e][1] = src[1];
+      }
+      float m = top;
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        l[e] = j0 + kShare * e < np ? l[e] : -INFINITY;
+        m = fmaxf(m, l[e]);
+      }
+      const float base = m > -INFINITY ? m : 0.f;    // every part empty: all weights are zero
+      const float f = exp2_hw(top - base);
+      top = m;
+      sum *= f;
+      x0 *= f;
+      x1 *= f;
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const float w = exp2_hw(l[e] - base);
+        sum += w;
+        x0 += y[e][0] * w;
+        x1 += y[e][1] * w;
+      }
     }
     if constexpr (HEADS == 1) {
-      auto join = [](float v) {
+      float m = fmaxf(top, __uint_as_float(xor_lane_u32<16>(__float_as_uint(top))));
+      m = fmaxf(m, __uint_as_float(xor_lane_u32<32>(__float_as_uint(m))));
+      const float f = exp2_hw(top - (m > -INFINITY ? m : 0.f));
+      top = m;
+      auto join = [&](float v) {
+        v *= f;
         v += __uint_as_float(xor_lane_u32<16>(__float_as_uint(v)));
         return v + __uint_as_float(xor_lane_u32<32>(__float_as_uint(v)));
       };
@@ -1045,6 +1100,8 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
   if (fp8 && (!scale_ok(q_scale) || !scale_ok(k_scale) || !scale_ok(v_scale))) return MSA_ERR_INVALID;
   if (seqs->total_q_rows == 0) return MSA_OK;
   if (!q || !k || !v || !o || !lse) return MSA_ERR_INVALID;
+  for (const void* x : {q, k, v, static_cast<const void*>(o)})
+    if (reinterpret_cast<uintptr_t>(x) & 15) return MSA_ERR_UNSUPPORTED;   // 16-byte pieces
   const flash::LogitScale scale = flash::logit_scale(softmax_scale * q_scale * k_scale * kLog2E);
   const int G = H_q / H_kv;
   int waves;

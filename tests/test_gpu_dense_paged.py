@@ -185,6 +185,23 @@ def test_captured_with_lengths_that_grow(case):
         check_outputs(got[0].float().cpu().numpy()[rows], got[1].cpu().numpy()[rows], o_ref, l_ref, name)
 
 
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace and outputs of its own, give the bits of calls one after the other."""
+    made = [_make(CASES[i], False) for i in (12, 3)]
+    want = [msa.dense_attn_paged(*d, seqs) for _, d, seqs, _, _ in made]
+    streams = [torch.cuda.Stream() for _ in made]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for st, (_, d, seqs, _, _) in zip(streams, made):
+            with torch.cuda.stream(st):
+                got.append(msa.dense_attn_paged(*d, seqs))
+        torch.cuda.synchronize()
+        for (o, l), (o2, l2), case in zip(want, got, (CASES[12], CASES[3])):
+            n = sum(case[1])
+            assert torch.equal(o[:n], o2[:n]) and torch.equal(l[:n], l2[:n])
+
+
 @pytest.mark.parametrize("page", [16, 64])
 def test_pool_past_4_gib(page):
     """Pages whose bytes lie past 2^32 (and whose elements lie past 2^31): appended there, read from there."""

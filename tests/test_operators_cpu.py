@@ -133,20 +133,35 @@ PAGED_BAD = [
     (dict(seqs=_paged(page_size=16384, total_kv_rows=1 << 20)), INV), (dict(seqs=_paged(block_table_stride=1)), INV),
     (dict(seqs=_paged(total_kv_rows=1 << 31)), UNS), (dict(d=64), UNS), (dict(H=6, K=4), INV), (dict(H=34, K=2), UNS),
     (dict(H=65, K=65), UNS), (dict(q=None), INV), (dict(k=None), INV), (dict(v=None), INV), (dict(o=None), INV),
-    (dict(lse=None), INV),
+    (dict(lse=None), INV), (dict(q=8), UNS), (dict(k=24), UNS), (dict(v=40), UNS), (dict(o=56), UNS),
 ]
 
 
 @pytest.mark.parametrize("kw,want", PAGED_BAD)
 def test_dense_paged_refuses(kw, want):
-    a = dict(q=8, k=8, v=8, seqs=_paged(), H=8, K=2, d=128, o=8, lse=8)
+    a = dict(q=16, k=16, v=16, seqs=_paged(), H=8, K=2, d=128, o=16, lse=8)
     a.update(kw)
     L, s = msa.lib(), ctypes.byref(a["seqs"])
     tail = (s, a["H"], a["K"], a["d"], 0.1, a["o"], a["lse"], 8, 1 << 40, None)
     assert L.msa_dense_attn_paged(a["q"], a["k"], a["v"], *tail) == want
     assert L.msa_dense_attn_paged_fp8(a["q"], a["k"], a["v"], 1.0, 1.0, 1.0, *tail) == want
-    if all(a[n] is not None for n in ("q", "k", "v", "o", "lse")):
+    if set(kw) <= {"seqs", "d", "H", "K"}:
         assert L.msa_dense_attn_paged_workspace_size(s, a["H"], a["K"], a["d"]) == 0
+
+
+def test_dense_paged_workspace():
+    """Parts of two tiles for every CTA of a split call; none where the keys are not split; too small a one is refused
+    before anything is launched."""
+    L = msa.lib()
+    long = _paged(num_seqs=4, total_q_rows=4, max_q_rows=1, max_kv_len=65536, block_table_stride=1024, total_kv_rows=1 << 20)
+    need = L.msa_dense_attn_paged_workspace_size(ctypes.byref(long), 64, 8, 128)
+    assert need == 4 * 2 * 256 * 32 * 129
+    call = lambda ws, n: L.msa_dense_attn_paged(16, 16, 16, ctypes.byref(long), 64, 8, 128, 0.1, 16, 16, ws, n, None)  # noqa: E731
+    assert call(16, need - 1) == WS and call(None, need) == WS
+    short = _paged(num_seqs=4, total_q_rows=4, max_q_rows=1, max_kv_len=128)
+    assert L.msa_dense_attn_paged_workspace_size(ctypes.byref(short), 64, 8, 128) == 0
+    many = _paged(num_seqs=300, total_q_rows=300, max_q_rows=1, max_kv_len=65536, block_table_stride=1024, total_kv_rows=1 << 20)
+    assert L.msa_dense_attn_paged_workspace_size(ctypes.byref(many), 64, 8, 128) == 0
 
 
 # ------------------------------------------------------------------ binding
