@@ -147,17 +147,15 @@ def _stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
-def _call(name: str, device: torch.device, *args) -> None:
-    """The library's call ``name`` with the current stream of ``device`` as its last argument, whichever device is
-    current."""
-    fn, cur = getattr(_lib or lib(), name), torch._C._cuda_getDevice()
-    if cur == device.index:
-        st = fn(*args, torch._C._cuda_getCurrentRawStream(cur))
-    else:
-        with torch.cuda.device(device):
-            st = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
-    if st != MSA_OK:
-        _check(st, name)
+def _raw_stream(device: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _current(device: torch.device) -> bool:
+    """Whether the GPU ``device`` is the current one (calls launch there)."""
+    if device.type != "cuda":
+        raise ValueError(f"expected tensors on a GPU, got {device}")
+    return torch._C._cuda_getDevice() == device.index
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -412,21 +410,20 @@ def dense_attn(q, k, v, seqs: Seqs, softmax_scale=None, out=None, lse=None, work
 
 
 # ---------------------------------------------------------------- dense attention on a paged cache
-def _ws_args(ws: Optional[torch.Tensor]):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
-
-
 def dense_attn_paged_workspace_size(seqs: Seqs, num_q_heads: int, num_kv_heads: int, head_dim: int = 128) -> int:
     return int(lib().msa_dense_attn_paged_workspace_size(seqs.ref(), num_q_heads, num_kv_heads, head_dim))
 
 
 def _dense_paged(dtype, q, k, v, scales, seqs: Seqs, softmax_scale, out, lse, workspace):
+    dev = seqs.device
     Tq, H_q, d_h = q.shape
     H_kv = k.shape[1]
-    dev = seqs.device
     _need(q, "q", dtype, (seqs.total_q_rows, H_q, d_h), dev)
     _need(k, "k", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
     _need(v, "v", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return _dense_paged(dtype, q, k, v, scales, seqs, softmax_scale, out, lse, workspace)
     if out is None:
         out = torch.empty(Tq, H_q, d_h, dtype=torch.bfloat16, device=dev)
     else:
@@ -436,12 +433,17 @@ def _dense_paged(dtype, q, k, v, scales, seqs: Seqs, softmax_scale, out, lse, wo
     else:
         _need(lse, "lse", torch.float32, (Tq, H_q), dev)
     scale = 1.0 / math.sqrt(d_h) if softmax_scale is None else float(softmax_scale)
-    ref = seqs.ref()
+    L, ref = lib(), seqs.ref()
     if workspace is None:
-        workspace = _workspace(lib().msa_dense_attn_paged_workspace_size(ref, H_q, H_kv, d_h), dev, None)
-    name, scales = ("msa_dense_attn_paged", ()) if scales is None else ("msa_dense_attn_paged_fp8", scales)
-    _call(name, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), *scales, ref, H_q, H_kv, d_h, scale, out.data_ptr(),
-          lse.data_ptr(), *_ws_args(workspace))
+        workspace = _workspace(L.msa_dense_attn_paged_workspace_size(ref, H_q, H_kv, d_h), dev, None)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    if scales is None:
+        st = L.msa_dense_attn_paged(q.data_ptr(), k.data_ptr(), v.data_ptr(), ref, H_q, H_kv, d_h, scale, out.data_ptr(),
+                                    lse.data_ptr(), ws, ws_bytes, _raw_stream(dev))
+    else:
+        st = L.msa_dense_attn_paged_fp8(q.data_ptr(), k.data_ptr(), v.data_ptr(), *scales, ref, H_q, H_kv, d_h, scale,
+                                        out.data_ptr(), lse.data_ptr(), ws, ws_bytes, _raw_stream(dev))
+    _check(st, "msa_dense_attn_paged" if scales is None else "msa_dense_attn_paged_fp8")
     return out, lse
 
 
@@ -508,19 +510,20 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
 
 
 def _heads(t: torch.Tensor, name: str, rows: int, device):
-    """(heads, row stride) of a [rows, heads, dim] bf16 tensor whose rows may be apart (columns of a wider one)."""
-    shape = t.shape
-    if t.dtype == torch.bfloat16 and len(shape) == 3 and shape[0] == rows and t.device == device:
-        stride = t.stride()
-        _, h, d = shape
-        if (stride[2] == 1 or d == 1) and (stride[1] == d or h == 1):
-            return h, (stride[0] if rows > 1 else h * d)
-        raise ValueError(f"{name}: a row's heads must be contiguous")
+    """(heads, head size, row stride) of a [rows, heads, dim] bf16 tensor whose rows may be apart (columns of a wider
+    one)."""
+    if t.dtype is torch.bfloat16 and t.dim() == 3 and t.device == device:
+        n, h, d = t.shape
+        if n == rows:
+            sr, sh, sd = t.stride()
+            if (sd == 1 or d == 1) and (sh == d or h == 1):
+                return h, d, (sr if rows > 1 else h * d)
+            raise ValueError(f"{name}: a row's heads must be contiguous")
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name}: expected device {device}, got {t.device}")
-    raise ValueError(f"{name}: expected shape ({rows}, heads, dim), got {tuple(shape)}")
+    raise ValueError(f"{name}: expected shape ({rows}, heads, dim), got {tuple(t.shape)}")
 
 
 def _weight(w: Optional[torch.Tensor], name: str, dim: int, device):
@@ -538,32 +541,39 @@ def _rope(rope: Optional[Rope], device):
     return rope.ref()
 
 
-def _norm_rope(fp8, q, k, scales, seqs: Seqs, rope, q_weight, k_weight, eps, q_out, k_out):
-    T, dev = seqs.total_q_rows, seqs.device
-    H_q, q_stride = _heads(q, "q", T, dev)
-    d = q.shape[2]
-    H_kv, k_stride = 0, 0
+def _norm_rope(scales, q, k, seqs: Seqs, rope, q_weight, k_weight, eps, q_out, k_out):
+    dev, T = seqs.device, seqs.total_q_rows
+    dtype = torch.bfloat16 if scales is None else torch.uint8
+    H_q, d, q_stride = _heads(q, "q", T, dev)
+    H_kv, k_stride, k_ptr, k_out_ptr = 0, 0, None, None
     if k is not None:
-        H_kv, k_stride = _heads(k, "k", T, dev)
-        if k.shape[2] != d:
-            raise ValueError(f"k: expected head size {d}, got {k.shape[2]}")
-    dtype = torch.uint8 if fp8 else torch.bfloat16
-    if q_out is None:
-        q_out = torch.empty(T, H_q, d, dtype=dtype, device=dev)
-    else:
+        H_kv, d_k, k_stride = _heads(k, "k", T, dev)
+        if d_k != d:
+            raise ValueError(f"k: expected head size {d}, got {d_k}")
+    elif k_out is not None:
+        raise ValueError("k_out: given without k")
+    qw, kw = _weight(q_weight, "q_weight", d, dev), _weight(k_weight, "k_weight", d, dev)
+    if q_out is not None:
         _need(q_out, "q_out", dtype, (T, H_q, d), dev)
     if k_out is not None:
         _need(k_out, "k_out", dtype, (T, H_kv, d), dev)
-    elif k is not None:
-        k_out = torch.empty(T, H_kv, d, dtype=dtype, device=dev)
-    shared = (seqs.ref(), H_q, H_kv, d, _weight(q_weight, "q_weight", d, dev), _weight(k_weight, "k_weight", d, dev), float(eps),
-              _rope(rope, dev), q_out.data_ptr(), None if k_out is None else k_out.data_ptr())
-    k_ptr = None if k is None else k.data_ptr()
-    if fp8:
-        q_scale, k_scale = scales
-        _call("msa_qk_norm_rope_fp8", dev, q.data_ptr(), q_stride, k_ptr, k_stride, float(q_scale), float(k_scale), *shared)
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return _norm_rope(scales, q, k, seqs, rope, q_weight, k_weight, eps, q_out, k_out)
+    if q_out is None:
+        q_out = torch.empty(T, H_q, d, dtype=dtype, device=dev)
+    if k is not None:
+        if k_out is None:
+            k_out = torch.empty(T, H_kv, d, dtype=dtype, device=dev)
+        k_ptr, k_out_ptr = k.data_ptr(), k_out.data_ptr()
+    if scales is None:
+        st = lib().msa_qk_norm_rope(q.data_ptr(), q_stride, k_ptr, k_stride, seqs.ref(), H_q, H_kv, d, qw, kw, float(eps),
+                                    _rope(rope, dev), q_out.data_ptr(), k_out_ptr, _raw_stream(dev))
     else:
-        _call("msa_qk_norm_rope", dev, q.data_ptr(), q_stride, k_ptr, k_stride, *shared)
+        q_scale, k_scale = scales
+        st = lib().msa_qk_norm_rope_fp8(q.data_ptr(), q_stride, k_ptr, k_stride, float(q_scale), float(k_scale), seqs.ref(), H_q,
+                                        H_kv, d, qw, kw, float(eps), _rope(rope, dev), q_out.data_ptr(), k_out_ptr, _raw_stream(dev))
+    _check(st, "msa_qk_norm_rope" if scales is None else "msa_qk_norm_rope_fp8")
     return q_out, k_out
 
 
@@ -571,13 +581,13 @@ def qk_norm_rope(q, k, seqs: Seqs, rope: Optional[Rope], q_weight=None, k_weight
                  q_out=None, k_out=None):
     """Norm of each head and rotation by position of the new rows' q [Tq, H_q, d] and k [Tq, H_kv, d] (bf16; rows
     may be columns of a wider tensor; ``k`` may be None): (q_out, k_out), contiguous bf16."""
-    return _norm_rope(False, q, k, None, seqs, rope, q_weight, k_weight, eps, q_out, k_out)
+    return _norm_rope(None, q, k, seqs, rope, q_weight, k_weight, eps, q_out, k_out)
 
 
 def qk_norm_rope_fp8(q, k, scales, seqs: Seqs, rope: Optional[Rope], q_weight=None, k_weight=None, eps: float = 1e-6,
                      q_out=None, k_out=None):
     """The same into e4m3 codes (uint8) with per-tensor scales (q, k)."""
-    return _norm_rope(True, q, k, scales, seqs, rope, q_weight, k_weight, eps, q_out, k_out)
+    return _norm_rope(scales, q, k, seqs, rope, q_weight, k_weight, eps, q_out, k_out)
 
 
 def qk_norm_rope_backward_workspace_size(seqs: Seqs, num_q_heads: int, num_kv_heads: int, head_dim: int) -> int:
@@ -590,16 +600,15 @@ def _grad_side(name, seqs: Seqs, x, g, w, d, dw):
     if g is None:
         return None, 0, 0, None, 0, None, None
     T, dev = seqs.total_q_rows, seqs.device
-    h, stride = _heads(g, f"d_{name}_out", T, dev)
-    dim = g.shape[2]
+    h, dim, stride = _heads(g, f"d_{name}_out", T, dev)
     if stride != h * dim:
         raise ValueError(f"d_{name}_out: must be contiguous")
     x_ptr, x_stride, w_ptr = None, 0, None
     if w is not None:
         if x is None:
             raise ValueError(f"{name}: needed for the norm's gradient")
-        hx, x_stride = _heads(x, name, T, dev)
-        if hx != h or x.shape[2] != dim:
+        hx, dim_x, x_stride = _heads(x, name, T, dev)
+        if hx != h or dim_x != dim:
             raise ValueError(f"{name}: expected shape {tuple(g.shape)}, got {tuple(x.shape)}")
         x_ptr, w_ptr = x.data_ptr(), _weight(w, f"{name}_weight", dim, dev)
         if dw is None:
@@ -610,8 +619,8 @@ def _grad_side(name, seqs: Seqs, x, g, w, d, dw):
         raise ValueError(f"d_{name}_weight: given without {name}_weight")
     if d is None:
         return x_ptr, x_stride, h, torch.empty(T, h, dim, dtype=torch.bfloat16, device=dev), h * dim, w_ptr, dw
-    hd, d_stride = _heads(d, f"d_{name}", T, dev)
-    if hd != h or d.shape[2] != dim:
+    hd, dim_d, d_stride = _heads(d, f"d_{name}", T, dev)
+    if hd != h or dim_d != dim:
         raise ValueError(f"d_{name}: expected shape {tuple(g.shape)}, got {tuple(d.shape)}")
     return x_ptr, x_stride, h, d, d_stride, w_ptr, dw
 
@@ -629,63 +638,76 @@ def qk_norm_rope_backward(q, k, d_q_out, d_k_out, seqs: Seqs, rope: Optional[Rop
     dim = (d_k_out if d_q_out is None else d_q_out).shape[2]
     if d_k_out is not None and d_k_out.shape[2] != dim:
         raise ValueError(f"d_k_out: expected head size {dim}, got {d_k_out.shape[2]}")
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return qk_norm_rope_backward(q, k, d_q_out, d_k_out, seqs, rope, q_weight, k_weight, eps, d_q, d_k, d_q_weight,
+                                         d_k_weight, workspace)
     ref = seqs.ref()
     if workspace is None and (qw is not None or kw is not None):
         workspace = _workspace(lib().msa_qk_norm_rope_backward_workspace_size(ref, H_q, H_kv, dim), dev, None)
-    _call("msa_qk_norm_rope_backward", dev, q_in, q_stride, k_in, k_stride, _ptr(d_q_out), _ptr(d_k_out), ref, H_q, H_kv, dim,
-          qw, kw, float(eps), _rope(rope, dev), _ptr(d_q), dq_stride, _ptr(d_k), dk_stride, _ptr(d_q_weight), _ptr(d_k_weight),
-          *_ws_args(workspace))
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    st = lib().msa_qk_norm_rope_backward(
+        q_in, q_stride, k_in, k_stride, _ptr(d_q_out), _ptr(d_k_out), ref, H_q, H_kv, dim, qw, kw, float(eps),
+        _rope(rope, dev), _ptr(d_q), dq_stride, _ptr(d_k), dk_stride, _ptr(d_q_weight), _ptr(d_k_weight), ws, ws_bytes, _raw_stream(dev))
+    _check(st, "msa_qk_norm_rope_backward")
     return d_q, d_k, d_q_weight, d_k_weight
 
 
-def _append(fp8, k, v, scales, seqs: Seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
+def _append(scales, k, v, seqs: Seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
             index_rope):
-    T, dev = seqs.total_q_rows, seqs.device
-    H_kv, k_stride = _heads(k, "k", T, dev)
-    H_v, v_stride = _heads(v, "v", T, dev)
-    d = k.shape[2]
-    if v.shape != k.shape:
+    dev, T = seqs.device, seqs.total_q_rows
+    H_kv, d, k_stride = _heads(k, "k", T, dev)
+    H_v, d_v, v_stride = _heads(v, "v", T, dev)
+    if H_v != H_kv or d_v != d:
         raise ValueError(f"v: expected shape {tuple(k.shape)}, got {tuple(v.shape)}")
-    dtype = torch.uint8 if fp8 else torch.bfloat16
+    dtype = torch.bfloat16 if scales is None else torch.uint8
     _need(k_cache, "k_cache", dtype, (seqs.total_kv_rows, H_kv, d), dev)
     _need(v_cache, "v_cache", dtype, (seqs.total_kv_rows, H_kv, d), dev)
-    d_idx, i_stride, iw, ir = 0, 0, None, None
+    d_idx, i_stride, i_ptr, ic_ptr, iw, ir = 0, 0, None, None, None, None
     if (index_k is None) != (index_k_cache is None):
         raise ValueError("index_k and index_k_cache go together")
     if index_k is not None:
-        if index_k.dim() != 2:
-            raise ValueError(f"index_k: expected shape ({T}, d_idx), got {tuple(index_k.shape)}")
-        d_idx = index_k.shape[1]
-        if index_k.dtype != torch.bfloat16:
+        if index_k.dtype is not torch.bfloat16:
             raise TypeError(f"index_k: expected torch.bfloat16, got {index_k.dtype}")
-        if index_k.shape[0] != T or index_k.device != dev:
-            raise ValueError(f"index_k: expected {T} rows on {dev}, got {index_k.shape[0]} on {index_k.device}")
-        if index_k.stride(1) != 1 and d_idx != 1:
+        if index_k.dim() != 2 or index_k.shape[0] != T or index_k.device != dev:
+            raise ValueError(f"index_k: expected shape ({T}, d_idx) on {dev}, got {tuple(index_k.shape)} on {index_k.device}")
+        d_idx = index_k.shape[1]
+        i_stride, step = index_k.stride()
+        if step != 1 and d_idx != 1:
             raise ValueError("index_k: a row must be contiguous")
-        i_stride = index_k.stride(0) if T > 1 else d_idx
+        if T <= 1:
+            i_stride = d_idx
         _need(index_k_cache, "index_k_cache", torch.bfloat16, (seqs.total_kv_rows, d_idx), dev)
-        iw = _weight(index_k_weight, "index_k_weight", d_idx, dev)
-        ir = _rope(index_rope, dev)
-    shared = (_ptr(index_k), i_stride, seqs.ref(), H_kv, d, d_idx, _weight(k_weight, "k_weight", d, dev), iw, float(eps),
-              _rope(rope, dev), ir, k_cache.data_ptr(), v_cache.data_ptr(), _ptr(index_k_cache))
-    if fp8:
-        k_scale, v_scale = scales
-        _call("msa_kv_append_fp8", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, float(k_scale), float(v_scale), *shared)
+        i_ptr, ic_ptr = index_k.data_ptr(), index_k_cache.data_ptr()
+        iw, ir = _weight(index_k_weight, "index_k_weight", d_idx, dev), _rope(index_rope, dev)
+    kw = _weight(k_weight, "k_weight", d, dev)
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return _append(scales, k, v, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
+                           index_rope)
+    if scales is None:
+        st = lib().msa_kv_append(k.data_ptr(), k_stride, v.data_ptr(), v_stride, i_ptr, i_stride, seqs.ref(), H_kv, d, d_idx,
+                                 kw, iw, float(eps), _rope(rope, dev), ir, k_cache.data_ptr(), v_cache.data_ptr(), ic_ptr,
+                                 _raw_stream(dev))
     else:
-        _call("msa_kv_append", dev, k.data_ptr(), k_stride, v.data_ptr(), v_stride, *shared)
+        k_scale, v_scale = scales
+        st = lib().msa_kv_append_fp8(k.data_ptr(), k_stride, v.data_ptr(), v_stride, float(k_scale), float(v_scale), i_ptr,
+                                     i_stride, seqs.ref(), H_kv, d, d_idx, kw, iw, float(eps), _rope(rope, dev), ir,
+                                     k_cache.data_ptr(), v_cache.data_ptr(), ic_ptr, _raw_stream(dev))
+    _check(st, "msa_kv_append" if scales is None else "msa_kv_append_fp8")
 
 
 def kv_append(k, v, seqs: Seqs, rope: Optional[Rope], k_cache, v_cache, k_weight=None, eps: float = 1e-6, index_k=None,
               index_k_cache=None, index_k_weight=None, index_rope: Optional[Rope] = None) -> None:
     """The new rows' k (norm, rotation), v and index_k (norm, rotation) into their cache rows, in place."""
-    _append(False, k, v, None, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
+    _append(None, k, v, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
             index_rope)
 
 
 def kv_append_fp8(k, v, scales, seqs: Seqs, rope: Optional[Rope], k_cache, v_cache, k_weight=None, eps: float = 1e-6,
                   index_k=None, index_k_cache=None, index_k_weight=None, index_rope: Optional[Rope] = None) -> None:
     """The same with e4m3 k and v caches (uint8) and per-tensor scales (k, v); index keys stay bf16."""
-    _append(True, k, v, scales, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
+    _append(scales, k, v, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
             index_rope)
 
 
