@@ -374,7 +374,9 @@ typedef struct msa_rope {
  * bf16 outputs may be the inputs themselves where those are contiguous; other
  * overlaps are not allowed.  Rows behind the last sequence are left as they are.
  * With eps 0 a head of zeros gives NaN; sums of squares beyond fp32 (elements
- * of about 2^60) give 0.  No workspace.
+ * of about 2^60) give 0.  bf16 elements that neither a norm nor the rotation
+ * applies to keep their bits.  A scale is from 2^-126 to 2^126 (else
+ * MSA_ERR_INVALID).  No workspace.
  *
  * Supported: head_dim 64 or 128; up to 1024 heads each; strides a multiple of 4
  * elements, tensors 8-byte aligned (else MSA_ERR_UNSUPPORTED).
@@ -444,7 +446,8 @@ int msa_qk_norm_rope_backward(const void* q, int64_t q_stride, const void* k, in
  *              [total_kv_rows, num_kv_heads, head_dim]   UPDATED
  *   index_k_cache      bf16 [total_kv_rows, d_idx]        UPDATED
  *
- * Values are stored as they are (bf16) or as codes.  No workspace.
+ * Values are stored bit for bit (bf16) or as codes; scales as for
+ * msa_qk_norm_rope_fp8.  No workspace.
  * Supported: head_dim == 128; num_kv_heads <= 64; d_idx 64 or 128; contiguous, or
  * pages of a power of two from 16 to 8192 rows; strides and alignment as for
  * msa_qk_norm_rope.

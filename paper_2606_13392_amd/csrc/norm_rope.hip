@@ -19,6 +19,7 @@
 // Small ones by a chain of latencies (launch, rows, angles, elements): 64 rows
 // 4.3 us.
 #include <algorithm>
+#include <cfloat>
 
 #include "msa_common.h"
 #include "msa_profile.h"
@@ -243,9 +244,11 @@ __device__ __forceinline__ int run_part(const Part& pt, const Spec& sp, int64_t 
         *reinterpret_cast<uint32_t*>(y + d.a) = code4(u, pt.inv_scale);
         *reinterpret_cast<uint32_t*>(y + d.b) = code4(v, pt.inv_scale);
       } else {
+        // elements that nothing is applied to keep their bits (NaN payloads too)
+        const bool same = !pt.w && d.ang < 0;
         uint16_t* y = static_cast<uint16_t*>(pt.y) + to;
-        *reinterpret_cast<uint2*>(y + d.a) = pack4(u);
-        *reinterpret_cast<uint2*>(y + d.b) = pack4(v);
+        *reinterpret_cast<uint2*>(y + d.a) = same ? xa : pack4(u);
+        *reinterpret_cast<uint2*>(y + d.b) = same ? xb : pack4(v);
       }
     }
   }
@@ -520,7 +523,8 @@ int launch_forward(const char* name, Parts a, const msa_seqs* seqs, hipStream_t 
   return msa_host::launch_status();
 }
 
-bool scale_ok(float x) { return x > 0.f && x < 3.0e38f; }   // finite and positive
+// Positive, and with a reciprocal (which the codes are formed with) that is normal.
+bool scale_ok(float x) { return x >= FLT_MIN && x <= 1.f / FLT_MIN; }
 
 int validate_heads(const msa_seqs* seqs, int H_q, int H_kv, int dim, float eps, const msa_rope* rope) {
   int st = msa_host::validate_seqs(seqs);

@@ -140,6 +140,17 @@ def test_contiguous_rows_past_the_cache_are_dropped():
     assert torch.equal(guard, want)
 
 
+def test_values_keep_their_bits():
+    """Every bf16 pattern, NaN payloads, denormals and infinities among them, through v and the unrotated half of k."""
+    bits = torch.arange(65536, device="cuda", dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(512, 1, D)
+    seqs = padded_seqs([512], [512])
+    kc, vc = (torch.zeros((512, 1, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    _, rope = rope_pair(64, D, False, 1.0)
+    msa.kv_append(bits, bits, seqs, rope, kc, vc)
+    assert torch.equal(vc.view(torch.int16), bits.view(torch.int16))
+    assert torch.equal(kc.view(torch.int16)[..., 64:], bits.view(torch.int16)[..., 64:])
+
+
 def test_captured():
     case = CASES[2]
     x, w, kd, vd, seqs, (_, rope, _), _, to, caches, kw, pos, inter, rng = _make(case, False)

@@ -66,6 +66,16 @@ def test_code_scales_are_finite_and_positive(scale):
     assert L.msa_dense_attn_paged_fp8(8, 8, 8, scale, 1.0, 1.0, p, 8, 2, 128, 0.1, 8, 8, 8, 1 << 30, None) == INV
 
 
+@pytest.mark.parametrize("scale", [1e-40, 2.0 ** 127])
+def test_code_scales_have_a_normal_reciprocal(scale):
+    """1e-40 has an infinite one in fp32: a zero would become NaN."""
+    L, s = msa.lib(), ctypes.byref(_seqs())
+    for pair in ((scale, 1.0), (1.0, scale)):
+        assert L.msa_qk_norm_rope_fp8(8, 1024, 8, 256, *pair, s, 8, 2, 128, None, None, 0.0, None, 8, 8, None) == INV
+        assert L.msa_kv_append_fp8(8, 256, 8, 256, *pair, None, 0, s, 2, 128, 0, None, None, 0.0, None, None, 8, 8, None,
+                                   None) == INV
+
+
 def test_no_rows_need_no_tensors():
     L, s = msa.lib(), ctypes.byref(_seqs(total_q_rows=0, max_q_rows=0))
     assert L.msa_qk_norm_rope(None, 0, None, 0, s, 8, 2, 128, None, None, 0.0, None, None, None, None) == msa.MSA_OK
