@@ -14,8 +14,9 @@
 // after the point left in 32), the cosine and sine of the reduced turn in 32.
 // Everything between the bf16 input and the one rounding of the output is fp32.
 //
-// Large calls are bound by HBM: 39426 rows of 64 + 4 heads of 128 264 us, the
-// backward of 32768 rows of 64 + 8 heads 350 us, both 5.2 TB/s and every byte once.
+// Large calls are bound by HBM: 39426 rows of 64 + 4 heads of 128 256 us,
+// 5.4 TB/s, the backward of 32768 rows of 64 + 8 heads 346 us, 5.2 TB/s, every byte
+// once.
 // Small ones by a chain of latencies (launch, rows, angles, elements): 64 rows
 // 4.3 us.
 #include <algorithm>
@@ -498,14 +499,16 @@ int64_t iterations(const Parts& a, int nparts, int64_t rows) {
   return n;
 }
 
-// Rows per CTA: enough for 16 iterations (the angles, the search for the rows'
-// sequences and the weights are shared by them) while there are more than
-// `ctas` CTAs.  Forward: 2048, eight per CU, which run at once (3929 rows of 64
-// + 4 heads into E4M3 24.7 us; with 1024 26.4, with 4096 26.0).
+// Rows per CTA: enough for 8 iterations, which share the angles, the search for the
+// rows' sequences and the weights, while there are more than `ctas` CTAs.  39426 rows
+// of 64 + 4 heads take 256 us, and the backward of 32768 rows of 64 + 8 heads 346;
+// with 4 iterations 277 and 378, with 16 263 and 351.  Forward: 2048 CTAs, eight per
+// CU, which run at once (3929 rows of 64 + 4 heads into E4M3 24.7 us; with 1024 26.4,
+// with 4096 26.0).
 constexpr int kCtas = 2048;
 int rows_per_cta(const Parts& a, int nparts, int64_t total, int ctas) {
   int rows = 1;
-  while (rows < kMaxRows && iterations(a, nparts, rows) < 16 && (total + rows - 1) / rows > ctas) rows *= 2;
+  while (rows < kMaxRows && iterations(a, nparts, rows) < 8 && (total + rows - 1) / rows > ctas) rows *= 2;
   return rows;
 }
 
