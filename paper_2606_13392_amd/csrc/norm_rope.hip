@@ -15,7 +15,7 @@
 // Everything between the bf16 input and the one rounding of the output is fp32.
 //
 // Large calls are bound by HBM: 39426 rows of 64 + 4 heads of 128 256 us,
-// 5.4 TB/s, the backward of 32768 rows of 64 + 8 heads 346 us, 5.2 TB/s, every byte
+// 5.3 TB/s, the backward of 32768 rows of 64 + 8 heads 346 us, 5.2 TB/s, every byte
 // once.
 // Small ones by a chain of latencies (launch, rows, angles, elements): 64 rows
 // 4.3 us.
