@@ -319,7 +319,8 @@ int msa_dense_attn(const void* q, const void* k, const void* v, const msa_seqs* 
  * the lengths on the device: a result is bit-reproducible for equal inputs.
  *
  * Supported: head_dim == 128; 1 <= num_q_heads / num_kv_heads <= 16;
- * num_kv_heads <= 64; total_kv_rows < 2^31; q, k, v and o 16-byte aligned.
+ * num_kv_heads <= 64; total_kv_rows < 2^31; q, k, v, o and the workspace 16-byte
+ * aligned (else MSA_ERR_UNSUPPORTED).
  * ------------------------------------------------------------------------ */
 size_t msa_dense_attn_paged_workspace_size(const msa_seqs* seqs, int num_q_heads, int num_kv_heads,
                                            int head_dim);
@@ -410,7 +411,8 @@ int msa_qk_norm_rope_fp8(const void* q, int64_t q_stride, const void* k, int64_t
  *
  * fp32 in between.  Every output is bit-reproducible: the weight gradients add
  * rows in an order that the sizes fix.  Rows behind the last sequence are left
- * as they are and take no part.  The workspace is needed where a weight is given.
+ * as they are and take no part.  The workspace, 8-byte aligned, is needed where a
+ * weight is given.
  * Supported sizes as for msa_qk_norm_rope.
  * ------------------------------------------------------------------------ */
 size_t msa_qk_norm_rope_backward_workspace_size(const msa_seqs* seqs, int num_q_heads,

@@ -1115,6 +1115,7 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
   Parts parts{};
   if (pl.ctas > 0) {
     if (!workspace || workspace_bytes < part_bytes(ctas, waves)) return MSA_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(workspace) & 15) return MSA_ERR_UNSUPPORTED;
     parts.o = static_cast<float*>(workspace);
     parts.lse = parts.o + 2 * ctas * 32 * waves * kDim;
   }

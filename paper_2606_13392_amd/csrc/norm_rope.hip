@@ -666,6 +666,7 @@ extern "C" int msa_qk_norm_rope_backward(const void* q, int64_t q_stride, const 
     }
   const size_t need = norms ? msa_qk_norm_rope_backward_workspace_size(seqs, num_q_heads, num_kv_heads, head_dim) : 0;
   if (norms && (!workspace || workspace_bytes < need)) return MSA_ERR_WORKSPACE;
+  if (norms && !aligned8(workspace)) return MSA_ERR_UNSUPPORTED;
   if (!norms) {                          // the transposed rotation alone
     if (seqs->total_q_rows == 0) return MSA_OK;
     int n = 0;

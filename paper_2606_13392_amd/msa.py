@@ -223,6 +223,11 @@ def _workspace(nbytes: int, device, ws: Optional[torch.Tensor]) -> Optional[torc
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+def _need_workspace(ws: Optional[torch.Tensor], device) -> None:
+    if ws is not None and (ws.device != device or not ws.is_contiguous()):
+        raise ValueError(f"workspace: expected a contiguous tensor on {device}")
+
+
 # ---------------------------------------------------------------- Index Branch
 def index_topk_workspace_size(seqs: Seqs, num_kv_heads: int, d_idx: int, block_size: int, topk: int) -> int:
     return int(lib().msa_index_topk_workspace_size(seqs.ref(), num_kv_heads, d_idx, block_size, topk))
@@ -421,6 +426,7 @@ def _dense_paged(dtype, q, k, v, scales, seqs: Seqs, softmax_scale, out, lse, wo
     _need(q, "q", dtype, (seqs.total_q_rows, H_q, d_h), dev)
     _need(k, "k", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
     _need(v, "v", dtype, (seqs.total_kv_rows, H_kv, d_h), dev)
+    _need_workspace(workspace, dev)
     if not _current(dev):
         with torch.cuda.device(dev):
             return _dense_paged(dtype, q, k, v, scales, seqs, softmax_scale, out, lse, workspace)
@@ -638,6 +644,7 @@ def qk_norm_rope_backward(q, k, d_q_out, d_k_out, seqs: Seqs, rope: Optional[Rop
     dim = (d_k_out if d_q_out is None else d_q_out).shape[2]
     if d_k_out is not None and d_k_out.shape[2] != dim:
         raise ValueError(f"d_k_out: expected head size {dim}, got {d_k_out.shape[2]}")
+    _need_workspace(workspace, dev)
     if not _current(dev):
         with torch.cuda.device(dev):
             return qk_norm_rope_backward(q, k, d_q_out, d_k_out, seqs, rope, q_weight, k_weight, eps, d_q, d_k, d_q_weight,

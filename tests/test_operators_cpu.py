@@ -219,6 +219,20 @@ def test_binding_checks_shapes_and_types():
         msa.dense_attn_paged(q, k[:3], k[:3], s)
 
 
+def test_workspace_is_aligned_and_on_the_device():
+    L = msa.lib()
+    long = _paged(num_seqs=4, total_q_rows=4, max_q_rows=1, max_kv_len=65536, block_table_stride=1024, total_kv_rows=1 << 20)
+    assert L.msa_dense_attn_paged(16, 16, 16, ctypes.byref(long), 64, 8, 128, 0.1, 16, 16, 24, 1 << 40, None) == UNS
+    assert L.msa_qk_norm_rope_backward(8, 1024, 8, 256, 8, 8, ctypes.byref(_seqs()), 8, 2, 128, 8, 8, 0.0,
+                                       ctypes.byref(_rope()), 8, 1024, 8, 256, 8, 8, 12, 1 << 30, None) == UNS
+    s, q = _cpu_seqs(), torch.zeros((4, 2, 128), dtype=torch.bfloat16)
+    for ws in (torch.empty(1 << 20, dtype=torch.uint8, device="meta"), torch.zeros((4, 1 << 10), dtype=torch.uint8)[:, ::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            msa.dense_attn_paged(q, q, q, s, workspace=ws)
+        with pytest.raises(ValueError, match="workspace"):
+            msa.qk_norm_rope_backward(q, None, q, None, s, None, torch.ones(128), workspace=ws)
+
+
 def test_rope_frequencies():
     f, m = msa.rope_frequencies(64, 10000.0)
     assert f.dtype == torch.float64 and m == 1.0
