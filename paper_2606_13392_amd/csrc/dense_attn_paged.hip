@@ -543,8 +543,9 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
         constexpr bool masked = decltype(masked_t)::value;
         __builtin_amdgcn_s_waitcnt(0);        // this thread's copies of K_{b+1} and V_b have landed
         __syncthreads();                      // everyone's have, and block b-1's readers are done
-        // the next copies go out between the S^T slots: in front of them (some sixty
-        // scalar and address instructions) they held up all eight waves (1977 us)
+        // the next copies go out between the last S^T slots: in front of them (some
+        // sixty scalar and address instructions) they held up all eight waves (1977
+        // us); after slots 6 and 10 1830, 12 and 14 1815 (E4M3: 325, 322)
         auto move_k = [&]() __attribute__((always_inline)) {
           if constexpr (kCodes) {
             if (b + 2 < b_end) put(rk, false, ring.k[b & 1]);
@@ -572,8 +573,8 @@ __global__ __launch_bounds__(WAVES* kWave, WAVES >= 4 ? 2 : 1) void paged_attn_k
         __builtin_amdgcn_sched_barrier(0);
         f32x16 acc_s[MT];
         scores(ring.k[(b + 1) & 1], acc_s, [&](int j) __attribute__((always_inline)) {
-          if (j == 6) move_k();
-          if (j == 10) move_v();
+          if (j == 12) move_k();
+          if (j == 14) move_v();
         });
         Soft z;
         pv(ring.v[b & 1], [&](int j) __attribute__((always_inline)) {
