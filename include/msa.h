@@ -367,8 +367,8 @@ typedef struct msa_rope {
  *          heads of head_dim, e.g. columns of a joint projection's output
  *   k      bf16 rows [total_q_rows], k_stride apart, num_kv_heads heads
  *   q_weight, k_weight   fp32 [head_dim], or NULL
- *   q_out  bf16 (fp8: E4M3 codes of y / q_scale, to nearest even, at most 448 in
- *          size) [total_q_rows, num_q_heads, head_dim] contiguous   OUTPUT
+ *   q_out  bf16 (fp8: E4M3 codes of the fp32 quotient y / q_scale, to nearest even,
+ *          at most 448 in size) [total_q_rows, num_q_heads, head_dim] contiguous   OUTPUT
  *   k_out  the same with num_kv_heads, k_scale                      OUTPUT
  *
  * Either tensor is left out with 0 heads.  fp32 in between, one rounding.  The
@@ -443,8 +443,8 @@ int msa_qk_norm_rope_backward(const void* q, int64_t q_stride, const void* k, in
  *              with index_k_cache: no index keys (d_idx, its stride, weight and
  *              rope are then ignored)
  *   k_weight, index_k_weight, eps, rope, index_rope   as in msa_qk_norm_rope
- *   k_cache, v_cache   bf16 (fp8: E4M3 codes of y / k_scale and v / v_scale, to
- *              nearest even, at most 448 in size)
+ *   k_cache, v_cache   bf16 (fp8: E4M3 codes of the fp32 quotients y / k_scale and
+ *              v / v_scale, to nearest even, at most 448 in size)
  *              [total_kv_rows, num_kv_heads, head_dim]   UPDATED
  *   index_k_cache      bf16 [total_kv_rows, d_idx]        UPDATED
  *
