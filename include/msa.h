@@ -407,7 +407,7 @@ int msa_qk_norm_rope_fp8(const void* q, int64_t q_stride, const void* k, int64_t
  *   d_q, d_k   bf16 rows d_q_stride / d_k_stride elements apart   OUTPUT (each may
  *              be the contiguous gradient it is formed from)
  *   d_q_weight, d_k_weight   fp32 [head_dim]   OUTPUT, or NULL to skip; written,
- *              not added to
+ *              not added to (zeros for a tensor with 0 heads, or without rows)
  *
  * fp32 in between.  Every output is bit-reproducible: the weight gradients add
  * rows in an order that the sizes fix.  Rows behind the last sequence are left

@@ -437,16 +437,17 @@ __global__ __launch_bounds__(kThreads) void norm_rope_backward_kernel(Parts a, m
   }
 }
 
-// d w = sum of the CTAs' partials: a CTA takes 16 elements, 64 threads each,
-// which are added in a fixed order.  (16 threads per element, whose 64 reads
-// waited for one another, took 20 us.)
+// d w = sum of the CTAs' partials (a tensor without heads has none): a CTA takes
+// 16 elements, 64 threads each, which are added in a fixed order.  (16 threads per
+// element, whose 64 reads waited for one another, took 20 us.)
 constexpr int kGradThreads = 1024;
-__global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(const float* __restrict__ dw_part, int ctas, int D,
-                                                                 float* dq_w, float* dk_w) {
+__global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(const float* __restrict__ dw_part, int q_ctas,
+                                                                 int k_ctas, int D, float* dq_w, float* dk_w) {
   constexpr int kRows = kGradThreads / 16, kBatch = 4;
   __shared__ float red[kRows][17];
   const int i = blockIdx.y;
   float* out = i ? dk_w : dq_w;
+  const int ctas = i ? k_ctas : q_ctas;
   if (!out) return;                      // uniform over the CTA
   const int e = threadIdx.x & 15, j = threadIdx.x >> 4;
   const int col = blockIdx.x * 16 + e;
@@ -696,30 +697,31 @@ extern "C" int msa_qk_norm_rope_backward(const void* q, int64_t q_stride, const 
   const size_t need = norms ? msa_qk_norm_rope_backward_workspace_size(seqs, num_q_heads, num_kv_heads, head_dim) : 0;
   if (norms && (!workspace || workspace_bytes < need)) return MSA_ERR_WORKSPACE;
   if (norms && !aligned8(workspace)) return MSA_ERR_UNSUPPORTED;
-  if (!norms) {                          // the transposed rotation alone
-    if (seqs->total_q_rows == 0) return MSA_OK;
+  int64_t ctas = 0;
+  auto* part = static_cast<float*>(workspace);
+  if (norms) {
+    for (int i = 0; i < 2; ++i) {
+      a.part[i] = part_of(in[i].x, in[i].stride, in[i].heads, head_dim, in[i].w, in[i].d, in[i].d_stride, spec);
+      a.part[i].g = static_cast<const uint16_t*>(in[i].g);
+    }
+    a.rows = rows_per_cta(a, 2, seqs->total_q_rows, kGradCtas);
+    ctas = grad_ctas(seqs, a);
+    if (ctas > 0)
+      msa_prof::launch("norm_rope_backward_kernel", norm_rope_backward_kernel, dim3(static_cast<unsigned>(ctas)),
+                       dim3(kThreads), angle_bytes(a), stream, a, *seqs, part);
+  } else if (seqs->total_q_rows > 0) {   // the transposed rotation alone
     int n = 0;
     for (const In& t : in)
       if (t.heads > 0)
         a.part[n++] = part_of(t.g, static_cast<int64_t>(t.heads) * head_dim, t.heads, head_dim, nullptr, t.d, t.d_stride, spec);
-    return n == 2 ? launch_forward<2, false>("norm_rope_kernel", a, seqs, stream)
-                  : launch_forward<1, false>("norm_rope_kernel", a, seqs, stream);
+    st = n == 2 ? launch_forward<2, false>("norm_rope_kernel", a, seqs, stream)
+                : launch_forward<1, false>("norm_rope_kernel", a, seqs, stream);
+    if (st != MSA_OK) return st;
   }
-  for (int i = 0; i < 2; ++i) {
-    a.part[i] = part_of(in[i].x, in[i].stride, in[i].heads, head_dim, in[i].w, in[i].d, in[i].d_stride, spec);
-    a.part[i].g = static_cast<const uint16_t*>(in[i].g);
-  }
-  a.rows = rows_per_cta(a, 2, seqs->total_q_rows, kGradCtas);
-  const int64_t ctas = grad_ctas(seqs, a);
-  auto* part = static_cast<float*>(workspace);
-  if (ctas > 0)
-    msa_prof::launch("norm_rope_backward_kernel", norm_rope_backward_kernel, dim3(static_cast<unsigned>(ctas)), dim3(kThreads),
-                     angle_bytes(a), stream, a, *seqs, part);
-  float* dqw = num_q_heads > 0 ? d_q_weight : nullptr;
-  float* dkw = num_kv_heads > 0 ? d_k_weight : nullptr;
-  if (dqw || dkw)
+  if (d_q_weight || d_k_weight)
     msa_prof::launch("norm_grad_kernel", norm_grad_kernel, dim3(head_dim / 16, 2), dim3(kGradThreads), 0, stream,
-                     static_cast<const float*>(part), static_cast<int>(ctas), head_dim, dqw, dkw);
+                     static_cast<const float*>(part), static_cast<int>(num_q_heads > 0 ? ctas : 0),
+                     static_cast<int>(num_kv_heads > 0 ? ctas : 0), head_dim, d_q_weight, d_k_weight);
   return msa_host::launch_status();
 }
 
