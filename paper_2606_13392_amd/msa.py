@@ -604,6 +604,8 @@ def _grad_side(name, seqs: Seqs, x, g, w, d, dw):
     """(input, its row stride, heads, gradient, its row stride, weight, its gradient) of q or k; no heads where the
     tensor's upstream gradient is None."""
     if g is None:
+        if d is not None or dw is not None:
+            raise ValueError(f"d_{name} or d_{name}_weight: given without d_{name}_out")
         return None, 0, 0, None, 0, None, None
     T, dev = seqs.total_q_rows, seqs.device
     h, dim, stride = _heads(g, f"d_{name}_out", T, dev)
@@ -633,9 +635,9 @@ def _grad_side(name, seqs: Seqs, x, g, w, d, dw):
 
 def qk_norm_rope_backward(q, k, d_q_out, d_k_out, seqs: Seqs, rope: Optional[Rope], q_weight=None, k_weight=None,
                           eps: float = 1e-6, d_q=None, d_k=None, d_q_weight=None, d_k_weight=None, workspace=None):
-    """Gradients of qk_norm_rope: (d_q, d_k, d_q_weight, d_k_weight); a weight's is None where it is None.  ``q`` and
-    ``k`` are the forward's inputs (not read, and may be None, without weight); d_q and d_k may be columns of a wider
-    tensor."""
+    """Gradients of qk_norm_rope: (d_q, d_k, d_q_weight, d_k_weight); a weight's is None where it is None, both of a
+    tensor's where its upstream gradient is.  ``q`` and ``k`` are the forward's inputs (not read, and may be None,
+    without weight); d_q and d_k may be columns of a wider tensor."""
     if d_q_out is None and d_k_out is None:
         raise ValueError("d_q_out or d_k_out is needed")
     dev = seqs.device
