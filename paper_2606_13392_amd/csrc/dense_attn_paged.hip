@@ -1107,7 +1107,9 @@ int paged_attn(const void* q, const void* k, const void* v, bool fp8, float q_sc
   if (!q || !k || !v || !o || !lse) return MSA_ERR_INVALID;
   for (const void* x : {q, k, v, static_cast<const void*>(o)})
     if (reinterpret_cast<uintptr_t>(x) & 15) return MSA_ERR_UNSUPPORTED;   // 16-byte pieces
-  const flash::LogitScale scale = flash::logit_scale(softmax_scale * q_scale * k_scale * kLog2E);
+  // in 64 bits: scales of the codes far from 1 may cancel
+  const flash::LogitScale scale =
+      flash::logit_scale(static_cast<float>(static_cast<double>(softmax_scale) * q_scale * k_scale * kLog2E));
   const int G = H_q / H_kv;
   int waves;
   int64_t ctas;
