@@ -310,8 +310,8 @@ constexpr int kGradCtas = 1024;          // CTAs at most: partial weight gradien
 //   d x = rstd (h w - xh m),  d w = sum over rows and heads of h xh.
 // Each lane sums its 8 elements' d w over the heads it takes; the CTA's lane
 // groups are added in LDS in their order, and the CTAs by norm_grad_kernel.
-__device__ __forceinline__ int run_part_back(const Part& pt, const Spec& sp, int64_t row0, int n, float eps, const int32_t* pos,
-                                             const float* cs, int it, int step, float (&dwa)[4], float (&dwb)[4]) {
+__device__ __forceinline__ void run_part_back(const Part& pt, const Spec& sp, int64_t row0, int n, float eps, const int32_t* pos,
+                                              const float* cs, float (&dwa)[4], float (&dwb)[4]) {
   const int group = threadIdx.x >> pt.lg_lanes, groups = kThreads >> pt.lg_lanes;
   const int total = n * pt.heads;
   const int iters = (total + groups - 1) / groups;
@@ -347,10 +347,10 @@ __device__ __forceinline__ int run_part_back(const Part& pt, const Spec& sp, int
     }
   };
   Raw4 next{};
-  if (it < iters) load(it, next);
-  for (; it < iters; it += step) {
+  if (iters > 0) load(0, next);
+  for (int it = 0; it < iters; ++it) {
     const Raw4 cur = next;
-    if (it + step < iters) load(it + step, next);
+    if (it + 1 < iters) load(it + 1, next);
     int r, h;
     at(it, &r, &h);
     const bool keep = it * groups + group < total && pos[r] != INT32_MIN;
@@ -391,7 +391,6 @@ __device__ __forceinline__ int run_part_back(const Part& pt, const Spec& sp, int
       *reinterpret_cast<uint2*>(y + d.b) = pack4(v);
     }
   }
-  return it - iters;
 }
 
 __global__ __launch_bounds__(kThreads) void norm_rope_backward_kernel(Parts a, msa_seqs sq, float* dw_part) {
@@ -408,12 +407,9 @@ __global__ __launch_bounds__(kThreads) void norm_rope_backward_kernel(Parts a, m
     __syncthreads();
     fill_angles(a.spec[0], pos, n, cs);
     __syncthreads();
-    int it = 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (a.part[i].heads > 0) {
-        run_part_back(a.part[i], a.spec[0], row0, n, a.eps, pos, cs, it, 1, dw[i][0], dw[i][1]);
-      }
+      if (a.part[i].heads > 0) run_part_back(a.part[i], a.spec[0], row0, n, a.eps, pos, cs, dw[i][0], dw[i][1]);
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
