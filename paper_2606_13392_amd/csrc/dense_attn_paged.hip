@@ -33,8 +33,9 @@
 // sequences of 5 - 34 keys (bf16: 1e-6).
 //
 // Tiles are bound by MFMA issue with the softmax between (64 heads on 8: 2 x 2048
-// rows on 16K keys 1.84 ms, 1.10 PFLOP/s), the few-row kernel by HBM reads (32
-// tokens on 4K - 60K keys 415 us, 5.7 TB/s; 64 on 32K 1.40 ms, 6.1 TB/s).
+// rows on 16K keys 1.78 - 1.92 ms by the card, 1.06 - 1.14 PFLOP/s), the few-row
+// kernel by HBM reads (32 tokens on 4K - 60K keys 415 us, 5.7 TB/s; 64 on 32K
+// 1.40 ms, 6.1 TB/s).
 #include <initializer_list>
 
 #include "flash_tile.h"
@@ -58,7 +59,11 @@ using flash::xor32f;
 // wait for the copies just issued before the first read of the sub-block that
 // has landed (2 x 2048 rows on 16K keys 2035 us instead of 1977); every step
 // waits for them itself before its barrier.  M0 holds the LDS address, one wait
-// state ahead of the copy.
+// state ahead of the copy.  It is a reserved register, which the compiler notes at
+// every clobber: nothing else in these kernels uses it (LDS accesses do not need it,
+// and no register is indexed by a variable).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<size_t>((__attribute__((address_space(3))) const void*)(p)));
 }
@@ -69,6 +74,7 @@ __device__ __forceinline__ void copy16(const char* base, uint32_t offset, uint32
 __device__ __forceinline__ void copy16(const char* src, uint32_t lds) {                      // src each lane its own
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(src), "s"(lds) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 // Places of a sequence's key rows in the pool, in units of min(page, 64) rows:
 // a window of 64 units, one per lane, and the one behind it.  SMALL: pages of
@@ -1070,6 +1076,12 @@ int validate_paged(const msa_seqs* seqs, int H_q, int H_kv, int head_dim) {
 // 97.4 (all of them equally long; of 4K - 60K 421 against what the longest takes,
 // over 600); 512 rows on 1024 keys 37.1 / 35.1, 2048 52.7 / 59.7; 64 rows 512 22.1
 // / 21.5, 1024 24.9 / 33.8.
+// The steps counted are those of a tile that sees all of its sequence's keys, which
+// holds for rows far behind a long context.  A prompt's early tiles see few: split,
+// their CTAs end early and the others have full shares (3800 rows without context
+// 382 us, 4200, which are too many tiles to be split, 319).  The same bound keeps
+// decode batches of more than about 100 sequences on 8 groups whole, whatever their
+// lengths (4K - 60K: 96 sequences 5.8 TB/s, 128 4.6).
 constexpr int kFewRowsGain = 11, kTileGain = 9;      // steps that a split has to save
 Plan plan_of(const msa_seqs* seqs, int H_q, int H_kv, int* waves, int64_t* ctas) {
   const int qpw = 32 / (H_q / H_kv);
