@@ -374,8 +374,9 @@ typedef struct msa_rope {
  * Either tensor is left out with 0 heads.  fp32 in between, one rounding.  The
  * bf16 outputs may be the inputs themselves where those are contiguous; other
  * overlaps are not allowed.  Rows behind the last sequence are left as they are.
- * With eps 0 a head of zeros gives NaN; sums of squares beyond fp32 (elements
- * of about 2^60) give 0.  bf16 elements that neither a norm nor the rotation
+ * With eps 0 a head of zeros gives NaN, and one whose mean square is below fp32's
+ * normal range (elements of about 2^-63) is unspecified; sums of squares beyond
+ * fp32 (elements of about 2^60) give 0.  bf16 elements that neither a norm nor the rotation
  * applies to keep their bits.  A scale is from 2^-126 to 2^126 (else
  * MSA_ERR_INVALID).  No workspace.
  *

@@ -83,8 +83,8 @@ __device__ __forceinline__ uint2 pack4(const float (&f)[4]) {
 }
 // E4M3 codes of f / scale, to nearest even; beyond the format's range its largest
 // value (the conversion alone would give NaN), NaN stays.  f * down is exact
-// (or rounds to a code of zero), and the quotient itself where the scale is a
-// power of two.  Else f * down * inv_m alone is off by up to 1.5 steps of fp32,
+// (unless its code is zero or the largest), and the quotient itself where the scale
+// is a power of two.  Else f * down * inv_m alone is off by up to 1.5 steps of fp32,
 // which takes 60 of the 65536 bf16 values across the middle between two codes at
 // a scale of 0.4375; one step with the product's remainder, which fp32 holds, gives
 // the rounded quotient (compared with the division for every bf16 mantissa and
