@@ -25,6 +25,13 @@
  *   msa_kv_append(_fp8)      new keys, values and index keys into the (paged) cache
  *   msa_dense_attn_paged(_fp8)   dense causal attention over a paged cache
  *
+ * and the same for layers whose keys and values come from one latent vector per token:
+ *
+ *   msa_latent_append(_fp8)  latents and shared key parts into the (paged) cache
+ *   msa_latent_attn_paged(_fp8)   attention on that cache (absorbed form)
+ *   msa_latent_attn          attention on per-head keys and values (expanded form)
+ *   msa_latent_attn_backward its gradients
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Every tensor argument is a DEVICE pointer to contiguous row-major memory
@@ -79,7 +86,9 @@
  * is a serving layout, not part of the paper.  Every call accepts it except
  * msa_dense_attn, which returns MSA_ERR_UNSUPPORTED for a paged layout
  * (msa_dense_attn_paged takes it; that call and msa_kv_append, which have no
- * block size, accept any power of two from 16 to 8192 as page_size); the
+ * block size, accept any power of two from 16 to 8192 as page_size; so do
+ * msa_latent_append and msa_latent_attn_paged, while msa_latent_attn and its
+ * backward are for a contiguous key side); the
  * training calls then write dK, dV and d index_k in the pool's rows (rows of
  * pages no sequence lists get zero; keys in pages shared by several
  * sequences get the sum of their gradients).
@@ -467,6 +476,89 @@ int msa_kv_append_fp8(const void* k, int64_t k_stride, const void* v, int64_t v_
                       const float* k_weight, const float* index_k_weight, float eps,
                       const msa_rope* rope, const msa_rope* index_rope, void* k_cache,
                       void* v_cache, void* index_k_cache, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Latent attention
+ *
+ * Token j has one latent vector c_j of latent_dim elements, from which every
+ * head's key and value are products, and one rotated key part r_j of 64 elements
+ * that the heads share.  With a head's query of two parts, n_i (128) and the
+ * rotated e_i (64), its key matrix A and its value matrix B (128 x latent_dim):
+ *     S_ij = softmax_scale (n_i . A c_j + e_i . r_j),   P = softmax over j <= i,
+ *     O_i = sum_j P_ij B c_j.
+ * Expanded form (msa_latent_attn): the products A c_j, B c_j are made for every
+ * token and head before the call.  Absorbed form (msa_latent_attn_paged): the
+ * query is A^T n_i (latent_dim elements), the cache holds c_j and r_j alone, and
+ * the call returns sum_j P_ij c_j, to be multiplied by B.  Both give the same O
+ * and LSE; the products are the caller's.  softmax_scale is that of the expanded
+ * head (1 / sqrt(128 + 64), say) in both.
+ * ------------------------------------------------------------------------ */
+
+/* ------------------------------------------------------------------------
+ * msa_latent_append / msa_latent_append_fp8 -- the new rows' latents and shared
+ * key parts into the cache:
+ *     row = [ c / sqrt(mean(c^2) + eps) * weight,  rotation of k_rope by position ]
+ * Row t of sequence s goes to the cache row of its position, as in msa_kv_append
+ * (contiguous or paged; rows without a place in the cache are not stored).
+ *
+ *   latent     bf16 rows [total_q_rows], latent_stride elements apart, of latent_dim
+ *              elements, e.g. columns of a joint projection's output
+ *   k_rope     bf16 rows, k_rope_stride apart, of 64 elements
+ *   weight     fp32 [latent_dim], or NULL: no norm
+ *   rope       the rotation of k_rope (rot_dim at most 64), or NULL
+ *   cache      bf16 (fp8: E4M3 codes of the fp32 quotients by cache_scale, to nearest
+ *              even, at most 448 in size) [total_kv_rows, latent_dim + 64]   UPDATED
+ *
+ * fp32 in between, one rounding; bf16 elements that neither the norm nor the
+ * rotation applies to keep their bits.  eps, weights and scales as for
+ * msa_qk_norm_rope(_fp8).  No workspace.
+ * Supported: latent_dim 256 or 512; pages of a power of two from 16 to 8192 rows;
+ * strides a multiple of 4 elements, tensors 8-byte aligned (else
+ * MSA_ERR_UNSUPPORTED).
+ * ------------------------------------------------------------------------ */
+int msa_latent_append(const void* latent, int64_t latent_stride, const void* k_rope, int64_t k_rope_stride,
+                      const msa_seqs* seqs, int latent_dim, const float* weight, float eps, const msa_rope* rope,
+                      void* cache, hipStream_t stream);
+int msa_latent_append_fp8(const void* latent, int64_t latent_stride, const void* k_rope, int64_t k_rope_stride,
+                          float cache_scale, const msa_seqs* seqs, int latent_dim, const float* weight, float eps,
+                          const msa_rope* rope, void* cache, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * msa_latent_attn_paged / msa_latent_attn_paged_fp8 -- latent attention, absorbed
+ * form, of each sequence's new rows over its paged cache; one token per sequence,
+ * draft rows and chunks, mixed in a batch.
+ *
+ *   q          bf16 [total_q_rows, num_heads, latent_dim], rows q_stride and heads
+ *              q_head_stride elements apart (a product made head by head is
+ *              [num_heads, total_q_rows, latent_dim]: strides latent_dim and
+ *              total_q_rows * latent_dim)
+ *   q_rope     bf16 [total_q_rows, num_heads, 64], with strides of its own
+ *   cache      bf16 (fp8: E4M3 codes of value / cache_scale) [total_kv_rows, latent_dim + 64]
+ *   o          bf16 [total_q_rows, num_heads, latent_dim]   OUTPUT: sum_j P_ij c_j
+ *   lse        fp32 [total_q_rows, num_heads]               OUTPUT, natural log
+ *
+ * A row without a visible key gets O = 0 and LSE = -inf; rows of o and lse behind
+ * the last sequence are left as they are.  What the cache holds behind a
+ * sequence's last key does not matter, NaN included; a NaN or infinity among a
+ * sequence's own new keys may reach rows before it.  The weights P are rounded to
+ * bf16 for the second product, their sums are of the unrounded ones.  Results are
+ * bit-reproducible for equal inputs.  cache_scale is finite and positive (else
+ * MSA_ERR_INVALID).  A contiguous key side returns MSA_ERR_UNSUPPORTED.
+ *
+ * Supported: latent_dim 256 or 512; num_heads <= 1024; pages of a power of two from
+ * 16 to 8192 rows; total_kv_rows < 2^31; strides a multiple of 8 elements; q, q_rope,
+ * cache, o and the workspace 16-byte aligned (else MSA_ERR_UNSUPPORTED).
+ * ------------------------------------------------------------------------ */
+size_t msa_latent_attn_paged_workspace_size(const msa_seqs* seqs, int num_heads, int latent_dim);
+int msa_latent_attn_paged(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope,
+                          int64_t q_rope_stride, int64_t q_rope_head_stride, const void* cache,
+                          const msa_seqs* seqs, int num_heads, int latent_dim, float softmax_scale, void* o,
+                          float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+int msa_latent_attn_paged_fp8(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope,
+                              int64_t q_rope_stride, int64_t q_rope_head_stride, const void* cache,
+                              float cache_scale, const msa_seqs* seqs, int num_heads, int latent_dim,
+                              float softmax_scale, void* o, float* lse, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * msa_sparse_attn_backward -- training backward of the Main Branch.

@@ -548,3 +548,68 @@ def norm_rope_backward(x: np.ndarray, g: np.ndarray, positions: Sequence[int], w
     u = x / rms
     hw = h * weight
     return (hw - u * (hw * u).mean(-1, keepdims=True)) / rms, (h * u).sum((0, 1))
+
+
+# --------------------------------------------------------------------------
+# Latent attention: scores of two parts, keys and values per head or shared
+# --------------------------------------------------------------------------
+def _latent_weights(q, q_rope, k, k_rope, lo, pos, scale):
+    """Scores and log-sum-exp of one row's heads over key rows lo .. lo + pos."""
+    k = k[lo:lo + pos + 1]
+    if k.shape[1] == 1:                                     # one key for all heads
+        z = q @ k[:, 0].T
+    else:
+        z = np.einsum("hd,jhd->hj", q, k)
+    z = scale * (z + q_rope @ k_rope[lo:lo + pos + 1].T)
+    m = z.max(-1, keepdims=True)
+    return z, (m + np.log(np.exp(z - m).sum(-1, keepdims=True)))[:, 0]
+
+
+def latent_attention(q, q_rope, k, k_rope, v, layout: Layout, scale: float, rows: Optional[Iterable[int]] = None):
+    """Causal attention with S = scale (q . k + q_rope . k_rope) (float64).  q [T, H, d], q_rope [T, H, r]; k [N, H or 1,
+    d], v [N, H or 1, dv], k_rope [N, r].  Returns O [rows, H, dv], LSE [rows, H] and sum_j P |v|, the size
+    that O's errors go by; a row without a visible key has zeros and -inf."""
+    rows = list(range(layout.total_q_rows)) if rows is None else [int(r) for r in rows]
+    H = q.shape[1]
+    o = np.zeros((len(rows), H, v.shape[2]))
+    size = np.zeros_like(o)
+    lse = np.full((len(rows), H), -np.inf)
+    for i, r in enumerate(rows):
+        s, pos = layout.locate(r)
+        if pos < 0:
+            continue
+        lo = layout.kv_starts[s]
+        z, lse[i] = _latent_weights(q[r], q_rope[r], k, k_rope, lo, pos, scale)
+        p = np.exp(z - lse[i][:, None])
+        vals = v[lo:lo + pos + 1]
+        if vals.shape[1] == 1:
+            o[i], size[i] = p @ vals[:, 0], p @ np.abs(vals[:, 0])
+        else:
+            o[i], size[i] = np.einsum("hj,jhd->hd", p, vals), np.einsum("hj,jhd->hd", p, np.abs(vals))
+    return o, lse, size
+
+
+def latent_attention_backward(q, q_rope, k, k_rope, v, o, lse, d_o, layout: Layout, scale: float):
+    """Gradients of sum(d_o O) at the given O and LSE: (d_q, d_q_rope, d_k, d_k_rope, d_v), float64; and for each the sum of
+    the sizes of its terms, which errors go by: a term's factor is P (|dO . v| + |dO| . |o|), not their difference."""
+    T, H = q.shape[:2]
+    grads = [np.zeros_like(np.asarray(x, dtype=np.float64)) for x in (q, q_rope, k, k_rope, v)]
+    sizes = [np.zeros_like(x) for x in grads]
+    for r in range(T):
+        s, pos = layout.locate(r)
+        if pos < 0:
+            continue
+        K = slice(layout.kv_starts[s], layout.kv_starts[s] + pos + 1)
+        for h in range(H):
+            z = scale * (k[K, h] @ q[r, h] + k_rope[K] @ q_rope[r, h])
+            p = np.exp(z - lse[r, h])
+            dp = v[K, h] @ d_o[r, h]
+            dz = scale * p * (dp - d_o[r, h] @ o[r, h])
+            az = abs(scale) * p * (np.abs(v[K, h]) @ np.abs(d_o[r, h]) + np.abs(d_o[r, h]) @ np.abs(o[r, h]))
+            for out, w, f in ((grads, dz, lambda x: x), (sizes, az, np.abs)):
+                out[0][r, h] = w @ f(k[K, h])
+                out[1][r, h] = w @ f(k_rope[K])
+                out[2][K, h] += np.outer(w, f(q[r, h]))
+                out[3][K] += np.outer(w, f(q_rope[r, h]))
+                out[4][K, h] += np.outer(p, f(d_o[r, h]))
+    return grads, sizes

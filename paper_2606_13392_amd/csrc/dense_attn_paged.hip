@@ -43,38 +43,18 @@
 namespace {
 
 using namespace msa;
+using flash::copy16;
 using flash::kAhead;
 using flash::kDim;
 using flash::kLn_2;
 using flash::kLog2E;
 using flash::kSub;
 using flash::k_seg;
+using flash::lds_address;
 using flash::lds_tr4;
 using flash::Ring;
 using flash::v_seg;
 using flash::xor32f;
-
-// global_load_lds: lane l's 16 bytes land at dst + 16 l (dst wave-uniform).  From
-// inline assembly: the compiler cannot tell the ring's buffers apart and would
-// wait for the copies just issued before the first read of the sub-block that
-// has landed (2 x 2048 rows on 16K keys 2035 us instead of 1977); every step
-// waits for them itself before its barrier.  M0 holds the LDS address, one wait
-// state ahead of the copy.  It is a reserved register, which the compiler notes at
-// every clobber: nothing else in these kernels uses it (LDS accesses do not need it,
-// and no register is indexed by a variable).
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-  return static_cast<uint32_t>(reinterpret_cast<size_t>((__attribute__((address_space(3))) const void*)(p)));
-}
-__device__ __forceinline__ void copy16(const char* base, uint32_t offset, uint32_t lds) {   // base, lds wave-uniform
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-               :: "v"(offset), "s"(base), "s"(lds) : "m0", "memory");
-}
-__device__ __forceinline__ void copy16(const char* src, uint32_t lds) {                      // src each lane its own
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(src), "s"(lds) : "m0", "memory");
-}
-#pragma clang diagnostic pop
 
 // Places of a sequence's key rows in the pool, in units of min(page, 64) rows:
 // a window of 64 units, one per lane, and the one behind it.  SMALL: pages of

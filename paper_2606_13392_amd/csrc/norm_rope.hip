@@ -469,6 +469,103 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(const float* __
   if (j == 0) out[col] = red[0][e];
 }
 
+// ---------------------------------------------------------------- latent cache rows
+// A row of the latent cache: the norm of the token's latent (R elements, a wave
+// with R / 64 each) and its shared key part, rotated (64 elements, one pair for
+// each of 32 lanes).  A wave takes every fourth of the CTA's rows; their elements
+// are requested before the rows are located.
+template <int R>
+__global__ __launch_bounds__(kThreads) void latent_append_kernel(const uint16_t* __restrict__ latent, int64_t latent_stride,
+                                                                 const uint16_t* __restrict__ k_rope, int64_t k_rope_stride,
+                                                                 const float* __restrict__ weight, float eps, Spec sp, Code code,
+                                                                 msa_seqs sq, int rows, void* __restrict__ cache) {
+  constexpr int kRot = 64, N = R / kWave;
+  __shared__ int32_t pos[kMaxRows];
+  __shared__ int64_t dst[kMaxRows];
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows;
+  const int n = static_cast<int>(min(static_cast<int64_t>(rows), sq.total_q_rows - row0));
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  // the lane's pair (lanes below 32): rotated ones first, then the rest of the part
+  const int i = lane & 31;
+  const bool turned = i < sp.pairs;
+  const int a = !turned ? 2 * i : sp.inter ? 2 * i : i;
+  const int b = !turned || sp.inter ? a + 1 : sp.pairs + i;
+  uint2 x[2];                            // 8 or 4 elements
+  uint32_t ka = 0, kb = 0;
+  auto load = [&](int r) {
+    const uint16_t* src = latent + (row0 + r) * latent_stride + N * lane;
+    x[0] = *reinterpret_cast<const uint2*>(src);
+    if constexpr (N == 8) x[1] = *reinterpret_cast<const uint2*>(src + 4);
+    const uint16_t* kr = k_rope + (row0 + r) * k_rope_stride;
+    ka = kr[a];
+    kb = kr[b];
+  };
+  int r = wave;
+  if (r < n) load(r);
+  if (threadIdx.x < kWave) locate_rows(sq, row0, n, pos, dst);
+  float w[N];
+#pragma unroll
+  for (int c = 0; c < N; ++c) w[c] = weight ? weight[N * lane + c] : 1.f;
+  const double freq = turned ? sp.freq[i] : 0.0;
+  __syncthreads();
+  for (; r < n; r += kThreads / kWave) {
+    const int64_t to = dst[r];
+    if (to >= 0) {                       // the same in every lane
+      float u[4], v[4] = {}, ra = __uint_as_float(ka << 16), rb = __uint_as_float(kb << 16);
+      unpack4(x[0], u);
+      if constexpr (N == 8) unpack4(x[1], v);
+      if (weight) {
+        float ss = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ss = fmaf(u[c], u[c], fmaf(v[c], v[c], ss));
+        ss = head_sum(ss, 4);
+        ss += __uint_as_float(xor_lane_u32<16>(__float_as_uint(ss)));
+        ss += __uint_as_float(xor_lane_u32<32>(__float_as_uint(ss)));
+        const float rstd = rsqrtf(ss * (1.f / R) + eps);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          u[c] = u[c] * rstd * w[c];
+          if constexpr (N == 8) v[c] = v[c] * rstd * w[4 + c];
+        }
+      }
+      if (turned) {
+        double turns = static_cast<double>(pos[r]) * freq * 0.15915494309189533577;   // 1 / (2 pi)
+        turns -= rint(turns);
+        float s, c;
+        sincospif(2.f * static_cast<float>(turns), &s, &c);
+        c *= sp.scale;
+        s *= sp.scale;
+        const float y = fmaf(ra, c, -(rb * s));
+        rb = fmaf(rb, c, ra * s);
+        ra = y;
+      }
+      const int64_t at = to * (R + kRot);
+      if (code.on) {
+        uint8_t* y = static_cast<uint8_t*>(cache) + at;
+        *reinterpret_cast<uint32_t*>(y + N * lane) = code4(u, code);
+        if constexpr (N == 8) *reinterpret_cast<uint32_t*>(y + N * lane + 4) = code4(v, code);
+        const float pair[4] = {ra, rb, 0.f, 0.f};
+        const uint32_t cd = code4(pair, code);
+        if (lane < 32) {
+          y[R + a] = static_cast<uint8_t>(cd);
+          y[R + b] = static_cast<uint8_t>(cd >> 8);
+        }
+      } else {
+        // elements that nothing is applied to keep their bits (NaN payloads too)
+        uint16_t* y = static_cast<uint16_t*>(cache) + at;
+        *reinterpret_cast<uint2*>(y + N * lane) = weight ? pack4(u) : x[0];
+        if constexpr (N == 8) *reinterpret_cast<uint2*>(y + N * lane + 4) = weight ? pack4(v) : x[1];
+        const uint32_t pr = turned ? pack_bf16x2(ra, rb) : (ka | (kb << 16));
+        if (lane < 32) {
+          y[R + a] = static_cast<uint16_t>(pr);
+          y[R + b] = static_cast<uint16_t>(pr >> 16);
+        }
+      }
+    }
+    if (r + kThreads / kWave < n) load(r + kThreads / kWave);
+  }
+}
+
 // ---------------------------------------------------------------- host side
 int validate_rope(const msa_rope* r, int dim) {
   if (!r || r->rot_dim == 0) return MSA_OK;
@@ -630,6 +727,37 @@ int kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, 
   return launch_forward<3, true>("kv_append_kernel", a, seqs, stream);
 }
 
+// Rows per CTA: four, one per wave, while there are more than 2048 CTAs (all that
+// run at once), else one, so that few rows spread over the chip.
+int latent_append(const void* latent, int64_t latent_stride, const void* k_rope, int64_t k_rope_stride, bool fp8, float scale,
+                  const msa_seqs* seqs, int R, const float* weight, float eps, const msa_rope* rope, void* cache,
+                  hipStream_t stream) {
+  int st = msa_host::validate_seqs(seqs);
+  if (st != MSA_OK) return st;
+  if (R < 1 || !(eps >= 0.f && eps < 3.0e38f)) return MSA_ERR_INVALID;
+  if (R != 256 && R != 512) return MSA_ERR_UNSUPPORTED;
+  if ((st = validate_rope(rope, 64)) != MSA_OK) return st;
+  if (fp8 && !scale_ok(scale)) return MSA_ERR_INVALID;
+  if (seqs->block_table && !(msa_host::is_pow2(seqs->page_size) && seqs->page_size >= 16 && seqs->page_size <= 8192))
+    return MSA_ERR_INVALID;
+  if (seqs->total_q_rows == 0) return MSA_OK;
+  if ((st = check_rows(latent, latent_stride, 1, R)) != MSA_OK) return st;
+  if ((st = check_rows(k_rope, k_rope_stride, 1, 64)) != MSA_OK) return st;
+  if (!cache) return MSA_ERR_INVALID;
+  if (!aligned8(cache)) return MSA_ERR_UNSUPPORTED;
+  const int64_t total = seqs->total_q_rows;
+  int rows = 1;
+  while (rows < kMaxRows && (total + rows - 1) / rows > kCtas) rows *= 2;
+  const int64_t ctas = (total + rows - 1) / rows;
+  if (ctas >= (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;          // a grid's limit
+  const Code code = fp8 ? code_of(scale) : Code{};
+  msa_prof::launch("latent_append_kernel", R == 512 ? latent_append_kernel<512> : latent_append_kernel<256>,
+                   dim3(static_cast<unsigned>(ctas)), dim3(kThreads), 0, stream, static_cast<const uint16_t*>(latent),
+                   latent_stride, static_cast<const uint16_t*>(k_rope), k_rope_stride, weight, eps, spec_of(rope), code, *seqs,
+                   rows, cache);
+  return msa_host::launch_status();
+}
+
 int64_t grad_ctas(const msa_seqs* seqs, const Parts& a) {
   return std::min<int64_t>(kGradCtas, (seqs->total_q_rows + a.rows - 1) / a.rows);
 }
@@ -737,4 +865,18 @@ extern "C" int msa_kv_append_fp8(const void* k, int64_t k_stride, const void* v,
                                  void* k_cache, void* v_cache, void* index_k_cache, hipStream_t stream) {
   return kv_append(k, k_stride, v, v_stride, true, k_scale, v_scale, index_k, index_k_stride, seqs, num_kv_heads, head_dim,
                    d_idx, k_weight, index_k_weight, eps, rope, index_rope, k_cache, v_cache, index_k_cache, stream);
+}
+
+extern "C" int msa_latent_append(const void* latent, int64_t latent_stride, const void* k_rope, int64_t k_rope_stride,
+                                 const msa_seqs* seqs, int latent_dim, const float* weight, float eps, const msa_rope* rope,
+                                 void* cache, hipStream_t stream) {
+  return latent_append(latent, latent_stride, k_rope, k_rope_stride, false, 1.f, seqs, latent_dim, weight, eps, rope, cache,
+                       stream);
+}
+
+extern "C" int msa_latent_append_fp8(const void* latent, int64_t latent_stride, const void* k_rope, int64_t k_rope_stride,
+                                     float cache_scale, const msa_seqs* seqs, int latent_dim, const float* weight, float eps,
+                                     const msa_rope* rope, void* cache, hipStream_t stream) {
+  return latent_append(latent, latent_stride, k_rope, k_rope_stride, true, cache_scale, seqs, latent_dim, weight, eps, rope,
+                       cache, stream);
 }

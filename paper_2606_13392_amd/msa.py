@@ -30,6 +30,8 @@ EXPORTS = [
     "msa_qk_norm_rope", "msa_qk_norm_rope_fp8",
     "msa_qk_norm_rope_backward_workspace_size", "msa_qk_norm_rope_backward",
     "msa_kv_append", "msa_kv_append_fp8",
+    "msa_latent_append", "msa_latent_append_fp8",
+    "msa_latent_attn_paged_workspace_size", "msa_latent_attn_paged", "msa_latent_attn_paged_fp8",
     "msa_sparse_attn_backward_workspace_size", "msa_sparse_attn_backward",
     "msa_sparse_kl_backward_workspace_size", "msa_sparse_kl_backward",
     "msa_profile_enable", "msa_profile_reset", "msa_profile_kernel_name", "msa_profile_read",
@@ -116,6 +118,16 @@ def lib() -> ctypes.CDLL:
         L.msa_kv_append.restype = I
         L.msa_kv_append_fp8.argtypes = [P, N, P, N, F, F, P, N, S, I, I, I, P, P, F, R, R, P, P, P, P]
         L.msa_kv_append_fp8.restype = I
+        L.msa_latent_append.argtypes = [P, N, P, N, S, I, P, F, R, P, P]
+        L.msa_latent_append.restype = I
+        L.msa_latent_append_fp8.argtypes = [P, N, P, N, F, S, I, P, F, R, P, P]
+        L.msa_latent_append_fp8.restype = I
+        L.msa_latent_attn_paged_workspace_size.argtypes = [S, I, I]
+        L.msa_latent_attn_paged_workspace_size.restype = Z
+        L.msa_latent_attn_paged.argtypes = [P, N, N, P, N, N, P, S, I, I, F, P, P, P, Z, P]
+        L.msa_latent_attn_paged.restype = I
+        L.msa_latent_attn_paged_fp8.argtypes = [P, N, N, P, N, N, P, F, S, I, I, F, P, P, P, Z, P]
+        L.msa_latent_attn_paged_fp8.restype = I
         L.msa_sparse_attn_backward_workspace_size.argtypes = [S, I, I, I, I, I]
         L.msa_sparse_attn_backward_workspace_size.restype = Z
         L.msa_sparse_attn_backward.argtypes = [P, P, P, P, P, P, P, S, I, I, I, I, I, F, P, P, P, P, Z, P]
@@ -718,6 +730,126 @@ def kv_append_fp8(k, v, scales, seqs: Seqs, rope: Optional[Rope], k_cache, v_cac
     """The same with e4m3 k and v caches (uint8) and per-tensor scales (k, v); index keys stay bf16."""
     _append(scales, k, v, seqs, rope, k_cache, v_cache, k_weight, eps, index_k, index_k_cache, index_k_weight,
             index_rope)
+
+
+# ---------------------------------------------------------------- latent attention
+LATENT_HEAD_DIM = 128             # a head's own key part, and its values (expanded form)
+LATENT_ROPE_DIM = 64              # the key part that the heads share
+
+
+def _latent_scale(softmax_scale) -> float:
+    if softmax_scale is None:
+        return 1.0 / math.sqrt(LATENT_HEAD_DIM + LATENT_ROPE_DIM)
+    return float(softmax_scale)
+
+
+def _strided(t: torch.Tensor, name: str, shape: Sequence[int], device):
+    """(row stride, head stride) of a bf16 [rows, heads, dim] tensor whose rows and heads may lie anywhere."""
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    rows, heads, dim = t.stride()
+    if dim != 1:
+        raise ValueError(f"{name}: a head must be contiguous")
+    return (rows if shape[0] > 1 else 0), (heads if shape[1] > 1 else 0)
+
+
+def _rows(t: torch.Tensor, name: str, rows: int, dim: Optional[int], device):
+    """Row stride of a bf16 [rows, dim] tensor whose rows may be apart (columns of a wider one)."""
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    if t.dim() != 2 or t.shape[0] != rows or (dim is not None and t.shape[1] != dim):
+        raise ValueError(f"{name}: expected shape ({rows}, {'latent' if dim is None else dim}), got {tuple(t.shape)}")
+    stride, step = t.stride()
+    if step != 1:
+        raise ValueError(f"{name}: a row must be contiguous")
+    return stride if rows > 1 else t.shape[1]
+
+
+def _latent_append(scale, latent, k_rope, seqs: Seqs, rope, cache, weight, eps):
+    dev, T = seqs.device, seqs.total_q_rows
+    l_stride = _rows(latent, "latent", T, None, dev)
+    k_stride = _rows(k_rope, "k_rope", T, LATENT_ROPE_DIM, dev)
+    R = latent.shape[1]
+    _need(cache, "cache", torch.bfloat16 if scale is None else torch.uint8, (seqs.total_kv_rows, R + LATENT_ROPE_DIM), dev)
+    w = _weight(weight, "weight", R, dev)
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return _latent_append(scale, latent, k_rope, seqs, rope, cache, weight, eps)
+    if scale is None:
+        st = lib().msa_latent_append(latent.data_ptr(), l_stride, k_rope.data_ptr(), k_stride, seqs.ref(), R, w, float(eps),
+                                     _rope(rope, dev), cache.data_ptr(), _raw_stream(dev))
+    else:
+        st = lib().msa_latent_append_fp8(latent.data_ptr(), l_stride, k_rope.data_ptr(), k_stride, float(scale), seqs.ref(), R,
+                                         w, float(eps), _rope(rope, dev), cache.data_ptr(), _raw_stream(dev))
+    _check(st, "msa_latent_append" if scale is None else "msa_latent_append_fp8")
+
+
+def latent_append(latent, k_rope, seqs: Seqs, rope: Optional[Rope], cache, weight=None, eps: float = 1e-6) -> None:
+    """The new rows' latents [Tq, R] (norm, if ``weight``) and shared key parts [Tq, 64] (rotation) into their rows of
+    ``cache`` [Tkv, R + 64], in place; rows may be columns of a wider tensor."""
+    _latent_append(None, latent, k_rope, seqs, rope, cache, weight, eps)
+
+
+def latent_append_fp8(latent, k_rope, scale, seqs: Seqs, rope: Optional[Rope], cache, weight=None, eps: float = 1e-6) -> None:
+    """The same into a cache of e4m3 codes (uint8) with a per-tensor scale."""
+    _latent_append(scale, latent, k_rope, seqs, rope, cache, weight, eps)
+
+
+def latent_attn_paged_workspace_size(seqs: Seqs, num_heads: int, latent_dim: int) -> int:
+    return int(lib().msa_latent_attn_paged_workspace_size(seqs.ref(), num_heads, latent_dim))
+
+
+def _latent_paged(cache_scale, q, q_rope, cache, seqs: Seqs, softmax_scale, out, lse, workspace):
+    dev, T = seqs.device, seqs.total_q_rows
+    if q.dim() != 3:
+        raise ValueError(f"q: expected shape ({T}, heads, latent), got {tuple(q.shape)}")
+    H, R = q.shape[1], q.shape[2]
+    qs, qh = _strided(q, "q", (T, H, R), dev)
+    es, eh = _strided(q_rope, "q_rope", (T, H, LATENT_ROPE_DIM), dev)
+    _need(cache, "cache", torch.bfloat16 if cache_scale is None else torch.uint8, (seqs.total_kv_rows, R + LATENT_ROPE_DIM), dev)
+    _need_workspace(workspace, dev)
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return _latent_paged(cache_scale, q, q_rope, cache, seqs, softmax_scale, out, lse, workspace)
+    if out is None:
+        out = torch.empty(T, H, R, dtype=torch.bfloat16, device=dev)
+    else:
+        _need(out, "o", torch.bfloat16, (T, H, R), dev)
+    if lse is None:
+        lse = torch.empty(T, H, dtype=torch.float32, device=dev)
+    else:
+        _need(lse, "lse", torch.float32, (T, H), dev)
+    L, ref = lib(), seqs.ref()
+    if workspace is None:
+        workspace = _workspace(L.msa_latent_attn_paged_workspace_size(ref, H, R), dev, None)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    scale = _latent_scale(softmax_scale)
+    if cache_scale is None:
+        st = L.msa_latent_attn_paged(q.data_ptr(), qs, qh, q_rope.data_ptr(), es, eh, cache.data_ptr(), ref, H, R, scale,
+                                     out.data_ptr(), lse.data_ptr(), ws, ws_bytes, _raw_stream(dev))
+    else:
+        st = L.msa_latent_attn_paged_fp8(q.data_ptr(), qs, qh, q_rope.data_ptr(), es, eh, cache.data_ptr(), float(cache_scale),
+                                         ref, H, R, scale, out.data_ptr(), lse.data_ptr(), ws, ws_bytes, _raw_stream(dev))
+    _check(st, "msa_latent_attn_paged" if cache_scale is None else "msa_latent_attn_paged_fp8")
+    return out, lse
+
+
+def latent_attn_paged(q, q_rope, cache, seqs: Seqs, softmax_scale=None, out=None, lse=None, workspace=None):
+    """Latent attention, absorbed form, over a paged cache [Tkv, R + 64]: (O bf16 [Tq, H, R], the weighted latents, LSE fp32
+    [Tq, H]) of q [Tq, H, R] (queries times the key up-projection) and q_rope [Tq, H, 64], both with any row and
+    head strides.  ``softmax_scale`` defaults to that of the expanded head, 1 / sqrt(128 + 64)."""
+    return _latent_paged(None, q, q_rope, cache, seqs, softmax_scale, out, lse, workspace)
+
+
+def latent_attn_paged_fp8(q, q_rope, cache, scale, seqs: Seqs, softmax_scale=None, out=None, lse=None, workspace=None):
+    """The same on a cache of e4m3 codes (uint8) with a per-tensor scale; queries stay bf16."""
+    return _latent_paged(float(scale), q, q_rope, cache, seqs, softmax_scale, out, lse, workspace)
 
 
 # ---------------------------------------------------------------- kernel timing
