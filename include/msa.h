@@ -561,6 +561,74 @@ int msa_latent_attn_paged_fp8(const void* q, int64_t q_stride, int64_t q_head_st
                               size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * msa_latent_attn -- latent attention, expanded form: causal attention of prompts,
+ * training batches, and chunks whose context was expanded for them.
+ *
+ *   q          bf16 [total_q_rows, num_heads, 128], rows q_stride and heads
+ *              q_head_stride elements apart
+ *   q_rope     bf16 [total_q_rows, num_heads, 64], with strides of its own
+ *   kv         bf16 [total_kv_rows, num_heads, 256] contiguous: a head's own key part
+ *              (128), then its values (128), as one up-projection of the latents gives them
+ *   k_rope     bf16 rows [total_kv_rows], k_rope_stride elements apart, of 64 elements: the
+ *              shared key part, e.g. columns of a contiguous latent cache
+ *   o          bf16 [total_q_rows, num_heads, 128]   OUTPUT
+ *   lse        fp32 [total_q_rows, num_heads]        OUTPUT, natural log
+ *
+ * Rows without a visible key get O = 0 and LSE = -inf; rows behind the last sequence
+ * are left as they are.  A NaN or infinity among a sequence's own new keys may reach
+ * rows before it.  The weights are rounded to bf16 for the second product, their sums
+ * are of the unrounded ones.  Results are bit-reproducible for equal inputs.
+ *
+ * Supported: num_heads <= 256; contiguous key side; total_q_rows * num_heads < 2^31;
+ * strides a multiple of 8 elements, k_rope_stride at most 2^20; tensors 16-byte
+ * aligned (else MSA_ERR_UNSUPPORTED).  The query may give 0: then the workspace is
+ * not read and may be NULL.
+ * ------------------------------------------------------------------------ */
+size_t msa_latent_attn_workspace_size(const msa_seqs* seqs, int num_heads);
+int msa_latent_attn(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope,
+                    int64_t q_rope_stride, int64_t q_rope_head_stride, const void* kv, const void* k_rope,
+                    int64_t k_rope_stride, const msa_seqs* seqs, int num_heads, float softmax_scale, void* o,
+                    float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * msa_latent_attn_backward -- gradients of msa_latent_attn.
+ *
+ * For the upstream gradient dO of O, with P_ij = exp(S_ij - LSE_i), D_i = dO_i . O_i
+ * and dS_ij = P_ij (dO_i . v_j - D_i), for each head
+ *   dq_i = scale sum_j dS_ij k_j,   dq_rope_i = scale sum_j dS_ij k_rope_j,
+ *   dk_j = scale sum_i dS_ij q_i,   dv_j = sum_i P_ij dO_i,
+ * and, summed over the heads that share it,
+ *   dk_rope_j = scale sum_h sum_i dS_ij q_rope_i.
+ *
+ *   q .. k_rope, strides, seqs, num_heads, softmax_scale   as passed to the forward call
+ *   o, lse     the forward's outputs;  d_o  bf16 as o, the upstream gradient
+ *   d_q, d_q_rope   bf16 as q and q_rope, with strides of their own (rows and heads that
+ *              do not overlap; e.g. columns of a joint gradient)   OUTPUT
+ *   d_kv       bf16 [total_kv_rows, num_heads, 256]   OUTPUT: dk, then dv
+ *   d_k_rope   bf16 rows d_k_rope_stride elements apart, of 64 elements   OUTPUT
+ *
+ * Every key row is written (zeros where no query attends); query rows behind the last
+ * sequence are left as they are and take no part.  P and dS are rounded to bf16 for
+ * the products, everything else is fp32 with one rounding of each result; the heads'
+ * shares of d_k_rope are added in fp32 in the heads' order.  Every output is
+ * bit-reproducible.  Key ranges of different sequences must not overlap (the
+ * gradients of shared rows are unspecified).  No output may alias an input.
+ *
+ * Supported: as msa_latent_attn, with total_kv_rows * num_heads < 2^31, q_stride,
+ * q_rope_stride and k_rope_stride at most 2^24, d_q and d_q_rope 8-byte aligned with
+ * strides a multiple of 4 elements.
+ * ------------------------------------------------------------------------ */
+size_t msa_latent_attn_backward_workspace_size(const msa_seqs* seqs, int num_heads);
+int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope,
+                             int64_t q_rope_stride, int64_t q_rope_head_stride, const void* kv,
+                             const void* k_rope, int64_t k_rope_stride, const void* o, const float* lse,
+                             const void* d_o, const msa_seqs* seqs, int num_heads, float softmax_scale,
+                             void* d_q, int64_t d_q_stride, int64_t d_q_head_stride, void* d_q_rope,
+                             int64_t d_q_rope_stride, int64_t d_q_rope_head_stride, void* d_kv, void* d_k_rope,
+                             int64_t d_k_rope_stride, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * msa_sparse_attn_backward -- training backward of the Main Branch.
  *
  * Alg. 1 trains through the sparse attention of Sec. 3.1.  For an upstream

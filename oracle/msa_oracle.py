@@ -592,10 +592,10 @@ def latent_attention(q, q_rope, k, k_rope, v, layout: Layout, scale: float, rows
 def latent_attention_backward(q, q_rope, k, k_rope, v, o, lse, d_o, layout: Layout, scale: float):
     """Gradients of sum(d_o O) at the given O and LSE: (d_q, d_q_rope, d_k, d_k_rope, d_v), float64; and for each the sum of
     the sizes of its terms, which errors go by: a term's factor is P (|dO . v| + |dO| . |o|), not their difference."""
-    T, H = q.shape[:2]
+    H = q.shape[1]
     grads = [np.zeros_like(np.asarray(x, dtype=np.float64)) for x in (q, q_rope, k, k_rope, v)]
     sizes = [np.zeros_like(x) for x in grads]
-    for r in range(T):
+    for r in range(layout.total_q_rows):
         s, pos = layout.locate(r)
         if pos < 0:
             continue

@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libmsa.so")
 SOURCES = ["index_topk.hip", "sparse_attn.hip", "sparse_attn_prefill.hip", "sparse_attn_tile.hip",
            "sparse_attn_backward.hip",
            "sparse_kl_backward.hip", "dense_attn.hip", "dense_attn_paged.hip", "norm_rope.hip",
-           "latent_attn_paged.hip",
+           "latent_attn_paged.hip", "latent_attn.hip", "latent_attn_backward.hip",
            "msa_profile.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,545 @@
+// Gradients of latent attention's expanded form on gfx950.
+//
+// With P_ij = exp(scale (q_i . k_j + e_i . r_j) - LSE_i), D_i = dO_i . O_i and
+// dS_ij = P_ij (dO_i . v_j - D_i), for each head:
+//   dq_i = scale sum_j dS_ij k_j,  de_i = scale sum_j dS_ij r_j,
+//   dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dO_i,
+// and summed over the heads  dr_j = scale sum_h sum_i dS_ij e_i.
+//
+// Two kernels of one form, so that every sum has an order of its own and no
+// result depends on which CTA comes first: a wave keeps 32 rows of one side as
+// matrix operands in registers (queries and dO, or keys and values), streams the
+// other side 64 rows at a time through LDS, forms both score products of 32 x 32,
+// and adds the weights' products with the streamed rows, read down their columns.
+// What this repeats, the score products of the second kernel, is 20 of 72 matrix
+// products per 32 x 32; adding the queries' gradients from the key side would take
+// atomics, or a store and load of every dS.
+//
+// The products of one 32 streamed rows run ahead of the additions of the 32
+// before, between which the weights are formed.  The shared part's gradient leaves
+// per head in fp32 and latent_sum_kernel adds the heads in their order; it also
+// clears what no sequence owns.
+#include <initializer_list>
+#include <type_traits>
+
+#include "flash_tile.h"
+#include "latent_steps.h"
+
+namespace {
+
+using namespace msa;
+using flash::copy16;
+using flash::kDim;
+using flash::kLog2E;
+using flash::lds_address;
+using flash::lds_tr4;
+using flash::xor32f;
+using steps::TileGeom;
+using steps::tile_geom;
+
+constexpr int kRot = 64;                 // elements of the shared key part
+constexpr int kPair = 2 * kDim;          // a key's own part and its values
+constexpr int kRowsT = 64;               // streamed rows per tile
+constexpr int kWaves = 4;                // one per SIMD: a wave's operands and sums take 240 (keys) or 352 registers
+constexpr int kThreads = kWaves * kWave;
+constexpr int kRowTile = 64 * kWaves, kKeyTile = 32 * kWaves;      // stationary rows per CTA
+
+// Streamed rows in LDS: 16-byte segments, permuted by the row so that reads of
+// 16 rows' segment and transposing reads of 4 rows x 4 segments fall on all
+// banks: rows of 256 bytes and of 128 (odd ones start in the other half of the
+// banks).  The permutations are XORs, so an operand's address is one XOR from
+// another's.
+__device__ __forceinline__ int wide_mix(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+__device__ __forceinline__ int half_mix(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
+
+struct Tile {
+  uint16_t own[kRowsT * kDim], other[kRowsT * kDim], rot[kRowsT * kRot];
+};
+
+__device__ __forceinline__ void copy4(const char* base, uint32_t offset, uint32_t lds) {   // lane l's 4 bytes land at lds + 4 l
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(offset), "s"(base), "s"(lds) : "m0", "memory");
+#pragma clang diagnostic pop
+}
+
+struct Side {                            // [rows, heads] vectors: elements between rows and between heads
+  const uint16_t* p;
+  int64_t row, head;
+};
+struct Grad {
+  uint16_t* p;
+  int64_t row, head;
+};
+struct Args {
+  Side q, e, k, v, r, o, d_o;            // k, v: a key's own part and values; r: the shared part (head 0)
+  const float* lse;                      // [T, H]
+  Grad d_q, d_e, d_k, d_v;
+  float* stat;                           // [2][H][T]: LSE in base 2, D
+  float* d_r;                            // [H][total_kv][64], before the scale
+  int H;
+  float scale, scale_log2;
+};
+
+// KEYS: keys are stationary, 32 to a wave, and queries streamed; else queries are
+// stationary, 64 to a wave, so that an operand read from LDS feeds two products
+// (the keys' sums leave no registers for that), and keys streamed.
+template <bool KEYS>
+__global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, msa_seqs sq, flash::Grid gr) {
+  constexpr int KO = kDim / 16, KS = (kDim + kRot) / 16;
+  constexpr int ND = KS / 2;                       // 32-dimension tiles of own and shared part
+  constexpr int NA = KEYS ? ND + kDim / 32 : ND;   // accumulator tiles
+  constexpr int NT = KEYS ? 1 : 2;                 // 32-row tiles of stationary rows per wave
+  constexpr int kTileRows = 32 * NT * kWaves;
+  constexpr int NK = 16 / kWaves, NR = 8 / kWaves; // copies of 1 KiB per wave: wide rows, half rows
+  constexpr int kAhead = KEYS ? 5 : 3;
+  __shared__ __align__(16) Tile ring[2];
+  __shared__ __align__(16) float stat[2][2][KEYS ? kRowsT : 4];   // streamed queries: LSE, D
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int n = lane & 31, h = lane >> 5;
+  const int hd = static_cast<int>(blockIdx.x % a.H), which = static_cast<int>(blockIdx.x / a.H);
+
+  // ------------------------------------------------ the CTA's tile of stationary rows
+  int s = 0, tile = 0;
+  if constexpr (KEYS) {
+    int base = 0;
+    bool found = false;
+    for (int c = 0; c < sq.num_seqs && !found; c += kWave) {
+      const int mine = c + lane < sq.num_seqs ? (max(tile_geom(sq, c + lane).kv_len, 0) + kKeyTile - 1) / kKeyTile : 0;
+      int incl = mine;
+#pragma unroll
+      for (int d = 1; d < kWave; d *= 2) {
+        const int x = __shfl_up(incl, d);
+        if (lane >= d) incl += x;
+      }
+      const int all = __builtin_amdgcn_readlane(incl, kWave - 1);
+      if (which < base + all) {
+        const int j = __popcll(__ballot(which >= base + incl));
+        s = c + j;
+        tile = which - base - (j > 0 ? __builtin_amdgcn_readlane(incl, j - 1) : 0);
+        found = true;
+      }
+      base += all;
+    }
+    if (!found) return;
+  } else {
+    flash::locate_tile(sq, gr, which, kTileRows, &s, &tile);
+  }
+  const TileGeom g = tile_geom(sq, s);
+  const int64_t first_key = seq_geom(sq, s).kv_start;
+  const int base_p = g.kv_len - g.q_rows;          // position of the sequence's first query row
+  const int limit = KEYS ? g.kv_len : g.q_rows;
+  const int x0 = tile * kTileRows;                 // first stationary row
+  if (x0 >= limit) return;
+  const int x_end = min(x0 + kTileRows, limit);
+  const int w0 = x0 + 32 * NT * wave;              // the wave's first; the lane's are w0 + n + 32 nt
+  const int64_t base_x = KEYS ? first_key : g.q_begin;
+  const int streamed = KEYS ? g.q_rows : g.kv_len; // rows of the other side
+  // tiles of streamed rows that some stationary row meets
+  const int first_row = KEYS ? max(0, x0 - base_p) : 0;
+  const int end_row = KEYS ? g.q_rows : min(max(base_p + x_end, 0), g.kv_len);
+  const int b_begin = first_row / kRowsT, b_end = first_row < end_row ? (end_row + kRowsT - 1) / kRowsT : b_begin;
+
+  // ------------------------------------------------ copies of streamed rows
+  const Side own = KEYS ? a.q : a.k, other = KEYS ? a.d_o : a.v, rot = KEYS ? a.e : a.r;
+  const int64_t row0 = KEYS ? g.q_begin : first_key;
+  const char* own_p = reinterpret_cast<const char*>(own.p + row0 * own.row + hd * own.head);
+  const char* other_p = reinterpret_cast<const char*>(other.p + row0 * other.row + hd * other.head);
+  const char* rot_p = reinterpret_cast<const char*>(rot.p + row0 * rot.row + hd * rot.head);
+  const uint32_t own_s = static_cast<uint32_t>(own.row * 2), other_s = static_cast<uint32_t>(other.row * 2),
+                 rot_s = static_cast<uint32_t>(rot.row * 2);
+  const uint32_t lds0 = lds_address(&ring[0]);
+  constexpr uint32_t kOwnAt = 0, kOtherAt = sizeof(uint16_t) * kRowsT * kDim, kRotAt = 2 * kOtherAt;
+  auto copy = [&](int b, int buf) {
+    const int last = streamed - 1 - b * kRowsT;    // rows past the end repeat the last one
+    const uint32_t dst = lds0 + buf * static_cast<uint32_t>(sizeof(Tile)) + 1024 * wave;
+    const int64_t at = static_cast<int64_t>(b) * kRowsT;
+    const char* p0 = own_p + at * own_s;
+    const char* p1 = other_p + at * other_s;
+    const char* p2 = rot_p + at * rot_s;
+    int ln = lane;
+    asm volatile("" : "+v"(ln));                   // as above
+#pragma unroll
+    for (int c = 0; c < NK; ++c) {
+      const int r = 4 * (c * kWaves + wave) + (ln >> 4);
+      const uint32_t seg = 16 * ((ln & 15) ^ wide_mix(r)), rr = min(r, last);
+      copy16(p0, rr * own_s + seg, dst + kOwnAt + 1024 * kWaves * c);
+      copy16(p1, rr * other_s + seg, dst + kOtherAt + 1024 * kWaves * c);
+    }
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const int r = 8 * (c * kWaves + wave) + (ln >> 3);
+      copy16(p2, min(r, last) * rot_s + 16 * ((ln & 7) ^ half_mix(r)), dst + kRotAt + 1024 * kWaves * c);
+    }
+    if constexpr (KEYS) {
+      if (wave < 2) {
+        const float* src = a.stat + (static_cast<int64_t>(wave) * a.H + hd) * sq.total_q_rows + row0 + at;
+        copy4(reinterpret_cast<const char*>(src), 4 * min(lane, last), lds_address(&stat[buf][wave][0]));
+      }
+    }
+  };
+
+  // ------------------------------------------------ stationary operands
+  bf16x8 b1[NT][KS], b2[NT][KO];
+  float lane_lse[NT] = {}, lane_d[NT] = {};
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const Side f = KEYS ? a.k : a.q, t = KEYS ? a.r : a.e, w = KEYS ? a.v : a.d_o;
+    const bool valid = w0 + 32 * nt + n < limit;
+    const int64_t mine = base_x + (valid ? w0 + 32 * nt + n : x0);
+    const uint16_t* fp = f.p + mine * f.row + hd * f.head + 8 * h;
+    const uint16_t* tp = t.p + mine * t.row + hd * t.head + 8 * h;
+    const uint16_t* wp = w.p + mine * w.row + hd * w.head + 8 * h;
+#pragma unroll
+    for (int st = 0; st < KS; ++st) b1[nt][st] = ld_bf16x8(st < KO ? fp + 16 * st : tp + 16 * (st - KO));
+#pragma unroll
+    for (int st = 0; st < KO; ++st) b2[nt][st] = ld_bf16x8(wp + 16 * st);
+    if constexpr (!KEYS) {
+      const uint16_t* op = a.o.p + mine * a.o.row + hd * a.o.head + 8 * h;
+#pragma unroll
+      for (int st = 0; st < KO; ++st) {
+        const bf16x8 ov = ld_bf16x8(op + 16 * st);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          lane_d[nt] = fmaf(static_cast<float>(ov[i]), static_cast<float>(b2[nt][st][i]), lane_d[nt]);
+      }
+      lane_d[nt] += xor32f(lane_d[nt]);
+      lane_lse[nt] = a.lse[mine * a.H + hd] * kLog2E;
+      if (valid && h == 0) {
+        a.stat[static_cast<int64_t>(hd) * sq.total_q_rows + mine] = lane_lse[nt];
+        a.stat[(static_cast<int64_t>(a.H) + hd) * sq.total_q_rows + mine] = lane_d[nt];
+      }
+    }
+  }
+
+  // ------------------------------------------------ operand addresses
+  const uint32_t row_own = n * 2 * kDim + 16 * (h ^ wide_mix(n));
+  const uint32_t row_rot = n * 2 * kRot + 16 * (h ^ half_mix(n));
+  uint32_t col_own, col_rot;
+  {
+    // transposed operand: in each 16-lane group, lane j addresses row k0 + j/4, dims n0 + 4(j%4) .. +3 and
+    // receives rows k0 .. k0+3 of dim n0 + j
+    const int gq = lane >> 4, jj = lane & 15;
+    const int rl = 4 * h + (jj >> 2), seg = 2 * (gq & 1) + ((jj & 3) >> 1);
+    col_own = rl * 2 * kDim + 16 * (seg ^ wide_mix(rl)) + 8 * (jj & 1);
+    col_rot = rl * 2 * kRot + 16 * (seg ^ half_mix(rl)) + 8 * (jj & 1);
+  }
+  auto tr8 = [](const char* p0, const char* p1) {
+    const uint2 y0 = lds_tr4(reinterpret_cast<const uint16_t*>(p0)), y1 = lds_tr4(reinterpret_cast<const uint16_t*>(p1));
+    return __builtin_bit_cast(bf16x8, make_uint4(y0.x, y0.y, y1.x, y1.y));
+  };
+
+  f32x16 acc[NA][NT];
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[i][nt] = f32x16{};
+  bf16x8 ps[NT][2], pp[NT][2];                           // pending dS and (KEYS) P of 32 streamed rows, as B operands
+
+  // both score products of streamed rows 32 half .. + 31: lane (n, h) gets rows 8(i/4) + 4h + i%4 against its own
+  auto products = [&](int buf, int half, f32x16 (&z)[NT], f32x16 (&dz)[NT]) {
+    const char* t = reinterpret_cast<const char*>(&ring[buf]);
+    const char* t_own = t + kOwnAt + half * 32 * 2 * kDim;
+    const char* t_rot = t + kRotAt + half * 32 * 2 * kRot;
+    const char* t_other = t + kOtherAt + half * 32 * 2 * kDim;
+    uint32_t at_own = row_own, at_rot = row_rot;
+    asm volatile("" : "+v"(at_own), "+v"(at_rot));   // the addresses are formed here each time: held, they spill
+    auto read = [&](int j) -> bf16x8 {
+      const char* p = j < KO ? t_own + (at_own ^ (32 * j)) : j < KS ? t_rot + (at_rot ^ (32 * (j - KO)))
+                                                                     : t_other + (at_own ^ (32 * (j - KS)));
+      return ld_bf16x8(reinterpret_cast<const uint16_t*>(p));
+    };
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) z[nt] = dz[nt] = f32x16{};
+    bf16x8 op[KS + KO];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) op[j] = read(j);
+#pragma unroll
+    for (int j = 0; j < KS + KO; ++j) {
+      if (j + kAhead < KS + KO) op[j + kAhead] = read(j + kAhead);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if (j < KS) z[nt] = mfma32x32x16(op[j], b1[nt][j < KS ? j : 0], z[nt]);
+        else dz[nt] = mfma32x32x16(op[j], b2[nt][j < KS ? 0 : j - KS], dz[nt]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // adds the pending weights' products with their streamed rows; beside(j) after the j-th slot
+  constexpr int kSlots = 2 * NA;
+  auto additions = [&](int buf, int half, auto beside) {
+    const char* t = reinterpret_cast<const char*>(&ring[buf]);
+    uint32_t at_own = col_own, at_rot = col_rot;
+    asm volatile("" : "+v"(at_own), "+v"(at_rot));   // as above
+    auto read = [&](int j) -> bf16x8 {
+      const int u = j / NA, i = j % NA;            // 16 streamed rows, accumulator tile
+      const int r = 32 * half + 16 * u;
+      if (i < KO / 2 || i >= ND) {
+        const char* p = t + (i < ND ? kOwnAt : kOtherAt) + r * 2 * kDim;
+        const uint32_t at = at_own ^ (64 * (i < ND ? i : i - ND));
+        return tr8(p + at, p + (at ^ 32) + 8 * 2 * kDim);
+      }
+      const char* p = t + kRotAt + r * 2 * kRot;
+      const uint32_t at = at_rot ^ (64 * (i - KO / 2));
+      return tr8(p + at, p + (at ^ 16) + 8 * 2 * kRot);
+    };
+    bf16x8 op[kSlots];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) op[j] = read(j);
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j) {
+      if (j + kAhead < kSlots) op[j + kAhead] = read(j + kAhead);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+        acc[j % NA][nt] = mfma32x32x16(op[j], j % NA < ND ? ps[nt][j / NA] : pp[nt][j / NA], acc[j % NA][nt]);
+      beside(j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // P and dS of 32 streamed rows in kSlots pieces: z becomes P, dz dS.  The last two pieces pack them, each after the
+  // last slot that adds what was there before.
+  f32x4 row_lse{}, row_d{};
+  auto weigh = [&](int buf, int row, auto masked, f32x16 (&z)[NT], f32x16 (&dz)[NT], int j) __attribute__((always_inline)) {
+    constexpr int kLast = kSlots - 2;
+    static_assert(kLast >= NA, "");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i * kLast / 16 != j) continue;
+      if constexpr (KEYS) {
+        if (i % 4 == 0) {
+          const int at = (row & (kRowsT - 1)) + 8 * (i / 4) + 4 * h;
+          row_lse = *reinterpret_cast<const f32x4*>(&stat[buf][0][at]);
+          row_d = *reinterpret_cast<const f32x4*>(&stat[buf][1][at]);
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p = exp2_hw(fmaf(z[nt][i], a.scale_log2, KEYS ? -row_lse[i % 4] : -lane_lse[nt]));
+        if constexpr (decltype(masked)::value) {
+          const int x = w0 + 32 * nt + n, y = row + 8 * (i / 4) + 4 * h + (i % 4);
+          const bool seen = KEYS ? x <= base_p + y && y < g.q_rows : y <= base_p + x;
+          p = seen ? p : 0.f;
+        }
+        z[nt][i] = p;
+        dz[nt][i] = p * (dz[nt][i] - (KEYS ? row_d[i % 4] : lane_d[nt]));
+      }
+    }
+    if (j >= kLast) {
+      const int u = j - kLast;
+      auto pack = [&](const f32x16& v) {
+        uint4 y;
+        y.x = pack_bf16x2(v[8 * u + 0], v[8 * u + 1]);
+        y.y = pack_bf16x2(v[8 * u + 2], v[8 * u + 3]);
+        y.z = pack_bf16x2(v[8 * u + 4], v[8 * u + 5]);
+        y.w = pack_bf16x2(v[8 * u + 6], v[8 * u + 7]);
+        return __builtin_bit_cast(bf16x8, y);
+      };
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        ps[nt][u] = pack(dz[nt]);
+        if constexpr (KEYS) pp[nt][u] = pack(z[nt]);
+      }
+    }
+  };
+  // whether some lane of the wave has a streamed row of tile b that it does not meet
+  auto is_masked = [&](int b) {
+    return KEYS ? base_p + b * kRowsT < w0 + 32 * NT - 1 || (b + 1) * kRowsT > g.q_rows : (b + 1) * kRowsT > base_p + w0 + 1;
+  };
+  auto sync = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  if (b_begin < b_end) {
+    copy(b_begin, 0);
+    if (b_begin + 1 < b_end) copy(b_begin + 1, 1);
+    // copies per wave and tile; (KEYS, waves 0 and 1) one more, so waiting for the older tile's leaves none of it
+    constexpr int kCopies = 2 * NK + NR;
+    if (b_begin + 1 < b_end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    sync();
+    f32x16 z[NT], dz[NT];
+    products(0, 0, z, dz);
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j) weigh(0, b_begin * kRowsT, std::true_type{}, z, dz, j);
+    // rows 32 .. 63 of tile b, then rows 0 .. 31 of tile b + 1: the products of these, the additions of those before
+    auto step = [&](int b, auto masked) __attribute__((always_inline)) {
+      const int buf = (b - b_begin) & 1;
+      products(buf, 1, z, dz);
+      additions(buf, 0, [&](int j) __attribute__((always_inline)) { weigh(buf, b * kRowsT + 32, masked, z, dz, j); });
+      if (b + 1 == b_end) return;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // tile b + 1 has landed
+      sync();
+      products(buf ^ 1, 0, z, dz);
+      additions(buf, 1, [&](int j) __attribute__((always_inline)) { weigh(buf ^ 1, (b + 1) * kRowsT, masked, z, dz, j); });
+      sync();                                                      // tile b's readers are done
+      if (b + 2 < b_end) copy(b + 2, buf);
+    };
+    int b = b_begin;
+    if constexpr (KEYS)
+      for (; b < b_end && (is_masked(b) || is_masked(b + 1)); ++b) step(b, std::true_type{});
+    for (; b + 1 < b_end && !is_masked(b + 1) && !is_masked(b); ++b) step(b, std::false_type{});
+    for (; b < b_end; ++b) step(b, std::true_type{});
+    additions((b_end - 1 - b_begin) & 1, 1, [](int) {});
+  }
+
+  // ------------------------------------------------ results: lane (n, h) holds dims 32i + 8(e/4) + 4h + e%4 of its row
+  auto store = [&](const f32x16& v, float f, uint16_t* y) {
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      uint2 p;
+      p.x = pack_bf16x2(v[4 * e4 + 0] * f, v[4 * e4 + 1] * f);
+      p.y = pack_bf16x2(v[4 * e4 + 2] * f, v[4 * e4 + 3] * f);
+      *reinterpret_cast<uint2*>(y + 8 * e4) = p;
+    }
+  };
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int x = w0 + 32 * nt + n;
+    if (x >= limit) continue;
+    const int64_t mine = base_x + x;
+    const Grad to = KEYS ? a.d_k : a.d_q;
+    uint16_t* y = to.p + mine * to.row + hd * to.head + 4 * h;
+#pragma unroll
+    for (int i = 0; i < KO / 2; ++i) store(acc[i][nt], a.scale, y + 32 * i);
+    if constexpr (KEYS) {
+      uint16_t* yv = a.d_v.p + mine * a.d_v.row + hd * a.d_v.head + 4 * h;
+#pragma unroll
+      for (int i = 0; i < kDim / 32; ++i) store(acc[ND + i][nt], 1.f, yv + 32 * i);
+      float* yr = a.d_r + (static_cast<int64_t>(hd) * sq.total_kv_rows + mine) * kRot + 4 * h;
+#pragma unroll
+      for (int i = KO / 2; i < ND; ++i)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4)
+          *reinterpret_cast<f32x4*>(yr + 32 * (i - KO / 2) + 8 * e4) =
+              f32x4{acc[i][nt][4 * e4], acc[i][nt][4 * e4 + 1], acc[i][nt][4 * e4 + 2], acc[i][nt][4 * e4 + 3]};
+    } else {
+      uint16_t* ye = a.d_e.p + mine * a.d_e.row + hd * a.d_e.head + 4 * h;
+#pragma unroll
+      for (int i = KO / 2; i < ND; ++i) store(acc[i][nt], a.scale, ye + 32 * (i - KO / 2));
+    }
+  }
+}
+
+// The shared part's gradient: the heads' sums, added in their order, times the
+// scale.  A wave takes a key row, one element per lane.  Rows that no sequence
+// owns get zeros, in d_kv too.
+__global__ __launch_bounds__(256) void latent_sum_kernel(const float* __restrict__ d_r, msa_seqs sq, int H, float scale,
+                                                         uint16_t* __restrict__ d_kv, uint16_t* __restrict__ out, int64_t out_row) {
+  const int lane = lane_id();
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave;
+  if (row >= sq.total_kv_rows) return;
+  bool owned = false;
+  for (int c = 0; c < sq.num_seqs && !owned; c += kWave) {
+    bool here = false;
+    if (c + lane < sq.num_seqs) {
+      const int64_t start = seq_geom(sq, c + lane).kv_start;
+      here = row >= start && row < start + tile_geom(sq, c + lane).kv_len;
+    }
+    owned = __ballot(here) != 0;
+  }
+  float sum = 0.f;
+  if (owned) {
+    for (int h0 = 0; h0 < H; h0 += 8) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = d_r[(static_cast<int64_t>(min(h0 + i, H - 1)) * sq.total_kv_rows + row) * kRot + lane];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += h0 + i < H ? v[i] : 0.f;
+    }
+  } else {
+    u32x4* y = reinterpret_cast<u32x4*>(d_kv + row * H * kPair);
+    for (int i = lane; i < H * kPair / 8; i += kWave) y[i] = u32x4{};
+  }
+  out[row * out_row + lane] = static_cast<uint16_t>(pack_bf16x2(sum * scale, 0.f));
+}
+
+// ---------------------------------------------------------------- host side
+int validate_backward(const msa_seqs* seqs, int H) {
+  int st = msa_host::validate_seqs(seqs);
+  if (st != MSA_OK) return st;
+  if (H < 1) return MSA_ERR_INVALID;
+  if (seqs->block_table) return MSA_ERR_UNSUPPORTED;   // contiguous key side only
+  if (H > 256) return MSA_ERR_UNSUPPORTED;
+  if (seqs->total_q_rows * H >= (int64_t(1) << 31) || seqs->total_kv_rows * H >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
+  return MSA_OK;
+}
+size_t stat_bytes(const msa_seqs* s, int H) { return msa_host::align_up(sizeof(float) * 2 * H * s->total_q_rows, 256); }
+size_t work_bytes(const msa_seqs* s, int H) { return stat_bytes(s, H) + sizeof(float) * kRot * H * s->total_kv_rows; }
+
+bool aligned(const void* p, int by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) == 0; }
+
+}  // namespace
+
+extern "C" size_t msa_latent_attn_backward_workspace_size(const msa_seqs* seqs, int num_heads) {
+  return validate_backward(seqs, num_heads) == MSA_OK ? work_bytes(seqs, num_heads) : 0;
+}
+
+extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t q_head_stride, const void* q_rope,
+                                        int64_t q_rope_stride, int64_t q_rope_head_stride, const void* kv, const void* k_rope,
+                                        int64_t k_rope_stride, const void* o, const float* lse, const void* d_o,
+                                        const msa_seqs* seqs, int num_heads, float softmax_scale, void* d_q, int64_t d_q_stride,
+                                        int64_t d_q_head_stride, void* d_q_rope, int64_t d_q_rope_stride,
+                                        int64_t d_q_rope_head_stride, void* d_kv, void* d_k_rope, int64_t d_k_rope_stride,
+                                        void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int st = validate_backward(seqs, num_heads);
+  if (st != MSA_OK) return st;
+  const int H = num_heads;
+  const int64_t T = seqs->total_q_rows, N = seqs->total_kv_rows;
+  if (N == 0) return MSA_OK;                           // then there are no rows either
+  if (T > 0 && (!q || !q_rope || !o || !lse || !d_o || !d_q || !d_q_rope)) return MSA_ERR_INVALID;
+  if (!kv || !k_rope || !d_kv || !d_k_rope) return MSA_ERR_INVALID;
+  // rows and heads of the results do not overlap
+  auto apart = [&](int64_t row, int64_t head, int dim) {
+    if ((T > 1 && row < dim) || (H > 1 && head < dim)) return false;
+    return T <= 1 || H == 1 || row >= (H - 1) * head + dim || head >= (T - 1) * row + dim;
+  };
+  for (int64_t x : {q_stride, q_head_stride, q_rope_stride, q_rope_head_stride, k_rope_stride, d_q_stride, d_q_head_stride,
+                    d_q_rope_stride, d_q_rope_head_stride, d_k_rope_stride})
+    if (x < 0) return MSA_ERR_INVALID;
+  if (T > 0 && (!apart(d_q_stride, d_q_head_stride, kDim) || !apart(d_q_rope_stride, d_q_rope_head_stride, kRot)))
+    return MSA_ERR_INVALID;
+  if (N > 1 && d_k_rope_stride < kRot) return MSA_ERR_INVALID;
+  for (const void* x : {q, q_rope, kv, k_rope, o, d_o, static_cast<const void*>(d_kv)})
+    if (!aligned(x, 16)) return MSA_ERR_UNSUPPORTED;
+  if (!aligned(d_q, 8) || !aligned(d_q_rope, 8) || !aligned(d_k_rope, 2)) return MSA_ERR_UNSUPPORTED;
+  if ((q_stride | q_head_stride | q_rope_stride | q_rope_head_stride | k_rope_stride) % 8 != 0) return MSA_ERR_UNSUPPORTED;
+  if ((d_q_stride | d_q_head_stride | d_q_rope_stride | d_q_rope_head_stride) % 4 != 0) return MSA_ERR_UNSUPPORTED;
+  for (int64_t x : {q_stride, q_rope_stride, k_rope_stride})
+    if (x > (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;           // 64 rows' offsets are 32 bits
+  if (!workspace || workspace_bytes < work_bytes(seqs, H)) return MSA_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return MSA_ERR_UNSUPPORTED;
+  const auto* kvp = static_cast<const uint16_t*>(kv);
+  auto* dkv = static_cast<uint16_t*>(d_kv);
+  const int64_t kv_row = static_cast<int64_t>(H) * kPair, o_row = static_cast<int64_t>(H) * kDim;
+  Args a{};
+  a.q = Side{static_cast<const uint16_t*>(q), q_stride, q_head_stride};
+  a.e = Side{static_cast<const uint16_t*>(q_rope), q_rope_stride, q_rope_head_stride};
+  a.k = Side{kvp, kv_row, kPair};
+  a.v = Side{kvp + kDim, kv_row, kPair};
+  a.r = Side{static_cast<const uint16_t*>(k_rope), k_rope_stride, 0};
+  a.o = Side{static_cast<const uint16_t*>(o), o_row, kDim};
+  a.d_o = Side{static_cast<const uint16_t*>(d_o), o_row, kDim};
+  a.lse = lse;
+  a.d_q = Grad{static_cast<uint16_t*>(d_q), d_q_stride, d_q_head_stride};
+  a.d_e = Grad{static_cast<uint16_t*>(d_q_rope), d_q_rope_stride, d_q_rope_head_stride};
+  a.d_k = Grad{dkv, kv_row, kPair};
+  a.d_v = Grad{dkv + kDim, kv_row, kPair};
+  a.stat = static_cast<float*>(workspace);
+  a.d_r = reinterpret_cast<float*>(static_cast<char*>(workspace) + stat_bytes(seqs, H));
+  a.H = H;
+  a.scale = softmax_scale;
+  a.scale_log2 = softmax_scale * kLog2E;
+  int64_t tiles;
+  const flash::Grid gr = flash::plan_grid(seqs, kRowTile, seqs->max_q_rows, &tiles);
+  const int64_t key_tiles = seqs->num_seqs == 1 ? (std::min<int64_t>(seqs->max_kv_len, N) + kKeyTile - 1) / kKeyTile
+                                                : N / kKeyTile + seqs->num_seqs;
+  if (std::max(tiles, key_tiles) * H >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
+  if (T > 0)
+    msa_prof::launch("latent_backward_q_kernel", latent_backward_kernel<false>, dim3(static_cast<unsigned>(tiles * H)),
+                     dim3(kThreads), 0, stream, a, *seqs, gr);
+  msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true>,
+                   dim3(static_cast<unsigned>(key_tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
+  msa_prof::launch("latent_sum_kernel", latent_sum_kernel, dim3(static_cast<unsigned>((N + 3) / 4)), dim3(256), 0, stream,
+                   static_cast<const float*>(a.d_r), *seqs, H, softmax_scale, dkv, static_cast<uint16_t*>(d_k_rope),
+                   d_k_rope_stride);
+  return msa_host::launch_status();
+}

@@ -21,9 +21,11 @@
 // out evenly over the chip; a CTA forms the numbering from the lengths on the
 // device.  Where a tile is shared by several CTAs each leaves its part in fp32,
 // and latent_merge_kernel joins them by the log-sum-exp rule in key order.
+#include <initializer_list>
 #include <type_traits>
 
 #include "flash_tile.h"
+#include "latent_steps.h"
 
 namespace {
 
@@ -34,9 +36,12 @@ using flash::kLog2E;
 using flash::lds_address;
 using flash::lds_tr4;
 using flash::xor32f;
+using steps::kKeys;
+using steps::Share;
+using steps::TileGeom;
+using steps::tile_geom;
 
 constexpr int kRot = 64;                 // elements of the shared rotated part
-constexpr int kKeys = 64;                // keys per step
 constexpr int kRows = 64;                // (row, head) pairs per tile
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
@@ -66,56 +71,6 @@ struct LatentParts {
   float* lse;                            // [CTA][2][64], base 2
   int4* tile;                            // [CTA]: the tile in slot 1: sequence, tile, parts (0: none)
 };
-
-struct TileGeom {
-  int q_begin, q_rows, kv_len;
-};
-__device__ __forceinline__ TileGeom tile_geom(const msa_seqs& sq, int s) {
-  const SeqGeom g = seq_geom(sq, s);
-  TileGeom t;
-  t.q_begin = g.q_begin;
-  t.q_rows = static_cast<int>(max<int64_t>(0, min<int64_t>(min(g.q_rows, sq.max_q_rows), sq.total_q_rows - g.q_begin)));
-  t.kv_len = min(g.kv_len, sq.max_kv_len);
-  return t;
-}
-// Steps that tile x of a sequence is numbered with: those of its last row, at
-// least one.  `ahead` keys lie before the sequence's first row.
-struct TileSteps {
-  int64_t ahead;
-  int last_steps, tiles, rows;
-  __device__ __forceinline__ TileSteps(const TileGeom& g, int rows_per_tile) {
-    ahead = max(g.kv_len - g.q_rows, 0);
-    last_steps = max(1, (g.kv_len + kKeys - 1) / kKeys);
-    tiles = (g.q_rows + rows_per_tile - 1) / rows_per_tile;
-    rows = rows_per_tile;
-  }
-  __device__ __forceinline__ int64_t one(int64_t x) const {        // of a tile that is not the last
-    return (ahead + (x + 1) * rows + kKeys - 1) >> 6;
-  }
-  __device__ __forceinline__ int64_t of(int x) const { return x < tiles - 1 ? one(x) : last_steps; }
-  // of tiles 0 .. x - 1, x < tiles: one(y + 64) = one(y) + rows
-  __device__ __forceinline__ int64_t before(int x) const {
-    const int64_t q = x >> 6;
-    const int r = x & 63;
-    int64_t part = 0, all = 0;
-    for (int y = 0; y < (q > 0 ? 64 : r); ++y) {
-      const int64_t c = one(y);
-      all += c;
-      if (y < r) part += c;
-    }
-    return q * all + 64 * rows * (q * (q - 1) / 2) + part + static_cast<int64_t>(r) * rows * q;
-  }
-  __device__ __forceinline__ int64_t total() const { return tiles < 1 ? 0 : before(tiles - 1) + last_steps; }
-};
-
-__device__ __forceinline__ int64_t scan_incl(int64_t v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const int64_t x = __shfl_up(static_cast<long long>(v), d);
-    if (lane_id() >= d) v += x;
-  }
-  return v;
-}
 
 // T: cache elements, uint16_t = bf16 bits, uint8_t = E4M3 codes (o_scale
 // multiplies O); R: latent elements.
@@ -147,65 +102,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
   const int block = (id >> 3) % pl.blocks, range = (id >> 3) / pl.blocks * 8 + (id & 7);
   const int cta = range * pl.blocks + block;
 
-  // ------------------------------------------------ the share's steps
-  struct Chunk {
-    int64_t incl, mine;                    // per lane: steps up to and of sequence 64 c + lane
-  };
-  auto chunk = [&](int c) {
-    const int s = 64 * c + lane;
-    int64_t cost = 0;
-    if (s < sq.num_seqs) cost = TileSteps(tile_geom(sq, s), pl.rows).total();
-    return Chunk{scan_incl(cost), cost};
-  };
-  auto last_of = [](int64_t v) { return static_cast<int64_t>(readlane_u64(static_cast<uint64_t>(v), kWave - 1)); };
-  const int chunks = (sq.num_seqs + 63) >> 6;
-  Chunk ch = chunk(0);
-  int64_t total = last_of(ch.incl);
-  for (int c = 1; c < chunks; ++c) total += last_of(chunk(c).incl);
-  const int64_t per = max<int64_t>(pl.min_steps, (total + pl.ranges - 1) / pl.ranges);
-  int64_t u = range * per;
-  const int64_t u_end = min(u + per, total);
+  Share sh(sq, pl.rows, pl.ranges, pl.min_steps, range);
   if (threadIdx.x == 0) parts.tile[cta] = make_int4(0, 0, 0, 0);
-  if (u >= u_end) return;
-  int s = 0;
-  int64_t first = 0;                       // first step of sequence s
-  {
-    int64_t base = 0;
-    for (int c = 0;; ++c) {
-      if (c > 0) ch = chunk(c);
-      const int64_t all = last_of(ch.incl);
-      if (u < base + all) {
-        const uint64_t m = __ballot(u >= base + ch.incl);         // sequences that end before u
-        const int j = __popcll(m);
-        s = 64 * c + j;
-        first = base + (j > 0 ? static_cast<int64_t>(readlane_u64(static_cast<uint64_t>(ch.incl), j - 1)) : 0);
-        break;
-      }
-      base += all;
-    }
-  }
-  TileGeom g = tile_geom(sq, s);
-  TileSteps ts(g, pl.rows);
-  int x = 0;                               // tile of the sequence
-  int64_t tile_first = first;
-  if (ts.tiles > 1) {
-    // as TileSteps::before, the sums within a period of 64 tiles one per lane
-    const int64_t incl = scan_incl(ts.one(lane));
-    const int64_t all = last_of(incl);
-    auto before = [&](int y) {
-      const int64_t k = y >> 6;
-      const int r = y & 63;
-      const int64_t part = r > 0 ? static_cast<int64_t>(readlane_u64(static_cast<uint64_t>(incl), r - 1)) : 0;
-      return k * all + 64 * pl.rows * (k * (k - 1) / 2) + part + static_cast<int64_t>(r) * pl.rows * k;
-    };
-    int lo = 0, hi = ts.tiles - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (first + before(mid) <= u) lo = mid; else hi = mid - 1;
-    }
-    x = lo;
-    tile_first = first + before(x);
-  }
 
   // ------------------------------------------------ lane geometry
   const int tile_heads = min(pl.heads, H - block * pl.heads);     // of this block
@@ -235,17 +133,17 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
   const int lg_page = 31 - __clz(sq.page_size);
   const int max_page = static_cast<int>(sq.total_kv_rows >> lg_page) - 1;
 
-  while (u < u_end) {
-    const int64_t cost = ts.of(x);
-    const int64_t c_begin = u - tile_first, c_end = min(cost, c_begin + (u_end - u));
-    const int t0 = x * pl.rows, t_end = min(t0 + pl.rows, g.q_rows);
+  for (; sh.more(); sh.next()) {
+    const TileGeom& g = sh.g;
+    const int64_t c_begin = sh.begin(), c_end = sh.end();
+    const int t0 = sh.x * pl.rows, t_end = min(t0 + pl.rows, g.q_rows);
     const int base_p = g.kv_len - g.q_rows;                       // position of the sequence's first row
     const int seen = min(max(base_p + t_end, 0), g.kv_len);       // keys that the tile's last row sees
     const int visits = (seen + kKeys - 1) / kKeys;
     const int b_begin = static_cast<int>(min<int64_t>(c_begin, visits)), b_end = static_cast<int>(min<int64_t>(c_end, visits));
     const int nfree = max(0, base_p + t0 + 1) / kKeys;            // steps below see every row's keys
     const int pairs = (t_end - t0) * tile_heads;                  // rows of the tile
-    const int32_t* table = sq.block_table + static_cast<int64_t>(s) * sq.block_table_stride;
+    const int32_t* table = sq.block_table + static_cast<int64_t>(sh.s) * sq.block_table_stride;
 
     // this lane's row of the scores, and of the two row halves of O
     const int mine = 32 * rh + n;
@@ -513,20 +411,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         if (wave == 0 && h == 0) parts.lse[slot * kRows + 32 * j + n] = lse2[j];
       }
       if (b_begin == 0 && threadIdx.x == 0)
-        parts.tile[cta] = make_int4(s, x, static_cast<int>((tile_first + visits - 1) / per) - range + 1, 0);
-    }
-
-    // ------------------------------------------------ next tile
-    u += c_end - c_begin;
-    if (u < u_end) {
-      tile_first += cost;
-      if (++x == ts.tiles) {
-        x = 0;
-        do {
-          g = tile_geom(sq, ++s);
-        } while (g.q_rows < 1);            // steps are left, so a sequence with rows follows
-        ts = TileSteps(g, pl.rows);
-      }
+        parts.tile[cta] = make_int4(sh.s, sh.x, sh.parts(visits), 0);
     }
   }
 }

@@ -32,6 +32,8 @@ EXPORTS = [
     "msa_kv_append", "msa_kv_append_fp8",
     "msa_latent_append", "msa_latent_append_fp8",
     "msa_latent_attn_paged_workspace_size", "msa_latent_attn_paged", "msa_latent_attn_paged_fp8",
+    "msa_latent_attn_workspace_size", "msa_latent_attn",
+    "msa_latent_attn_backward_workspace_size", "msa_latent_attn_backward",
     "msa_sparse_attn_backward_workspace_size", "msa_sparse_attn_backward",
     "msa_sparse_kl_backward_workspace_size", "msa_sparse_kl_backward",
     "msa_profile_enable", "msa_profile_reset", "msa_profile_kernel_name", "msa_profile_read",
@@ -128,6 +130,14 @@ def lib() -> ctypes.CDLL:
         L.msa_latent_attn_paged.restype = I
         L.msa_latent_attn_paged_fp8.argtypes = [P, N, N, P, N, N, P, F, S, I, I, F, P, P, P, Z, P]
         L.msa_latent_attn_paged_fp8.restype = I
+        L.msa_latent_attn_workspace_size.argtypes = [S, I]
+        L.msa_latent_attn_workspace_size.restype = Z
+        L.msa_latent_attn.argtypes = [P, N, N, P, N, N, P, P, N, S, I, F, P, P, P, Z, P]
+        L.msa_latent_attn.restype = I
+        L.msa_latent_attn_backward_workspace_size.argtypes = [S, I]
+        L.msa_latent_attn_backward_workspace_size.restype = Z
+        L.msa_latent_attn_backward.argtypes = [P, N, N, P, N, N, P, P, N, P, P, P, S, I, F, P, N, N, P, N, N, P, P, N, P, Z, P]
+        L.msa_latent_attn_backward.restype = I
         L.msa_sparse_attn_backward_workspace_size.argtypes = [S, I, I, I, I, I]
         L.msa_sparse_attn_backward_workspace_size.restype = Z
         L.msa_sparse_attn_backward.argtypes = [P, P, P, P, P, P, P, S, I, I, I, I, I, F, P, P, P, P, Z, P]
@@ -850,6 +860,93 @@ def latent_attn_paged(q, q_rope, cache, seqs: Seqs, softmax_scale=None, out=None
 def latent_attn_paged_fp8(q, q_rope, cache, scale, seqs: Seqs, softmax_scale=None, out=None, lse=None, workspace=None):
     """The same on a cache of e4m3 codes (uint8) with a per-tensor scale; queries stay bf16."""
     return _latent_paged(float(scale), q, q_rope, cache, seqs, softmax_scale, out, lse, workspace)
+
+
+def latent_attn_workspace_size(seqs: Seqs, num_heads: int) -> int:
+    return int(lib().msa_latent_attn_workspace_size(seqs.ref(), num_heads))
+
+
+def latent_attn(q, q_rope, kv, k_rope, seqs: Seqs, softmax_scale=None, out=None, lse=None, workspace=None):
+    """Latent attention, expanded form: (O bf16 [Tq, H, 128], LSE fp32 [Tq, H]) of q [Tq, H, 128] and q_rope [Tq, H, 64], both
+    with any row and head strides, over kv [Tkv, H, 256] (a head's own key part, then its values) and the shared
+    k_rope [Tkv, 64], whose rows may be columns of a wider tensor."""
+    dev, T = seqs.device, seqs.total_q_rows
+    if q.dim() != 3:
+        raise ValueError(f"q: expected shape ({T}, heads, {LATENT_HEAD_DIM}), got {tuple(q.shape)}")
+    H = q.shape[1]
+    qs, qh = _strided(q, "q", (T, H, LATENT_HEAD_DIM), dev)
+    es, eh = _strided(q_rope, "q_rope", (T, H, LATENT_ROPE_DIM), dev)
+    _need(kv, "kv", torch.bfloat16, (seqs.total_kv_rows, H, 2 * LATENT_HEAD_DIM), dev)
+    ks = _rows(k_rope, "k_rope", seqs.total_kv_rows, LATENT_ROPE_DIM, dev)
+    _need_workspace(workspace, dev)
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return latent_attn(q, q_rope, kv, k_rope, seqs, softmax_scale, out, lse, workspace)
+    if out is None:
+        out = torch.empty(T, H, LATENT_HEAD_DIM, dtype=torch.bfloat16, device=dev)
+    else:
+        _need(out, "o", torch.bfloat16, (T, H, LATENT_HEAD_DIM), dev)
+    if lse is None:
+        lse = torch.empty(T, H, dtype=torch.float32, device=dev)
+    else:
+        _need(lse, "lse", torch.float32, (T, H), dev)
+    L, ref = lib(), seqs.ref()
+    if workspace is None:
+        workspace = _workspace(L.msa_latent_attn_workspace_size(ref, H), dev, None)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    st = L.msa_latent_attn(q.data_ptr(), qs, qh, q_rope.data_ptr(), es, eh, kv.data_ptr(), k_rope.data_ptr(), ks, ref, H,
+                           _latent_scale(softmax_scale), out.data_ptr(), lse.data_ptr(), ws, ws_bytes, _raw_stream(dev))
+    _check(st, "msa_latent_attn")
+    return out, lse
+
+
+def latent_attn_backward_workspace_size(seqs: Seqs, num_heads: int) -> int:
+    return int(lib().msa_latent_attn_backward_workspace_size(seqs.ref(), num_heads))
+
+
+def latent_attn_backward(q, q_rope, kv, k_rope, o, lse, d_o, seqs: Seqs, softmax_scale=None, d_q=None, d_q_rope=None, d_kv=None,
+                         d_k_rope=None, workspace=None):
+    """Gradients of latent_attn for the upstream gradient d_o, given its inputs and outputs: (d_q, d_q_rope, d_kv, d_k_rope), the
+    last summed over the heads; d_q, d_q_rope and d_k_rope may be columns of wider tensors."""
+    dev, T, N = seqs.device, seqs.total_q_rows, seqs.total_kv_rows
+    if q.dim() != 3:
+        raise ValueError(f"q: expected shape ({T}, heads, {LATENT_HEAD_DIM}), got {tuple(q.shape)}")
+    H = q.shape[1]
+    qs, qh = _strided(q, "q", (T, H, LATENT_HEAD_DIM), dev)
+    es, eh = _strided(q_rope, "q_rope", (T, H, LATENT_ROPE_DIM), dev)
+    _need(kv, "kv", torch.bfloat16, (N, H, 2 * LATENT_HEAD_DIM), dev)
+    ks = _rows(k_rope, "k_rope", N, LATENT_ROPE_DIM, dev)
+    _need(o, "o", torch.bfloat16, (T, H, LATENT_HEAD_DIM), dev)
+    _need(lse, "lse", torch.float32, (T, H), dev)
+    _need(d_o, "d_o", torch.bfloat16, (T, H, LATENT_HEAD_DIM), dev)
+    _need_workspace(workspace, dev)
+    if not _current(dev):
+        with torch.cuda.device(dev):
+            return latent_attn_backward(q, q_rope, kv, k_rope, o, lse, d_o, seqs, softmax_scale, d_q, d_q_rope, d_kv, d_k_rope,
+                                        workspace)
+    if d_q is None:
+        d_q = torch.empty(T, H, LATENT_HEAD_DIM, dtype=torch.bfloat16, device=dev)
+    dqs, dqh = _strided(d_q, "d_q", (T, H, LATENT_HEAD_DIM), dev)
+    if d_q_rope is None:
+        d_q_rope = torch.empty(T, H, LATENT_ROPE_DIM, dtype=torch.bfloat16, device=dev)
+    des, deh = _strided(d_q_rope, "d_q_rope", (T, H, LATENT_ROPE_DIM), dev)
+    if d_kv is None:
+        d_kv = torch.empty(N, H, 2 * LATENT_HEAD_DIM, dtype=torch.bfloat16, device=dev)
+    else:
+        _need(d_kv, "d_kv", torch.bfloat16, (N, H, 2 * LATENT_HEAD_DIM), dev)
+    if d_k_rope is None:
+        d_k_rope = torch.empty(N, LATENT_ROPE_DIM, dtype=torch.bfloat16, device=dev)
+    dks = _rows(d_k_rope, "d_k_rope", N, LATENT_ROPE_DIM, dev)
+    L, ref = lib(), seqs.ref()
+    if workspace is None:
+        workspace = _workspace(L.msa_latent_attn_backward_workspace_size(ref, H), dev, None)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    st = L.msa_latent_attn_backward(
+        q.data_ptr(), qs, qh, q_rope.data_ptr(), es, eh, kv.data_ptr(), k_rope.data_ptr(), ks, o.data_ptr(), lse.data_ptr(),
+        d_o.data_ptr(), ref, H, _latent_scale(softmax_scale), d_q.data_ptr(), dqs, dqh, d_q_rope.data_ptr(), des, deh,
+        d_kv.data_ptr(), d_k_rope.data_ptr(), dks, ws, ws_bytes, _raw_stream(dev))
+    _check(st, "msa_latent_attn_backward")
+    return d_q, d_q_rope, d_kv, d_k_rope
 
 
 # ---------------------------------------------------------------- kernel timing

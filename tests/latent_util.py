@@ -85,3 +85,52 @@ class PagedBatch:
         ref, l_ref, size = self.reference(rows, **kw)
         check_o(host(o)[rows], ref, size, what)
         check_lse(host(lse)[rows], l_ref, what)
+
+
+class ExpandedBatch:
+    """Queries, per-head keys and values with NaN in the rows that no sequence owns, the shared key part as columns of a
+    wider tensor, and the layout."""
+
+    def __init__(self, name, q_rows, kv_lens, H, pad=0, gap=3):
+        rng = self.rng = np.random.default_rng(sum(map(ord, name)))
+        T = sum(q_rows) + pad
+        starts = (gap + np.cumsum([0] + [m + gap for m in kv_lens])[:-1]).tolist()
+        N = self.N = starts[-1] + kv_lens[-1] + gap
+        self.n, self.H = sum(q_rows), H
+        self.q, self.q_rope = bf16(rng.standard_normal((T, H, 128))), bf16(rng.standard_normal((T, H, ROT)))
+        self.kv, self.k_rope = bf16(rng.standard_normal((N, H, 256))), bf16(rng.standard_normal((N, ROT)))
+        self.lay = O.Layout(q_rows, kv_lens, starts)
+        self.owned = np.zeros(N, dtype=bool)
+        for s, m in zip(starts, kv_lens):
+            self.owned[s:s + m] = True
+        kv, k_rope = self.kv.copy(), self.k_rope.copy()
+        kv[~self.owned] = np.nan
+        k_rope[~self.owned] = np.nan
+        joint = torch.zeros((T, H * (128 + ROT) + 8), dtype=torch.bfloat16, device="cuda")   # a query projection's rows
+        self.dq, self.dq_rope = joint[:, :H * 128].view(T, H, 128), joint[:, H * 128:H * (128 + ROT)].view(T, H, ROT)
+        self.dq.copy_(dev(self.q))
+        self.dq_rope.copy_(dev(self.q_rope))
+        wide = torch.zeros((N, 40 + ROT), dtype=torch.bfloat16, device="cuda")
+        self.dkv, self.dk_rope = dev(kv), wide[:, 40:]
+        self.dk_rope.copy_(dev(k_rope))
+        self.seqs = padded_seqs(q_rows, kv_lens, pad, kv_starts=starts, total_kv=N)
+
+    def reference(self, rows=None, scale=SCALE, lay=None):
+        return O.latent_attention(self.q, self.q_rope, self.kv[..., :128], self.k_rope, self.kv[..., 128:], lay or self.lay, scale,
+                                  rows)
+
+    def check(self, o, lse, rows, what, **kw):
+        ref, l_ref, size = self.reference(rows, **kw)
+        check_o(host(o)[rows], ref, size, what)
+        check_lse(host(lse)[rows], l_ref, what)
+
+
+def check_grad(got, ref, size, what, terms=1.0):
+    """A gradient in bf16: every term's factor (P or dS) carries the score's error (2 LSE_TOL of the weight), dS the error
+    of its difference (fp32 sums of 128 exact products: 2^-18 of their sizes), and one rounding to bf16; the fp32
+    sums add less than 2^-12 of the sum of sizes (4096 roundings); one rounding of the result.  ``size`` is the
+    sum of the terms' sizes."""
+    inner = (BF16_HALF + 2 * LSE_TOL + 2.0 ** -18 + 2.0 ** -12) * size * terms
+    tol = inner + BF16_HALF * (np.abs(ref) + inner)
+    err = np.abs(got - ref)
+    assert (err <= tol).all(), f"{what}: {(err > tol).sum()} values off, worst {(err / np.maximum(tol, 1e-300)).max():.2f} tolerances"
