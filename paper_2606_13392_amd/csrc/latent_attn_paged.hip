@@ -46,7 +46,9 @@ constexpr int kRows = 64;                // (row, head) pairs per tile
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kCtas = 256;               // one per CU: two buffers of keys fill its LDS
+constexpr int kMergeCtas = 1024;
 constexpr int kMinSteps = 4;             // steps per CTA, where there are few
+constexpr float kSlack = 8.f;
 constexpr int kAheadK = 6, kAheadV = 3;  // LDS operands requested so many products ahead
 
 // A cache row in LDS: 16-byte segments, the low three bits of their number
@@ -69,7 +71,7 @@ struct LatentPlan {
 struct LatentParts {
   float* o;                              // [CTA][2][64 rows x R, in the accumulators' order], normalised
   float* lse;                            // [CTA][2][64], base 2
-  int4* tile;                            // [CTA]: the tile in slot 1: sequence, tile, parts (0: none)
+  int4* tile;                            // [CTA]: the tile in slot 1: first query row, (row, head) pairs, parts (0: none)
 };
 
 // T: cache elements, uint16_t = bf16 bits, uint8_t = E4M3 codes (o_scale
@@ -170,56 +172,69 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       cur = fetch(w0 + lane);
       nxt = fetch(w0 + kWave + lane);
     }
-    u32x4 raw[kCodes ? NC : 1];
-    // Keys of step i: bf16 into buffer `buf` by copies of 1 KiB; codes into registers.
+    // Keys of a step: bf16 into a buffer by copies of 1 KiB; codes into registers, and from there widened.
     // Piece c * 64 + lane of the wave's 16 rows is 16 bytes; by copy it lands at its own
     // number, so it is the segment that the row's permutation stores there.  (Rows are a
     // multiple of 8 segments, so the permutation is one of the piece's low three bits.)
-    // Keys past the sequence's end repeat its last one: what memory holds there may be NaN.
-    auto get = [&](int i, int buf) {
-      const int64_t row = place(i);
-      const char* src = reinterpret_cast<const char*>(cache) + row * (W * static_cast<int64_t>(sizeof(T)));
-      const int key0 = i * kKeys + 16 * wave;
-      const uint32_t dst = lds_keys + buf * kBuf + 16 * wave * kRowBytes;
-      int piece = lane;
-      asm volatile("" : "+v"(piece));        // offsets are formed here each time: held, they spill
-      if (key0 + kGroup <= g.kv_len) {
-        if constexpr (kCodes) {
-#pragma unroll
-          for (int c = 0; c < NC; ++c) raw[c] = *reinterpret_cast<const u32x4*>(src + 16 * piece + c * 1024);
-        } else {
-          uint64_t mixes = piece_mixes;
-          asm volatile("" : "+v"(mixes));
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-            copy16(src, 16 * ((c * kWave + piece) ^ (static_cast<uint32_t>(mixes >> (3 * c)) & 7)), dst + c * 1024);
-        }
-      } else {
-        const int rem = g.kv_len - 1 - min(key0, last_group);     // last row of the group that may be read
+    // Offsets are formed anew each time: held, they spill.
+    u32x4 raw[kCodes ? NC : 1];
+    auto source = [&](int i) { return reinterpret_cast<const char*>(cache) + place(i) * (W * static_cast<int64_t>(sizeof(T))); };
+    auto full = [&](int i) { return i * kKeys + 16 * wave + kGroup <= g.kv_len; };
+    auto get = [&](const char* src, int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
+      if constexpr (kCodes)
+        raw[c] = *reinterpret_cast<const u32x4*>(src + 16 * piece + c * 1024);
+      else
+        copy16(src, 16 * ((c * kWave + piece) ^ (static_cast<uint32_t>(mixes >> (3 * c)) & 7)),
+               lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024);
+    };
+    // the last step's: keys past the sequence's end repeat its last one (what memory holds there may be NaN)
+    auto get_last = [&](int i, int buf) {
+      const char* src = source(i);
+      const int rem = g.kv_len - 1 - min(i * kKeys + 16 * wave, last_group);      // last row of the group that may be read
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+      auto offset = [&](int c, int* sg, int* r) {
+        *r = (c * kWave + ln) / kSrcSegs;
+        *sg = (c * kWave + ln) - *r * kSrcSegs;
+        return static_cast<uint32_t>(min(*r, rem) * static_cast<int>(W * sizeof(T)));
+      };
+      int sg, r;
+      if constexpr (kCodes) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const int r = (c * kWave + piece) / kSrcSegs, sg = (c * kWave + piece) % kSrcSegs;
-          const uint32_t off = min(r, rem) * (W * sizeof(T));
-          if constexpr (kCodes) raw[c] = *reinterpret_cast<const u32x4*>(src + off + 16 * sg);
-          else copy16(src, off + 16 * (sg ^ row_mix(r)), dst + c * 1024);
+          const uint32_t off = offset(c, &sg, &r);
+          raw[c] = *reinterpret_cast<const u32x4*>(src + off + 16 * sg);
+        }
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < NC; ++c) {
+          const uint32_t off = offset(c, &sg, &r);
+          copy16(src, off + 16 * (sg ^ row_mix(r)),
+                 __builtin_amdgcn_readfirstlane(lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024));
         }
       }
     };
-    auto put = [&](int buf) {                // codes, widened
+    auto get_all = [&](int i, int buf) {
+      if (!full(i)) {
+        get_last(i, buf);
+        return;
+      }
+      const char* src = source(i);
+      int piece = lane;
+      uint64_t mixes = piece_mixes;
+      asm volatile("" : "+v"(piece), "+v"(mixes));
+#pragma unroll
+      for (int c = 0; c < NC; ++c) get(src, buf, c, piece, mixes);
+    };
+    auto put = [&](int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
       if constexpr (kCodes) {
         char* dst = reinterpret_cast<char*>(keys[buf]) + 16 * wave * kRowBytes;
-        int piece = lane;
-        asm volatile("" : "+v"(piece));
-        uint64_t mixes = piece_mixes;
-        asm volatile("" : "+v"(mixes));
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int d = 2 * (c * kWave + piece) + b;
-            *reinterpret_cast<u32x4*>(dst + 16 * (d ^ (static_cast<int>(mixes >> (3 * c)) & 7))) =
-                widen(u32x2{raw[c][2 * b], raw[c][2 * b + 1]});
-          }
+        // which half goes first differs between lanes, so that 8 and 16 lanes' stores fall on all banks
+        const bool hi = ((piece >> 2) ^ (piece >> 3)) & 1;
+        const u32x2 a{raw[c][0], raw[c][1]}, b{raw[c][2], raw[c][3]};
+        const int mix = static_cast<int>(mixes >> (3 * c)) & 7, d = 2 * (c * kWave + piece);
+        *reinterpret_cast<u32x4*>(dst + 16 * ((d + hi) ^ mix)) = widen(hi ? b : a);
+        *reinterpret_cast<u32x4*>(dst + 16 * ((d + !hi) ^ mix)) = widen(hi ? a : b);
       }
     };
 
@@ -235,6 +250,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         u32x4 v = *reinterpret_cast<const u32x4*>(st < R / 16 ? qp + 16 * st : ep + 16 * (st - R / 16));
         if (mine >= pairs) v = u32x4{};
         bq[st] = __builtin_bit_cast(bf16x8, v ^ q_flip);
+        asm volatile("" : "+v"(bq[st]));     // the accumulation registers are for the sums
       }
     }
     f32x16 acc[TD][2];
@@ -243,22 +259,36 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
     float m_run[2] = {-INFINITY, -INFINITY}, l_run = 0.f;
 
     if (b_begin < b_end) {
-      get(b_begin, 0);
+      get_all(b_begin, 0);
       if constexpr (kCodes) {
-        put(0);
-        if (b_begin + 1 < b_end) get(b_begin + 1, 1);
-      } else {
-        if (b_begin + 1 < b_end) get(b_begin + 1, 1);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) put(0, c, lane, piece_mixes);
+        if (b_begin + 1 < b_end) get_all(b_begin + 1, 1);
       }
     }
+    // Step i: its keys are in buffer i - b_begin (mod 2).  bf16: the copies of step i + 1 go out
+    // between the score products, one by one (issued together they hold up the
+    // wave for as long as the products take).  Codes: those of step i + 1, in registers, are
+    // stored between the value products, and those of i + 2 requested.
     for (int i = b_begin; i < b_end; ++i) {
       const int buf = (i - b_begin) & 1;
       const char* kb = reinterpret_cast<const char*>(keys[buf]);
-      if constexpr (!kCodes) {               // the copies of step i have landed, those of i + 1 are under way
-        if (i + 1 < b_end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NC) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
+      int piece = lane;
+      uint64_t mixes = piece_mixes;
+      asm volatile("" : "+v"(piece), "+v"(mixes));
+      // everyone's keys of step i are in place, and the readers of step i - 1's are done
+      if constexpr (!kCodes) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      const int ahead = kCodes ? i + 2 : i + 1;
+      bool more = ahead < b_end;
+      const char* next = nullptr;
+      if constexpr (!kCodes) {
+        if (more && !full(ahead)) {
+          get_last(ahead, buf ^ 1);
+          more = false;
+        }
+        if (more) next = source(ahead);
+      }
       f32x16 sc = {};
       {
         // fenced slots: LDS operands are requested kAheadK products before their use
@@ -272,6 +302,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         for (int st = 0; st < KS; ++st) {
           if (st + kAheadK < KS) kr[st + kAheadK] = kread(st + kAheadK);
           sc = mfma32x32x16(kr[st], bq[st], sc);
+          if constexpr (!kCodes)
+            if (st % 2 == 1 && st / 2 < NC && more) get(next, buf ^ 1, st / 2, piece, mixes);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -288,14 +320,18 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       top = fmaxf(top, xor32f(top));
       if (h == 0) tops[kh][mine] = top;
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      float alpha[2], neg[2];
+      // The maxima that the weights are relative to move only when one is outgrown by 2^kSlack: among 64 rows
+      // some true maximum moves in most steps, and each time O would be rescaled (384 instructions a wave at
+      // R = 512).  Weights stay below 2^kSlack, exact powers of two apart from the usual ones.
+      float alpha[2] = {1.f, 1.f}, neg[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float m_new = fmaxf(m_run[j], fmaxf(tops[0][32 * j + n], tops[1][32 * j + n]));
-        const float mm = m_new == -INFINITY ? 0.f : m_new;        // rows with nothing visible yet
-        alpha[j] = exp2_hw((m_run[j] - mm) * scale_log2);
-        neg[j] = -mm * scale_log2;
-        m_run[j] = m_new;
+        const float m_new = fmaxf(tops[0][32 * j + n], tops[1][32 * j + n]);
+        if ((m_new - m_run[j]) * scale_log2 > kSlack) {           // the first visible keys among them: m_run is -inf
+          alpha[j] = exp2_hw((m_run[j] - m_new) * scale_log2);
+          m_run[j] = m_new;
+        }
+        neg[j] = m_run[j] == -INFINITY ? 0.f : -m_run[j] * scale_log2;   // rows with nothing visible yet
       }
       const float my_neg = rh ? neg[1] : neg[0];
       float sum = 0.f;
@@ -316,11 +352,18 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         *reinterpret_cast<uint4*>(weights + mine * kKeys + 8 * p_seg(mine, 2 * (2 * kh + b) + h)) = w;
       }
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      // (the pins keep O in accumulation registers on the way around, else it is moved in every step)
+      auto pin = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int td = 0; td < TD; ++td) asm volatile("" : "+a"(acc[td][0]), "+a"(acc[td][1]));
+      };
+      pin();
       if (__ballot(alpha[0] != 1.f || alpha[1] != 1.f)) {
 #pragma unroll
         for (int td = 0; td < TD; ++td)
 #pragma unroll
           for (int j = 0; j < 2; ++j) acc[td][j] *= alpha[j];
+        pin();
       }
       {
         constexpr int NU = kKeys / 16, NO = NU * TD;
@@ -340,6 +383,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         pread(0);
 #pragma unroll
         for (int k = 0; k < kAheadV; ++k) vr[k] = vread(k);
+        if constexpr (kCodes)
+          if (more && full(ahead)) next = source(ahead);
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
           const int us = k / TD, td = k % TD;
@@ -347,20 +392,20 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
           if (k + kAheadV < NO) vr[k + kAheadV] = vread(k + kAheadV);
 #pragma unroll
           for (int j = 0; j < 2; ++j) acc[td][j] = mfma32x32x16(vr[k], bp[us][j], acc[td][j]);
+          if constexpr (kCodes) {
+            const int c = k - 1;             // NC < NO
+            if (c >= 0 && c < NC && i + 1 < b_end) {
+              put(buf ^ 1, c, piece, mixes);   // whose readers are behind this step's first barrier
+              if (next) get(next, buf, c, piece, mixes);
+            }
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
-      }
-      if constexpr (kCodes) {
-        if (i + 1 < b_end) {
-          put(buf ^ 1);                      // its readers are behind the last barrier of step i - 1
-          if (i + 2 < b_end) get(i + 2, buf);
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      } else {
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the buffer's readers are done
-        if (i + 2 < b_end) get(i + 2, buf);
+        if constexpr (kCodes)
+          if (more && !next) get_last(ahead, buf);
       }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the buffers' readers are done
 
     // ------------------------------------------------ the tile's rows, or the share's part of them
     l_run += xor32f(l_run);
@@ -411,69 +456,127 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         if (wave == 0 && h == 0) parts.lse[slot * kRows + 32 * j + n] = lse2[j];
       }
       if (b_begin == 0 && threadIdx.x == 0)
-        parts.tile[cta] = make_int4(sh.s, sh.x, sh.parts(visits), 0);
+        parts.tile[cta] = make_int4(g.q_begin + t0, pairs, sh.parts(visits), 0);
     }
   }
 }
 
 // Joins the parts of a tile that several shares had: a = max LSE_c,
-// LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c, in key order.  Four
-// dimensions of a row per thread, in the order of the parts.
+// LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c.  A CTA forms the
+// list of such tiles and takes every gridDim.x-th share of them.  Of many tiles a
+// wave joins the parts of a piece, 4 dimensions of 32 rows in each half of it; of
+// few the CTA's four waves have every fourth part, in order, and join in LDS.  (A
+// CTA per share and piece, most of them without a tile, took 16 us for one token
+// on 8209 keys, this 5.)
+constexpr int kManyTiles = 16;
 template <int R>
-__global__ __launch_bounds__(256) void latent_merge_kernel(msa_seqs sq, LatentPlan pl, LatentParts parts, int H,
-                                                           uint16_t* __restrict__ o, float* __restrict__ lse) {
-  constexpr int TD = R / 128;
-  const int cta = static_cast<int>(blockIdx.x);
-  const int4 what = parts.tile[cta];
-  const int np = what.z;
-  if (np < 1) return;
-  const int block = cta % pl.blocks;
-  const int unit = blockIdx.y * 256 + threadIdx.x;
-  const int lane = unit & 63, rest = unit >> 6;
-  const int e4 = rest & 3, j = (rest >> 2) & 1, td = (rest >> 3) % TD, wave = (rest >> 3) / TD;
-  const int r = 32 * j + (lane & 31);
-  const TileGeom g = tile_geom(sq, what.x);
-  const int t0 = what.y * pl.rows, t_end = min(t0 + pl.rows, g.q_rows);
-  const int tile_heads = min(pl.heads, H - block * pl.heads);
-  if (r >= (t_end - t0) * tile_heads) return;
-  auto slot = [&](int c) { return 2 * (cta + static_cast<int64_t>(c) * pl.blocks) + (c == 0 ? 1 : 0); };
-  constexpr int kBatch = 8;
-  float top = -INFINITY, sum = 0.f;
-  f32x4 y{};
-  for (int c0 = 0; c0 < np; c0 += kBatch) {
-    float l[kBatch];
-    f32x4 v[kBatch];
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const int64_t at = slot(min(c0 + b, np - 1));
-      l[b] = parts.lse[at * kRows + r];
-      v[b] = reinterpret_cast<const f32x4*>(parts.o + at * kRows * R)[unit];
-    }
-    float m = top;
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      l[b] = c0 + b < np ? l[b] : -INFINITY;
-      m = fmaxf(m, l[b]);
-    }
-    const float base = m > -INFINITY ? m : 0.f;            // every part empty: all weights are zero
-    const float f = exp2_hw(top - base);
-    top = m;
-    sum *= f;
-    y *= f;
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const float w = exp2_hw(l[b] - base);
-      sum += w;
-      y += v[b] * w;
-    }
+__global__ __launch_bounds__(kThreads) void latent_merge_kernel(msa_seqs sq, LatentPlan pl, LatentParts parts, int H,
+                                                                uint16_t* __restrict__ o, float* __restrict__ lse) {
+  constexpr int TD = R / 128, kPieces = kRows * R / 4 / kWave;
+  __shared__ int16_t list[kCtas];
+  __shared__ int count[kWaves];
+  __shared__ f32x4 side_o[kWaves][kWave];
+  __shared__ float2 side_l[kWaves][kWave];
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int ctas = pl.ranges * pl.blocks;  // at most kCtas = kThreads
+  const bool has = static_cast<int>(threadIdx.x) < ctas && parts.tile[threadIdx.x].z > 0;
+  const uint64_t mask = __ballot(has);
+  if (lane == 0) count[wave] = __popcll(mask);
+  __syncthreads();
+  int before = 0, tiles = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += count[w];
+    tiles += count[w];
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  const int64_t head_row = (static_cast<int64_t>(g.q_begin) + t0 + r / tile_heads) * H + block * pl.heads + r % tile_heads;
-  uint2 w;
-  w.x = pack_bf16x2(y[0] * inv, y[1] * inv);
-  w.y = pack_bf16x2(y[2] * inv, y[3] * inv);
-  *reinterpret_cast<uint2*>(o + head_row * R + wave * (R / 4) + 32 * td + 8 * e4 + 4 * (lane >> 5)) = w;
-  if ((rest & ~4) == 0 && (lane >> 5) == 0) lse[head_row] = sum > 0.f ? (top + __log2f(sum)) * kLn_2 : -INFINITY;
+  if (has) list[before + __popcll(mask & ((1ull << lane) - 1))] = static_cast<int16_t>(threadIdx.x);
+  __syncthreads();
+  // parts c0, c0 + step, ... of a piece, joined
+  auto join = [&](int cta, int np, int piece, int r, int c0, int step, float& top, float& sum, f32x4& y) {
+    constexpr int kBatch = 8;
+    for (; c0 < np; c0 += step * kBatch) {
+      float l[kBatch];
+      f32x4 v[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int c = c0 + step * b;
+        l[b] = -INFINITY;
+        v[b] = f32x4{};
+        if (c < np) {
+          const int64_t at = 2 * (cta + static_cast<int64_t>(c) * pl.blocks) + (c == 0 ? 1 : 0);
+          l[b] = parts.lse[at * kRows + r];
+          v[b] = reinterpret_cast<const f32x4*>(parts.o + at * kRows * R)[piece * kWave + lane];
+        }
+      }
+      float m = top;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) m = fmaxf(m, l[b]);
+      const float base = m > -INFINITY ? m : 0.f;          // every part empty: all weights are zero
+      const float f = exp2_hw(top - base);
+      top = m;
+      sum *= f;
+      y *= f;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const float w = exp2_hw(l[b] - base);
+        sum += w;
+        y += v[b] * w;
+      }
+    }
+  };
+  auto write = [&](const int4& what, int block, int piece, float top, float sum, const f32x4& y) {
+    const int e4 = piece & 3, j = (piece >> 2) & 1, td = (piece >> 3) % TD, quarter = (piece >> 3) / TD;
+    const int r = 32 * j + (lane & 31);
+    const int tile_heads = min(pl.heads, H - block * pl.heads);
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const int64_t head_row = (static_cast<int64_t>(what.x) + r / tile_heads) * H + block * pl.heads + r % tile_heads;
+    uint2 w;
+    w.x = pack_bf16x2(y[0] * inv, y[1] * inv);
+    w.y = pack_bf16x2(y[2] * inv, y[3] * inv);
+    *reinterpret_cast<uint2*>(o + head_row * R + quarter * (R / 4) + 32 * td + 8 * e4 + 4 * (lane >> 5)) = w;
+    if ((piece & ~4) == 0 && lane < 32) lse[head_row] = sum > 0.f ? (top + __log2f(sum)) * kLn_2 : -INFINITY;
+  };
+  const bool many = tiles >= kManyTiles;
+  const int steps = many ? tiles * (kPieces / kWaves) : tiles * kPieces;
+  for (int i = blockIdx.x; i < steps; i += gridDim.x) {
+    const int n = many ? i * kWaves + wave : i;
+    const int cta = list[n / kPieces], piece = n % kPieces;
+    const int4 what = parts.tile[cta];
+    const int r = 32 * ((piece >> 2) & 1) + (lane & 31);
+    const bool mine = r < what.y;          // rows behind the tile's have no parts
+    float top = -INFINITY, sum = 0.f;
+    f32x4 y{};
+    if (many) {                            // a wave has a piece
+      if (!mine) continue;
+      join(cta, what.z, piece, r, 0, 1, top, sum, y);
+      write(what, cta % pl.blocks, piece, top, sum, y);
+      continue;
+    }
+    if (mine) join(cta, what.z, piece, r, wave, kWaves, top, sum, y);
+    side_o[wave][lane] = y;
+    side_l[wave][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (wave == 0 && mine) {
+      float2 l[kWaves];
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        l[w] = side_l[w][lane];
+        m = fmaxf(m, l[w].x);
+      }
+      const float base = m > -INFINITY ? m : 0.f;
+      sum = 0.f;
+      y = f32x4{};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2_hw(l[w].x - base);
+        sum = fmaf(l[w].y, f, sum);
+        y += side_o[w][lane] * f;
+      }
+      write(what, cta % pl.blocks, piece, m, sum, y);
+    }
+    __syncthreads();                       // the side areas are free again
+  }
 }
 
 // ---------------------------------------------------------------- host side
@@ -534,7 +637,7 @@ int latent_paged(const void* q, int64_t q_stride, int64_t q_head, const void* e,
                      static_cast<const uint16_t*>(q), q_stride, q_head, static_cast<const uint16_t*>(e), e_stride, e_head,
                      static_cast<const T*>(cache), *seqs, pl, parts, H, scale.log2, scale.q_flip, cache_scale,
                      static_cast<uint16_t*>(o), lse);
-    msa_prof::launch("latent_merge_kernel", latent_merge_kernel<RR>, dim3(ctas, kRows * RR / 4 / 256), dim3(256), 0, stream,
+    msa_prof::launch("latent_merge_kernel", latent_merge_kernel<RR>, dim3(kMergeCtas), dim3(kThreads), 0, stream,
                      *seqs, pl, parts, H, static_cast<uint16_t*>(o), lse);
   };
   using R256 = std::integral_constant<int, 256>;
