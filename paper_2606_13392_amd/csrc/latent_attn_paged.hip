@@ -91,6 +91,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
   constexpr int kGroup = 16;               // a wave copies 16 keys of a step: never across a page's end
   constexpr int kSrcSegs = W * sizeof(T) / 16;
   constexpr int NC = kGroup * kSrcSegs / kWave;      // 16-byte pieces per lane and step
+  constexpr int kEarly = (NC + 2) / 2;     // bf16: copies among the score products, the others among the value products
   static_assert(kGroup * kSrcSegs % kWave == 0, "");
   __shared__ __align__(16) uint16_t keys[2][kKeys * W];
   __shared__ __align__(16) uint16_t weights[kRows * kKeys];
@@ -109,6 +110,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
 
   // ------------------------------------------------ lane geometry
   const int tile_heads = min(pl.heads, H - block * pl.heads);     // of this block
+  const uint32_t heads_inv = (65536 + tile_heads - 1) / tile_heads;
+  auto per_row = [&](int r) { return static_cast<int>((static_cast<uint32_t>(r) * heads_inv) >> 16); };   // r / tile_heads, r < 64
   // K operand: row n of the wave's half, segment 2 st + h
   uint32_t k_at[4];
 #pragma unroll
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
 
     // this lane's row of the scores, and of the two row halves of O
     const int mine = 32 * rh + n;
-    const int my_t = t0 + min(mine, pairs - 1) / tile_heads;
+    const int my_t = t0 + per_row(min(mine, pairs - 1));
     const int p = mine < pairs ? base_p + my_t : -1;
 
     // places of the wave's 16-key groups of 64 steps, one per lane, and of the next 64
@@ -180,12 +183,20 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
     u32x4 raw[kCodes ? NC : 1];
     auto source = [&](int i) { return reinterpret_cast<const char*>(cache) + place(i) * (W * static_cast<int64_t>(sizeof(T))); };
     auto full = [&](int i) { return i * kKeys + 16 * wave + kGroup <= g.kv_len; };
+    // codes: through a buffer whose end is the sequence's, so that keys past it read as zeros; no step's
+    // requests hang on a branch (behind one, each store into LDS would wait for all of them)
+    auto codes_of = [&](int i, bool any) {
+      const int key0 = i * kKeys + 16 * wave;
+      const char* src = any ? source(i) : reinterpret_cast<const char*>(cache);
+      const int rows = any ? min(max(g.kv_len - key0, 0), kGroup) : 0;
+      return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, rows * static_cast<int>(W * sizeof(T)), 0x00020000);
+    };
+    auto get_codes = [&](auto from, int c, int piece) __attribute__((always_inline)) {
+      if constexpr (kCodes) raw[c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, 16 * piece, c * 1024, 0));
+    };
     auto get = [&](const char* src, int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
-      if constexpr (kCodes)
-        raw[c] = *reinterpret_cast<const u32x4*>(src + 16 * piece + c * 1024);
-      else
-        copy16(src, 16 * ((c * kWave + piece) ^ (static_cast<uint32_t>(mixes >> (3 * c)) & 7)),
-               lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024);
+      copy16(src, 16 * ((c * kWave + piece) ^ (static_cast<uint32_t>(mixes >> (3 * c)) & 7)),
+             lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024);
     };
     // the last step's: keys past the sequence's end repeat its last one (what memory holds there may be NaN)
     auto get_last = [&](int i, int buf) {
@@ -193,38 +204,29 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       const int rem = g.kv_len - 1 - min(i * kKeys + 16 * wave, last_group);      // last row of the group that may be read
       int ln = lane;
       asm volatile("" : "+v"(ln));
-      auto offset = [&](int c, int* sg, int* r) {
-        *r = (c * kWave + ln) / kSrcSegs;
-        *sg = (c * kWave + ln) - *r * kSrcSegs;
-        return static_cast<uint32_t>(min(*r, rem) * static_cast<int>(W * sizeof(T)));
-      };
-      int sg, r;
-      if constexpr (kCodes) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const uint32_t off = offset(c, &sg, &r);
-          raw[c] = *reinterpret_cast<const u32x4*>(src + off + 16 * sg);
-        }
-      } else {
 #pragma unroll 1
-        for (int c = 0; c < NC; ++c) {
-          const uint32_t off = offset(c, &sg, &r);
-          copy16(src, off + 16 * (sg ^ row_mix(r)),
-                 __builtin_amdgcn_readfirstlane(lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024));
-        }
+      for (int c = 0; c < NC; ++c) {
+        const int r = (c * kWave + ln) / kSrcSegs, sg = (c * kWave + ln) - r * kSrcSegs;
+        const uint32_t off = min(r, rem) * static_cast<int>(W * sizeof(T));
+        copy16(src, off + 16 * (sg ^ row_mix(r)),
+               __builtin_amdgcn_readfirstlane(lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024));
       }
     };
     auto get_all = [&](int i, int buf) {
-      if (!full(i)) {
-        get_last(i, buf);
-        return;
-      }
-      const char* src = source(i);
       int piece = lane;
       uint64_t mixes = piece_mixes;
       asm volatile("" : "+v"(piece), "+v"(mixes));
+      if constexpr (kCodes) {
+        const auto from = codes_of(i, true);
 #pragma unroll
-      for (int c = 0; c < NC; ++c) get(src, buf, c, piece, mixes);
+        for (int c = 0; c < NC; ++c) get_codes(from, c, piece);
+      } else if (!full(i)) {
+        get_last(i, buf);
+      } else {
+        const char* src = source(i);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) get(src, buf, c, piece, mixes);
+      }
     };
     auto put = [&](int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
       if constexpr (kCodes) {
@@ -238,38 +240,75 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       }
     };
 
-    // Q of the lane's row: k-step st holds elements 16 st + 8 h .. + 7
+    // Q of the tile's rows, through the second buffer: its own parts, 2 R bytes a row, segments in an order of the row
+    // that keeps the reads below free of bank conflicts, then the rotated ones as in a key.  Rows behind the tile's
+    // repeat its last.  (Straight from memory an operand's load touches 32 rows.)
+    constexpr int kOwnSegs = R / 8;
+    auto get_q = [&]() {
+      auto row_of = [&](int r, int64_t* hd) {
+        const int rr = min(r, pairs - 1), t = per_row(rr);
+        *hd = block * pl.heads + rr - t * tile_heads;
+        return static_cast<int64_t>(g.q_begin) + t0 + t;
+      };
+      int64_t hd;
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+#pragma unroll 1
+      for (int c = wave; c < kRows * kOwnSegs / kWave; c += kWaves) {
+        const int r = kOwnSegs == kWave ? c : 2 * c + (ln >> 5), sg = ln % kOwnSegs;
+        const int64_t row = row_of(r, &hd);
+        copy16(reinterpret_cast<const char*>(q + row * q_stride + hd * q_head + 8 * (sg ^ (r & 15))), lds_keys + kBuf + 1024 * c);
+      }
+#pragma unroll 1
+      for (int c = wave; c < kRows * kRot / 8 / kWave; c += kWaves) {
+        const int r = 8 * c + (ln >> 3), sg = ln & 7;
+        const int64_t row = row_of(r, &hd);
+        copy16(reinterpret_cast<const char*>(e + row * e_stride + hd * e_head + 8 * (sg ^ row_mix(r))),
+               lds_keys + kBuf + kRows * R * 2 + 1024 * c);
+      }
+    };
+    // k-step st holds elements 16 st + 8 h .. + 7 of the lane's row
     bf16x8 bq[KS];
-    {
-      const int hd = block * pl.heads + min(mine, pairs - 1) % tile_heads;
-      const int64_t row = g.q_begin + my_t;
-      const uint16_t* qp = q + row * q_stride + hd * q_head + 8 * h;
-      const uint16_t* ep = e + row * e_stride + hd * e_head + 8 * h;
+    auto read_q = [&]() {
+      int r = mine;
+      asm volatile("" : "+v"(r));
+      const uint16_t* own = keys[1] + r * R;
+      const uint16_t* rot = keys[1] + kRows * R + r * kRot;
+#pragma unroll
+      for (int st = 0; st < KS; ++st)
+        bq[st] = ld_bf16x8(st < R / 16 ? own + 8 * ((2 * st + h) ^ (r & 15)) : rot + 8 * ((2 * (st - R / 16) + h) ^ row_mix(r)));
+      if (q_flip != 0) {
+#pragma unroll
+        for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, bq[st]) ^ q_flip);
+      }
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        u32x4 v = *reinterpret_cast<const u32x4*>(st < R / 16 ? qp + 16 * st : ep + 16 * (st - R / 16));
-        if (mine >= pairs) v = u32x4{};
-        bq[st] = __builtin_bit_cast(bf16x8, v ^ q_flip);
-        asm volatile("" : "+v"(bq[st]));     // the accumulation registers are for the sums
+        // the accumulation registers are for the sums; with codes under way half of Q fits beside these
+        if (kCodes && st < KS / 2) asm volatile("" : "+a"(bq[st]));
+        else asm volatile("" : "+v"(bq[st]));
       }
-    }
+    };
     f32x16 acc[TD][2];
 #pragma unroll
     for (int i = 0; i < TD; ++i) acc[i][0] = acc[i][1] = f32x16{};
     float m_run[2] = {-INFINITY, -INFINITY}, l_run = 0.f;
 
     if (b_begin < b_end) {
+      get_q();
       get_all(b_begin, 0);
       if constexpr (kCodes) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) put(0, c, lane, piece_mixes);
         if (b_begin + 1 < b_end) get_all(b_begin + 1, 1);
       }
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCodes ? NC : 0) : "memory");
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      read_q();
     }
     // Step i: its keys are in buffer i - b_begin (mod 2).  bf16: the copies of step i + 1 go out
-    // between the score products, one by one (issued together they hold up the
-    // wave for as long as the products take).  Codes: those of step i + 1, in registers, are
-    // stored between the value products, and those of i + 2 requested.
+    // between the products of both kinds, one by one, so that requests are under
+    // way all the time.  Codes: those of step i + 1, in registers, are stored between the
+    // score products, and those of i + 2 requested.
     for (int i = b_begin; i < b_end; ++i) {
       const int buf = (i - b_begin) & 1;
       const char* kb = reinterpret_cast<const char*>(keys[buf]);
@@ -289,6 +328,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         }
         if (more) next = source(ahead);
       }
+      const auto codes = codes_of(ahead, kCodes && more);
       f32x16 sc = {};
       {
         // fenced slots: LDS operands are requested kAheadK products before their use
@@ -303,7 +343,12 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
           if (st + kAheadK < KS) kr[st + kAheadK] = kread(st + kAheadK);
           sc = mfma32x32x16(kr[st], bq[st], sc);
           if constexpr (!kCodes)
-            if (st % 2 == 1 && st / 2 < NC && more) get(next, buf ^ 1, st / 2, piece, mixes);
+            if (st % 3 == 1 && st / 3 < kEarly && more) get(next, buf ^ 1, st / 3, piece, mixes);
+          if constexpr (kCodes)
+            if (st % 4 == 1 && st / 4 < NC) {
+              put(buf ^ 1, st / 4, piece, mixes);     // behind the last step: a buffer that nobody reads
+              get_codes(codes, st / 4, piece);
+            }
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -383,8 +428,6 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         pread(0);
 #pragma unroll
         for (int k = 0; k < kAheadV; ++k) vr[k] = vread(k);
-        if constexpr (kCodes)
-          if (more && full(ahead)) next = source(ahead);
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
           const int us = k / TD, td = k % TD;
@@ -392,17 +435,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
           if (k + kAheadV < NO) vr[k + kAheadV] = vread(k + kAheadV);
 #pragma unroll
           for (int j = 0; j < 2; ++j) acc[td][j] = mfma32x32x16(vr[k], bp[us][j], acc[td][j]);
-          if constexpr (kCodes) {
-            const int c = k - 1;             // NC < NO
-            if (c >= 0 && c < NC && i + 1 < b_end) {
-              put(buf ^ 1, c, piece, mixes);   // whose readers are behind this step's first barrier
-              if (next) get(next, buf, c, piece, mixes);
-            }
-          }
+          if constexpr (!kCodes)
+            if (k % 2 == 0 && kEarly + k / 2 < NC && more) get(next, buf ^ 1, kEarly + k / 2, piece, mixes);
           __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (kCodes)
-          if (more && !next) get_last(ahead, buf);
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the buffers' readers are done
@@ -426,7 +462,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       for (int j = 0; j < 2; ++j) {
         const int r = 32 * j + n;
         if (r >= pairs) continue;
-        const int64_t head_row = (static_cast<int64_t>(g.q_begin) + t0 + r / tile_heads) * H + block * pl.heads + r % tile_heads;
+        const int64_t head_row = (static_cast<int64_t>(g.q_begin) + t0 + per_row(r)) * H + block * pl.heads + r - per_row(r) * tile_heads;
         uint16_t* orow = o + head_row * R + wave * (R / 4) + 4 * h;
 #pragma unroll
         for (int td = 0; td < TD; ++td)

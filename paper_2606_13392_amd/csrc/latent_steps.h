@@ -45,10 +45,21 @@ struct TileSteps {
     return (ahead + (x + 1) * rows + kKeys - 1) >> 6;
   }
   __device__ __forceinline__ int64_t of(int x) const { return x < tiles - 1 ? one(x) : last_steps; }
-  // of tiles 0 .. x - 1, x < tiles: one(y + 64) = one(y) + rows
-  __device__ __forceinline__ int64_t before(int x) const {
+  // of tiles 0 .. x - 1, x < tiles: the sum of floor((a + y rows) / 64), y < x
+  __device__ __forceinline__ int64_t before(int64_t x) const {
+    const int64_t a = ahead + rows + kKeys - 1;
+    if ((rows & (kKeys - 1)) == 0) return x * (a >> 6) + (rows >> 6) * (x * (x - 1) / 2);
+    if ((rows & (rows - 1)) == 0) {      // floor((a + y rows) / 64) = floor((floor(a / rows) + y) / m), m = 64 / rows
+      const int lg = 31 - __clz(rows), lm = 6 - lg;
+      auto below = [&](int64_t n) {      // the sum of floor(i / m), i < n
+        const int64_t q = n >> lm;
+        return ((q * (q - 1) / 2) << lm) + q * (n & ((1 << lm) - 1));
+      };
+      return below((a >> lg) + x) - below(a >> lg);
+    }
+    // one(y + 64) = one(y) + rows
     const int64_t q = x >> 6;
-    const int r = x & 63;
+    const int r = static_cast<int>(x & 63);
     int64_t part = 0, all = 0;
     for (int y = 0; y < (q > 0 ? 64 : r); ++y) {
       const int64_t c = one(y);
@@ -116,16 +127,18 @@ struct Share {
     g = tile_geom(sq, s);
     ts = TileSteps(g, rows);
     if (ts.tiles > 1) {
-      // as TileSteps::before, the sums within a period of 64 tiles one per lane
-      const int64_t incl = scan_incl(ts.one(lane_id()));
+      int lo = 0, hi = ts.tiles - 1;
+      const bool closed = (rows & (rows - 1)) == 0 || (rows & (kKeys - 1)) == 0;
+      // else as TileSteps::before, the sums within a period of 64 tiles one per lane
+      const int64_t incl = closed ? 0 : scan_incl(ts.one(lane_id()));
       const int64_t all = last_lane(incl);
       auto before = [&](int y) {
+        if (closed) return ts.before(y);
         const int64_t k = y >> 6;
         const int r = y & 63;
         const int64_t part = r > 0 ? static_cast<int64_t>(readlane_u64(static_cast<uint64_t>(incl), r - 1)) : 0;
         return k * all + 64 * rows * (k * (k - 1) / 2) + part + static_cast<int64_t>(r) * rows * k;
       };
-      int lo = 0, hi = ts.tiles - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (tile_first + before(mid) <= u) lo = mid; else hi = mid - 1;
