@@ -175,14 +175,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       cur = fetch(w0 + lane);
       nxt = fetch(w0 + kWave + lane);
     }
-    // Keys of a step: bf16 into a buffer by copies of 1 KiB; codes into registers, and from there widened.
+    // Keys of a step: bf16 into a buffer by copies of 1 KiB; codes into registers.
     // Piece c * 64 + lane of the wave's 16 rows is 16 bytes; by copy it lands at its own
     // number, so it is the segment that the row's permutation stores there.  (Rows are a
     // multiple of 8 segments, so the permutation is one of the piece's low three bits.)
     // Offsets are formed anew each time: held, they spill.
     u32x4 raw[kCodes ? NC : 1];
     auto source = [&](int i) { return reinterpret_cast<const char*>(cache) + place(i) * (W * static_cast<int64_t>(sizeof(T))); };
-    auto full = [&](int i) { return i * kKeys + 16 * wave + kGroup <= g.kv_len; };
     // codes: through a buffer whose end is the sequence's, so that keys past it read as zeros; no step's
     // requests hang on a branch (behind one, each store into LDS would wait for all of them)
     auto codes_of = [&](int i, bool any) {
@@ -194,23 +193,21 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
     auto get_codes = [&](auto from, int c, int piece) __attribute__((always_inline)) {
       if constexpr (kCodes) raw[c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, 16 * piece, c * 1024, 0));
     };
-    auto get = [&](const char* src, int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
-      copy16(src, 16 * ((c * kWave + piece) ^ (static_cast<uint32_t>(mixes >> (3 * c)) & 7)),
-             lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024);
+    // copies: pieces past the sequence's end repeat its last one (what memory holds there may be NaN), and behind the
+    // last step all repeat one; no copy hangs on a branch
+    struct Source {
+      const char* from;
+      uint32_t limit;                        // offset of the last piece that may be read
     };
-    // the last step's: keys past the sequence's end repeat its last one (what memory holds there may be NaN)
-    auto get_last = [&](int i, int buf) {
-      const char* src = source(i);
-      const int rem = g.kv_len - 1 - min(i * kKeys + 16 * wave, last_group);      // last row of the group that may be read
-      int ln = lane;
-      asm volatile("" : "+v"(ln));
-#pragma unroll 1
-      for (int c = 0; c < NC; ++c) {
-        const int r = (c * kWave + ln) / kSrcSegs, sg = (c * kWave + ln) - r * kSrcSegs;
-        const uint32_t off = min(r, rem) * static_cast<int>(W * sizeof(T));
-        copy16(src, off + 16 * (sg ^ row_mix(r)),
-               __builtin_amdgcn_readfirstlane(lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024));
-      }
+    auto keys_of = [&](int i) {
+      const int ii = min(i, b_end - 1);
+      const int rem = g.kv_len - 1 - min(ii * kKeys + 16 * wave, last_group);     // last row of the group that there is
+      const uint32_t limit = min(rem + 1, kGroup) * static_cast<int>(W * sizeof(T)) - 16;
+      return Source{source(ii), i < b_end ? limit : 0};
+    };
+    auto get = [&](const Source& src, int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
+      const uint32_t off = 16 * ((c * kWave + piece) ^ (static_cast<uint32_t>(mixes >> (3 * c)) & 7));
+      copy16(src.from, min(off, src.limit), lds_keys + buf * kBuf + 16 * wave * kRowBytes + c * 1024);
     };
     auto get_all = [&](int i, int buf) {
       int piece = lane;
@@ -220,10 +217,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         const auto from = codes_of(i, true);
 #pragma unroll
         for (int c = 0; c < NC; ++c) get_codes(from, c, piece);
-      } else if (!full(i)) {
-        get_last(i, buf);
       } else {
-        const char* src = source(i);
+        const Source src = keys_of(i);
 #pragma unroll
         for (int c = 0; c < NC; ++c) get(src, buf, c, piece, mixes);
       }
@@ -284,7 +279,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
         // the accumulation registers are for the sums; with codes under way half of Q fits beside these
-        if (kCodes && st < KS / 2) asm volatile("" : "+a"(bq[st]));
+        if (st < (kCodes ? KS / 2 : TD == 4 ? 10 : 0)) asm volatile("" : "+a"(bq[st]));
         else asm volatile("" : "+v"(bq[st]));
       }
     };
@@ -318,17 +313,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       // everyone's keys of step i are in place, and the readers of step i - 1's are done
       if constexpr (!kCodes) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      const int ahead = kCodes ? i + 2 : i + 1;
-      bool more = ahead < b_end;
-      const char* next = nullptr;
-      if constexpr (!kCodes) {
-        if (more && !full(ahead)) {
-          get_last(ahead, buf ^ 1);
-          more = false;
-        }
-        if (more) next = source(ahead);
-      }
-      const auto codes = codes_of(ahead, kCodes && more);
+      Source next{};
+      if constexpr (!kCodes) next = keys_of(i + 1);
+      const auto codes = codes_of(i + 2, kCodes && i + 2 < b_end);
       f32x16 sc = {};
       {
         // fenced slots: LDS operands are requested kAheadK products before their use
@@ -343,7 +330,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
           if (st + kAheadK < KS) kr[st + kAheadK] = kread(st + kAheadK);
           sc = mfma32x32x16(kr[st], bq[st], sc);
           if constexpr (!kCodes)
-            if (st % 3 == 1 && st / 3 < kEarly && more) get(next, buf ^ 1, st / 3, piece, mixes);
+            if (st % 3 == 1 && st / 3 < kEarly) get(next, buf ^ 1, st / 3, piece, mixes);
           if constexpr (kCodes)
             if (st % 4 == 1 && st / 4 < NC) {
               put(buf ^ 1, st / 4, piece, mixes);     // behind the last step: a buffer that nobody reads
@@ -436,7 +423,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
 #pragma unroll
           for (int j = 0; j < 2; ++j) acc[td][j] = mfma32x32x16(vr[k], bp[us][j], acc[td][j]);
           if constexpr (!kCodes)
-            if (k % 2 == 0 && kEarly + k / 2 < NC && more) get(next, buf ^ 1, kEarly + k / 2, piece, mixes);
+            if (k % 2 == 0 && kEarly + k / 2 < NC) get(next, buf ^ 1, kEarly + k / 2, piece, mixes);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
