@@ -43,6 +43,8 @@ using steps::tile_geom;
 
 constexpr int kRot = 64;                 // elements of the shared key part
 constexpr int kPair = 2 * kDim;          // a key's own part and its values
+constexpr float kSlack = 8.f;
+constexpr int kMinSteps = 4;             // per share, where there are few
 constexpr int kHeld = 256;               // CTAs of 8 waves that the chip holds
 
 struct ExpandedPlan {
@@ -53,7 +55,7 @@ struct ExpandedPlan {
 struct ExpandedParts {
   float* o;                              // [CTA][2][rows x 128, in the accumulators' order], normalised
   float* lse;                            // [CTA][2][rows], base 2
-  int4* tile;                            // [CTA]: the tile in slot 1: sequence, tile, parts (0: none)
+  int4* tile;                            // [CTA]: the tile in slot 1: first query row, rows, parts (0: none)
 };
 
 // Segment s of row r of the shared part: rows are 128 bytes, half of the banks.
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void latent_attn_kernel(
     // P of the pending sub-block in bf16, as the B operand of O^T = V^T P^T:
     // k-step u covers keys 16u + {4h + e, 8 + 4h + e}, e = 0..3
     bf16x8 bp[kKeys / 16];
-    float alpha_pend = 0.f;                       // alpha of the sub-block whose P is in bp
+    float alpha_pend = 1.f;                       // alpha of the sub-block whose P is in bp
 
     if (b_begin < b_end) {
       const int64_t first = seq_geom(sq, s).kv_start;
@@ -250,10 +252,12 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void latent_attn_kernel(
 #pragma unroll
           for (int a = 0; a < 16; ++a) z.m0 = fmaxf(z.m0, acc_s[1][a]);
           z.m0 = fmaxf(z.m0, xor32f(z.m0));
-          z.m_new = fmaxf(m_run, z.m0);
-          const float mm = z.m_new == -INFINITY ? 0.f : z.m_new;   // rows with nothing visible yet
-          z.alpha = exp2_hw((m_run - mm) * scale_log2);
-          z.neg = -mm * scale_log2;
+          // the maximum that weights are relative to moves only when it is outgrown by 2^kSlack (else O would be
+          // rescaled whenever some row's true one moves); the first visible keys outgrow -inf
+          const bool grown = (z.m0 - m_run) * scale_log2 > kSlack;
+          z.m_new = grown ? z.m0 : m_run;
+          z.alpha = grown ? exp2_hw((m_run - z.m0) * scale_log2) : 1.f;
+          z.neg = z.m_new == -INFINITY ? 0.f : -z.m_new * scale_log2;    // rows with nothing visible yet
         } else if (j < 14) {
 #pragma unroll
           for (int x = 0; x < 32; ++x) {
@@ -383,64 +387,80 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void latent_attn_kernel(
 #pragma unroll 1
   for (; sh.more(); sh.next())
     tile_rows(sh.g, sh.s, sh.x, sh.begin(), sh.end(), [&](int visits) {
-      if (threadIdx.x == 0) parts.tile[blockIdx.x] = make_int4(sh.s, sh.x, sh.parts(visits), 0);
+      if (threadIdx.x == 0)
+        parts.tile[blockIdx.x] = make_int4(sh.g.q_begin + sh.x * kTile, min(kTile, sh.g.q_rows - sh.x * kTile), sh.parts(visits), 0);
     });
 }
 
 // Joins the parts of a tile that several shares had: a = max LSE_c,
-// LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c, in key order.  Four
-// dimensions of a row per thread.
-template <int WAVES>
-__global__ __launch_bounds__(256) void latent_join_kernel(msa_seqs sq, ExpandedParts parts, int H, uint16_t* __restrict__ o,
+// LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c, in key order.  A CTA
+// forms the list of such tiles; a wave takes a piece, 4 dimensions of 32 rows in
+// each half of it.
+constexpr int kJoinCtas = 1024;
+__global__ __launch_bounds__(256) void latent_join_kernel(ExpandedParts parts, int ctas, int H, uint16_t* __restrict__ o,
                                                           float* __restrict__ lse) {
-  constexpr int kTile = 32 * WAVES;
-  const int4 what = parts.tile[blockIdx.x];
-  const int np = what.z;
-  if (np < 1) return;
-  const int unit = blockIdx.y * 256 + threadIdx.x;
-  const int lane = unit & 63, e4 = (unit >> 6) & 3, td = (unit >> 8) & 3, wave = unit >> 10;
-  const int r = 32 * wave + (lane & 31);
-  const TileGeom g = tile_geom(sq, what.x);
-  const int t = what.y * kTile + r;
-  if (t >= g.q_rows) return;
-  auto slot = [&](int c) { return 2 * (blockIdx.x + static_cast<int64_t>(c) * H) + (c == 0 ? 1 : 0); };
-  constexpr int kBatch = 8;
-  float top = -INFINITY, sum = 0.f;
-  f32x4 y{};
-  for (int c0 = 0; c0 < np; c0 += kBatch) {
-    float l[kBatch];
-    f32x4 v[kBatch];
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const int64_t at = slot(min(c0 + b, np - 1));
-      l[b] = parts.lse[at * kTile + r];
-      v[b] = reinterpret_cast<const f32x4*>(parts.o + at * kTile * kDim)[unit];
-    }
-    float m = top;
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      l[b] = c0 + b < np ? l[b] : -INFINITY;
-      m = fmaxf(m, l[b]);
-    }
-    const float base = m > -INFINITY ? m : 0.f;            // every part empty: all weights are zero
-    const float f = exp2_hw(top - base);
-    top = m;
-    sum *= f;
-    y *= f;
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const float w = exp2_hw(l[b] - base);
-      sum += w;
-      y += v[b] * w;
-    }
+  constexpr int kTile = 256, kPieces = kTile * kDim / 4 / kWave, kWaves = 4;
+  __shared__ int16_t list[kHeld];
+  __shared__ int count[kWaves];
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const bool has = static_cast<int>(threadIdx.x) < ctas && parts.tile[threadIdx.x].z > 0;    // ctas <= kHeld
+  const uint64_t mask = __ballot(has);
+  if (lane == 0) count[wave] = __popcll(mask);
+  __syncthreads();
+  int before = 0, tiles = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += count[w];
+    tiles += count[w];
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  const int64_t head_row = (static_cast<int64_t>(g.q_begin) + t) * H + blockIdx.x % H;
-  uint2 w;
-  w.x = pack_bf16x2(y[0] * inv, y[1] * inv);
-  w.y = pack_bf16x2(y[2] * inv, y[3] * inv);
-  *reinterpret_cast<uint2*>(o + head_row * kDim + 32 * td + 8 * e4 + 4 * (lane >> 5)) = w;
-  if (td == 0 && e4 == 0 && lane < 32) lse[head_row] = sum > 0.f ? (top + __log2f(sum)) * kLn_2 : -INFINITY;
+  if (has) list[before + __popcll(mask & ((1ull << lane) - 1))] = static_cast<int16_t>(threadIdx.x);
+  __syncthreads();
+  for (int i = blockIdx.x * kWaves + wave; i < tiles * kPieces; i += gridDim.x * kWaves) {
+    const int cta = list[i / kPieces], piece = i % kPieces;
+    const int4 what = parts.tile[cta];
+    const int np = what.z;
+    const int e4 = piece & 3, td = (piece >> 2) & 3, r = 32 * (piece >> 4) + (lane & 31);
+    if (r >= what.y) continue;             // rows behind the tile's have no parts
+    constexpr int kBatch = 8;
+    float top = -INFINITY, sum = 0.f;
+    f32x4 y{};
+    for (int c0 = 0; c0 < np; c0 += kBatch) {
+      float l[kBatch];
+      f32x4 v[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int c = c0 + b;
+        l[b] = -INFINITY;
+        v[b] = f32x4{};
+        if (c < np) {
+          const int64_t at = 2 * (cta + static_cast<int64_t>(c) * H) + (c == 0 ? 1 : 0);
+          l[b] = parts.lse[at * kTile + r];
+          v[b] = reinterpret_cast<const f32x4*>(parts.o + at * kTile * kDim)[piece * kWave + lane];
+        }
+      }
+      float m = top;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) m = fmaxf(m, l[b]);
+      const float base = m > -INFINITY ? m : 0.f;          // every part empty: all weights are zero
+      const float f = exp2_hw(top - base);
+      top = m;
+      sum *= f;
+      y *= f;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const float w = exp2_hw(l[b] - base);
+        sum += w;
+        y += v[b] * w;
+      }
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const int64_t head_row = (static_cast<int64_t>(what.x) + r) * H + cta % H;
+    uint2 w;
+    w.x = pack_bf16x2(y[0] * inv, y[1] * inv);
+    w.y = pack_bf16x2(y[2] * inv, y[3] * inv);
+    *reinterpret_cast<uint2*>(o + head_row * kDim + 32 * td + 8 * e4 + 4 * (lane >> 5)) = w;
+    if (td == 0 && e4 == 0 && lane < 32) lse[head_row] = sum > 0.f ? (top + __log2f(sum)) * kLn_2 : -INFINITY;
+  }
 }
 
 // ---------------------------------------------------------------- host side
@@ -454,21 +474,53 @@ int validate_expanded(const msa_seqs* seqs, int H) {
   return MSA_OK;
 }
 
-// Waves per CTA, and whether the steps are dealt out or each tile has a CTA.
+// Waves per CTA (one CTA of 8 per CU, or two of 4), and whether the steps are
+// dealt out or each tile has a CTA: what takes least by the sizes.  A step of a
+// full tile of 8 waves takes 2.66 us, of 4 waves 1.25 alone on a CU and 2.8 with
+// another beside it; shares cost 18 us more for their ends, parts and join.  Tiles
+// of a prompt see half of its keys on average, those of a chunk far behind a
+// context all, so they end in rounds.  (The lengths are on the device; the key
+// side's rows tell their mean where sequences lie one behind another.)
+// Measured, us, 8 waves / 4 waves / shares: one prompt of 777 rows, 20 heads 32.9 /
+// 23.5 / 30.9, 2000, 32 heads 73 / 61 / 88, 8000, 8 heads 236 / 200 / 211, 8192, 64
+// heads 1282 / 1296 / 1380; 20 documents of 100 - 1000 rows, 32 heads 81 / 66 / 113;
+// 2 x 512 rows on 16K keys, 64 heads 666 / 698 / 709; 2 x 500 on 8K, 20 heads 245 /
+// 183 / 125; 64 on 12K, 8 heads 207 / 226 / 33.
 ExpandedPlan plan_of(const msa_seqs* seqs, int H, int* waves, int64_t* ctas) {
-  ExpandedPlan pl{};
-  auto tiles_of = [&](int w) {
-    int64_t tiles;
-    pl.gr = flash::plan_grid(seqs, 32 * w, seqs->max_q_rows, &tiles);
-    return tiles;
+  const double rows = seqs->max_q_rows, keys = seqs->max_kv_len, seq_count = seqs->num_seqs;
+  const bool chunk = 2 * rows <= keys;
+  const double steps = std::max(1.0, keys / kKeys), avg = std::max(1.0, (keys - rows / 2) / kKeys);
+  const double mean = std::min(1.0, seqs->total_kv_rows / (seq_count * std::max(1.0, keys)));
+  auto tiles_with_rows = [&](int w) {      // at most
+    const int64_t per_seq = (seqs->max_q_rows + 32 * w - 1) / (32 * w);
+    return static_cast<double>(std::min<int64_t>(seqs->total_q_rows / (32 * w) + seqs->num_seqs, per_seq * seqs->num_seqs)) * H;
   };
+  const double u8 = tiles_with_rows(8), u4 = tiles_with_rows(4);
+  const double t8 = 2.66 * std::max(0.45, std::min(8.0, std::ceil(rows / 32)) / 8), t4 = 1.25, pair4 = 2.8;
+  double whole8 = steps * t8, whole4 = steps * t4;
+  if (chunk) {
+    whole8 *= std::ceil(u8 / kHeld);
+    if (u4 > 2 * kHeld) whole4 = std::ceil(u4 / (2 * kHeld)) * steps * pair4;
+    else if (u4 > kHeld) whole4 = steps * (t4 + (u4 / kHeld - 1) * (pair4 - t4));
+  } else {
+    whole8 = std::max(whole8, u8 / kHeld * avg * t8 * mean);
+    whole4 = std::max(whole4, u4 / (2 * kHeld) * avg * pair4 * mean);
+  }
+  // (shares have the last tiles' live waves alone to pay for)
+  const double filled = std::min(u8, (seqs->total_q_rows / 32 + seq_count) / 8 * H);
+  const double shares = filled / kHeld * avg * (rows >= 256 ? 2.66 : t8) * mean + 18;
+  ExpandedPlan pl{};
   *waves = 8;
-  int64_t tiles = tiles_of(8);
+  if (H <= kHeld && shares < std::min(whole8, whole4)) {
+    pl.ranges = std::max(1, kHeld / H);
+    pl.min_steps = kMinSteps;
+    *ctas = static_cast<int64_t>(pl.ranges) * H;
+    return pl;
+  }
+  if (whole4 < whole8) *waves = 4;
+  int64_t tiles;
+  pl.gr = flash::plan_grid(seqs, 32 * *waves, seqs->max_q_rows, &tiles);
   *ctas = tiles * H;
-  if (*ctas >= 4 * kHeld || H > kHeld) return pl;
-  pl.ranges = std::max(1, kHeld / H);
-  pl.min_steps = 4;
-  *ctas = static_cast<int64_t>(pl.ranges) * H;
   return pl;
 }
 size_t part_bytes(int64_t ctas, int waves) {
@@ -522,10 +574,11 @@ extern "C" int msa_latent_attn(const void* q, int64_t q_stride, int64_t q_head_s
                      static_cast<const uint16_t*>(q), q_stride, q_head_stride, static_cast<const uint16_t*>(q_rope),
                      q_rope_stride, q_rope_head_stride, static_cast<const uint16_t*>(kv), static_cast<const uint16_t*>(k_rope),
                      k_rope_stride, *seqs, pl, parts, num_heads, scale.log2, scale.q_flip, static_cast<uint16_t*>(o), lse);
-    if (pl.ranges > 0)
-      msa_prof::launch("latent_join_kernel", latent_join_kernel<W>, dim3(static_cast<unsigned>(ctas), 4 * W), dim3(256), 0,
-                       stream, *seqs, parts, num_heads, static_cast<uint16_t*>(o), lse);
   };
-  run(std::integral_constant<int, 8>{});
+  if (waves == 4) run(std::integral_constant<int, 4>{});
+  else run(std::integral_constant<int, 8>{});
+  if (pl.ranges > 0)
+    msa_prof::launch("latent_join_kernel", latent_join_kernel, dim3(kJoinCtas), dim3(256), 0, stream, parts,
+                     static_cast<int>(ctas), num_heads, static_cast<uint16_t*>(o), lse);
   return msa_host::launch_status();
 }

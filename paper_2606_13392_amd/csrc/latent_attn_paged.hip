@@ -47,7 +47,7 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kCtas = 256;               // one per CU: two buffers of keys fill its LDS
 constexpr int kMergeCtas = 1024;
-constexpr int kMinSteps = 4;             // steps per CTA, where there are few
+constexpr int kMinSteps = 2;             // steps per CTA, where there are few
 constexpr float kSlack = 8.f;
 constexpr int kAheadK = 6, kAheadV = 3;  // LDS operands requested so many products ahead
 
