@@ -40,6 +40,7 @@ using steps::tile_geom;
 constexpr int kRot = 64;                 // elements of the shared key part
 constexpr int kPair = 2 * kDim;          // a key's own part and its values
 constexpr int kRowsT = 64;               // streamed rows per tile
+constexpr int kRing = 3;
 constexpr int kWaves = 4;                // one per SIMD: a wave's operands and sums take 240 (keys) or 352 registers
 constexpr int kThreads = kWaves * kWave;
 constexpr int kRowTile = 64 * kWaves, kKeyTile = 32 * kWaves;      // stationary rows per CTA
@@ -51,6 +52,8 @@ constexpr int kRowTile = 64 * kWaves, kKeyTile = 32 * kWaves;      // stationary
 // another's.
 __device__ __forceinline__ int wide_mix(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
 __device__ __forceinline__ int half_mix(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
+
+typedef u32x4 u32x4_at8 __attribute__((aligned(8)));               // gradients of queries may stand at any multiple of 8
 
 struct Tile {
   uint16_t own[kRowsT * kDim], other[kRowsT * kDim], rot[kRowsT * kRot];
@@ -93,8 +96,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   constexpr int kTileRows = 32 * NT * kWaves;
   constexpr int NK = 16 / kWaves, NR = 8 / kWaves; // copies of 1 KiB per wave: wide rows, half rows
   constexpr int kAhead = KEYS ? 5 : 3;
-  __shared__ __align__(16) Tile ring[2];
-  __shared__ __align__(16) float stat[2][2][KEYS ? kRowsT : 4];   // streamed queries: LSE, D
+  __shared__ __align__(16) Tile ring[kRing];
+  __shared__ __align__(16) float stat[kRing][2][KEYS ? kRowsT : 4];   // streamed queries: LSE, D
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int n = lane & 31, h = lane >> 5;
@@ -151,34 +154,50 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
                  rot_s = static_cast<uint32_t>(rot.row * 2);
   const uint32_t lds0 = lds_address(&ring[0]);
   constexpr uint32_t kOwnAt = 0, kOtherAt = sizeof(uint16_t) * kRowsT * kDim, kRotAt = 2 * kOtherAt;
-  auto copy = [&](int b, int buf) {
-    const int last = streamed - 1 - b * kRowsT;    // rows past the end repeat the last one
-    const uint32_t dst = lds0 + buf * static_cast<uint32_t>(sizeof(Tile)) + 1024 * wave;
+  // a tile's copies, one at a time: piece 0 .. 2 NK - 1 wide rows, then half rows, then (KEYS) the statistics
+  constexpr int kCopies = 2 * NK + NR;
+  struct From {
+    const char *own, *other, *rot, *stat;
+    int last;                                      // rows past the end repeat the last one
+    uint32_t dst, dst_stat;
+  };
+  auto source = [&](int b, int buf) {
     const int64_t at = static_cast<int64_t>(b) * kRowsT;
-    const char* p0 = own_p + at * own_s;
-    const char* p1 = other_p + at * other_s;
-    const char* p2 = rot_p + at * rot_s;
-    int ln = lane;
-    asm volatile("" : "+v"(ln));                   // as above
-#pragma unroll
-    for (int c = 0; c < NK; ++c) {
-      const int r = 4 * (c * kWaves + wave) + (ln >> 4);
-      const uint32_t seg = 16 * ((ln & 15) ^ wide_mix(r)), rr = min(r, last);
-      copy16(p0, rr * own_s + seg, dst + kOwnAt + 1024 * kWaves * c);
-      copy16(p1, rr * other_s + seg, dst + kOtherAt + 1024 * kWaves * c);
-    }
-#pragma unroll
-    for (int c = 0; c < NR; ++c) {
-      const int r = 8 * (c * kWaves + wave) + (ln >> 3);
-      copy16(p2, min(r, last) * rot_s + 16 * ((ln & 7) ^ half_mix(r)), dst + kRotAt + 1024 * kWaves * c);
-    }
-    if constexpr (KEYS) {
-      if (wave < 2) {
-        const float* src = a.stat + (static_cast<int64_t>(wave) * a.H + hd) * sq.total_q_rows + row0 + at;
-        copy4(reinterpret_cast<const char*>(src), 4 * min(lane, last), lds_address(&stat[buf][wave][0]));
-      }
+    From f;
+    f.own = own_p + at * own_s;
+    f.other = other_p + at * other_s;
+    f.rot = rot_p + at * rot_s;
+    f.stat = reinterpret_cast<const char*>(a.stat + (static_cast<int64_t>(wave & 1) * a.H + hd) * sq.total_q_rows + row0 + at);
+    f.last = streamed - 1 - b * kRowsT;
+    f.dst = lds0 + buf * static_cast<uint32_t>(sizeof(Tile)) + 1024 * wave;
+    f.dst_stat = lds_address(&stat[0][0][0]) + (2 * buf + (wave & 1)) * static_cast<uint32_t>(sizeof(stat[0][0]));
+    return f;
+  };
+  auto copy_piece = [&](const From& f, int c, int ln) __attribute__((always_inline)) {
+    if (c < 2 * NK) {
+      const int r = 4 * ((c >> 1) * kWaves + wave) + (ln >> 4);
+      const uint32_t seg = 16 * ((ln & 15) ^ wide_mix(r)), rr = min(r, f.last);
+      if (c & 1) copy16(f.other, rr * other_s + seg, f.dst + kOtherAt + 1024 * kWaves * (c >> 1));
+      else copy16(f.own, rr * own_s + seg, f.dst + kOwnAt + 1024 * kWaves * (c >> 1));
+    } else if (c < kCopies) {
+      const int r = 8 * ((c - 2 * NK) * kWaves + wave) + (ln >> 3);
+      copy16(f.rot, min(r, f.last) * rot_s + 16 * ((ln & 7) ^ half_mix(r)), f.dst + kRotAt + 1024 * kWaves * (c - 2 * NK));
+    } else {
+      copy4(f.stat, 4 * min(ln, f.last), f.dst_stat);           // waves 2 and 3 the same again
     }
   };
+  constexpr int kAllCopies = kCopies + (KEYS ? 1 : 0);
+  auto copy = [&](int b, int buf) {
+    const From f = source(b, buf);
+    int ln = lane;
+    asm volatile("" : "+v"(ln));                   // offsets are formed here each time: held, they spill
+#pragma unroll
+    for (int c = 0; c < kAllCopies; ++c) copy_piece(f, c, ln);
+  };
+  if (b_begin < b_end) {
+    copy(b_begin, 0);
+    if (b_begin + 1 < b_end) copy(b_begin + 1, 1);
+  }
 
   // ------------------------------------------------ stationary operands
   bf16x8 b1[NT][KS], b2[NT][KO];
@@ -205,7 +224,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
           lane_d[nt] = fmaf(static_cast<float>(ov[i]), static_cast<float>(b2[nt][st][i]), lane_d[nt]);
       }
       lane_d[nt] += xor32f(lane_d[nt]);
-      lane_lse[nt] = a.lse[mine * a.H + hd] * kLog2E;
+      // a row that meets no key has an LSE of -infinity; +infinity keeps its weights 0 behind the mask too
+      const float lse = a.lse[mine * a.H + hd];
+      lane_lse[nt] = lse == -INFINITY ? INFINITY : lse * kLog2E;
       if (valid && h == 0) {
         a.stat[static_cast<int64_t>(hd) * sq.total_q_rows + mine] = lane_lse[nt];
         a.stat[(static_cast<int64_t>(a.H) + hd) * sq.total_q_rows + mine] = lane_d[nt];
@@ -238,13 +259,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   bf16x8 ps[NT][2], pp[NT][2];                           // pending dS and (KEYS) P of 32 streamed rows, as B operands
 
   // both score products of streamed rows 32 half .. + 31: lane (n, h) gets rows 8(i/4) + 4h + i%4 against its own
-  auto products = [&](int buf, int half, f32x16 (&z)[NT], f32x16 (&dz)[NT]) {
+  auto products = [&](int buf, int half, f32x16 (&z)[NT], f32x16 (&dz)[NT], auto beside) __attribute__((always_inline)) {
     const char* t = reinterpret_cast<const char*>(&ring[buf]);
     const char* t_own = t + kOwnAt + half * 32 * 2 * kDim;
     const char* t_rot = t + kRotAt + half * 32 * 2 * kRot;
     const char* t_other = t + kOtherAt + half * 32 * 2 * kDim;
     uint32_t at_own = row_own, at_rot = row_rot;
-    asm volatile("" : "+v"(at_own), "+v"(at_rot));   // the addresses are formed here each time: held, they spill
+    asm volatile("" : "+v"(at_own), "+v"(at_rot));   // as above
     auto read = [&](int j) -> bf16x8 {
       const char* p = j < KO ? t_own + (at_own ^ (32 * j)) : j < KS ? t_rot + (at_rot ^ (32 * (j - KO)))
                                                                      : t_other + (at_own ^ (32 * (j - KS)));
@@ -263,6 +284,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
         if (j < KS) z[nt] = mfma32x32x16(op[j], b1[nt][j < KS ? j : 0], z[nt]);
         else dz[nt] = mfma32x32x16(op[j], b2[nt][j < KS ? 0 : j - KS], dz[nt]);
       }
+      beside(j);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -300,6 +322,31 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   // P and dS of 32 streamed rows in kSlots pieces: z becomes P, dz dS.  The last two pieces pack them, each after the
   // last slot that adds what was there before.
   f32x4 row_lse{}, row_d{};
+  const int edge = (KEYS ? w0 + n - base_p : base_p + w0 + n) - 4 * h;
+  auto expo = [&](int buf, int row, auto masked, f32x16 (&z)[NT], int i) __attribute__((always_inline)) {
+    if constexpr (KEYS) {
+      if (i % 4 == 0) row_lse = *reinterpret_cast<const f32x4*>(&stat[buf][0][(row & (kRowsT - 1)) + 8 * (i / 4) + 4 * h]);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float p = exp2_hw(fmaf(z[nt][i], a.scale_log2, KEYS ? -row_lse[i % 4] : -lane_lse[nt]));
+      if constexpr (decltype(masked)::value) {
+        const int y = 8 * (i / 4) + i % 4;         // of the streamed row, less row + 4 h
+        p = (KEYS ? y >= edge - row : y <= edge + 32 * nt - row) ? p : 0.f;
+      }
+      z[nt][i] = p;
+    }
+  };
+  // Of the 16, this many go between the second score products, which need no result of theirs: additions of 24 matrix
+  // products do not cover all the work on 32 x 64 weights (8K rows of one sequence: 1.90 ms; with none 1.96, with 16
+  // the same), those of 20 cover the work on 32 x 32.
+  constexpr int kEarly = KEYS ? 0 : 12;
+  auto early = [&](int buf, int row, auto masked, f32x16 (&z)[NT], int j) __attribute__((always_inline)) {
+    constexpr int kFirst = KS + 1, kMany = KO - 1;
+#pragma unroll
+    for (int i = 0; i < kEarly; ++i)
+      if (j == kFirst + i * kMany / max(kEarly, 1)) expo(buf, row, masked, z, i);
+  };
   auto weigh = [&](int buf, int row, auto masked, f32x16 (&z)[NT], f32x16 (&dz)[NT], int j) __attribute__((always_inline)) {
     constexpr int kLast = kSlots - 2;
     static_assert(kLast >= NA, "");
@@ -307,23 +354,11 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     for (int i = 0; i < 16; ++i) {
       if (i * kLast / 16 != j) continue;
       if constexpr (KEYS) {
-        if (i % 4 == 0) {
-          const int at = (row & (kRowsT - 1)) + 8 * (i / 4) + 4 * h;
-          row_lse = *reinterpret_cast<const f32x4*>(&stat[buf][0][at]);
-          row_d = *reinterpret_cast<const f32x4*>(&stat[buf][1][at]);
-        }
+        if (i % 4 == 0) row_d = *reinterpret_cast<const f32x4*>(&stat[buf][1][(row & (kRowsT - 1)) + 8 * (i / 4) + 4 * h]);
       }
+      if (i >= kEarly) expo(buf, row, masked, z, i);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p = exp2_hw(fmaf(z[nt][i], a.scale_log2, KEYS ? -row_lse[i % 4] : -lane_lse[nt]));
-        if constexpr (decltype(masked)::value) {
-          const int x = w0 + 32 * nt + n, y = row + 8 * (i / 4) + 4 * h + (i % 4);
-          const bool seen = KEYS ? x <= base_p + y && y < g.q_rows : y <= base_p + x;
-          p = seen ? p : 0.f;
-        }
-        z[nt][i] = p;
-        dz[nt][i] = p * (dz[nt][i] - (KEYS ? row_d[i % 4] : lane_d[nt]));
-      }
+      for (int nt = 0; nt < NT; ++nt) dz[nt][i] = z[nt][i] * (dz[nt][i] - (KEYS ? row_d[i % 4] : lane_d[nt]));
     }
     if (j >= kLast) {
       const int u = j - kLast;
@@ -342,80 +377,121 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
       }
     }
   };
-  // whether some lane of the wave has a streamed row of tile b that it does not meet
+  // whether some lane of the wave does not meet some row of tile b (rows past the queries' end aside, see below)
   auto is_masked = [&](int b) {
-    return KEYS ? base_p + b * kRowsT < w0 + 32 * NT - 1 || (b + 1) * kRowsT > g.q_rows : (b + 1) * kRowsT > base_p + w0 + 1;
+    return KEYS ? base_p + b * kRowsT < w0 + 32 * NT - 1 : (b + 1) * kRowsT > base_p + w0 + 1;
   };
   auto sync = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // tile b's copies, all waves'; queries past the end get an LSE of +infinity, and so no weight
+  auto arrive = [&](int b, int buf) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (KEYS) {
+      if ((b + 1) * kRowsT > streamed && (wave & 1) == 0 && b * kRowsT + lane >= streamed) stat[buf][0][lane] = INFINITY;
+    }
+    sync();
+  };
 
   if (b_begin < b_end) {
-    copy(b_begin, 0);
-    if (b_begin + 1 < b_end) copy(b_begin + 1, 1);
-    // copies per wave and tile; (KEYS, waves 0 and 1) one more, so waiting for the older tile's leaves none of it
-    constexpr int kCopies = 2 * NK + NR;
-    if (b_begin + 1 < b_end) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    sync();
+    arrive(b_begin, 0);
     f32x16 z[NT], dz[NT];
-    products(0, 0, z, dz);
+    products(0, 0, z, dz, [&](int j) __attribute__((always_inline)) { early(0, b_begin * kRowsT, std::true_type{}, z, j); });
 #pragma unroll
     for (int j = 0; j < kSlots; ++j) weigh(0, b_begin * kRowsT, std::true_type{}, z, dz, j);
-    // rows 32 .. 63 of tile b, then rows 0 .. 31 of tile b + 1: the products of these, the additions of those before
-    auto step = [&](int b, auto masked) __attribute__((always_inline)) {
-      const int buf = (b - b_begin) & 1;
-      products(buf, 1, z, dz);
+    // Rows 32 .. 63 of tile b, then rows 0 .. 31 of tile b + 1: the products of these, the additions of those before.
+    // Behind the barrier tile b + 1 is there and tile b - 1's readers are done: its buffer takes tile b + 2,
+    // whose copies go out between the products.  (Behind the last tiles they repeat the last one.)
+    int b = b_begin, buf = 0;
+    auto step = [&](auto masked) __attribute__((always_inline)) {
+      const int next = buf == kRing - 1 ? 0 : buf + 1;
+      products(buf, 1, z, dz, [&](int j) __attribute__((always_inline)) { early(buf, b * kRowsT + 32, masked, z, j); });
       additions(buf, 0, [&](int j) __attribute__((always_inline)) { weigh(buf, b * kRowsT + 32, masked, z, dz, j); });
-      if (b + 1 == b_end) return;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // tile b + 1 has landed
-      sync();
-      products(buf ^ 1, 0, z, dz);
-      additions(buf, 1, [&](int j) __attribute__((always_inline)) { weigh(buf ^ 1, (b + 1) * kRowsT, masked, z, dz, j); });
-      sync();                                                      // tile b's readers are done
-      if (b + 2 < b_end) copy(b + 2, buf);
+      arrive(b + 1, next);
+      const From f = source(min(b + 2, b_end - 1), buf == 0 ? kRing - 1 : buf - 1);
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+      products(next, 0, z, dz, [&](int j) __attribute__((always_inline)) {
+        if (j % 2 == 1 && j / 2 < kAllCopies) copy_piece(f, j / 2, ln);
+        early(next, (b + 1) * kRowsT, masked, z, j);
+      });
+      if constexpr (kAllCopies > (KS + KO) / 2) copy_piece(f, kAllCopies - 1, ln);
+      additions(buf, 1, [&](int j) __attribute__((always_inline)) { weigh(next, (b + 1) * kRowsT, masked, z, dz, j); });
+      ++b;
+      buf = next;
     };
-    int b = b_begin;
-    if constexpr (KEYS)
-      for (; b < b_end && (is_masked(b) || is_masked(b + 1)); ++b) step(b, std::true_type{});
-    for (; b + 1 < b_end && !is_masked(b + 1) && !is_masked(b); ++b) step(b, std::false_type{});
-    for (; b < b_end; ++b) step(b, std::true_type{});
-    additions((b_end - 1 - b_begin) & 1, 1, [](int) {});
+    if constexpr (KEYS) {
+      while (b + 1 < b_end && (is_masked(b) || is_masked(b + 1))) step(std::true_type{});
+      while (b + 1 < b_end) step(std::false_type{});
+    } else {
+      while (b + 1 < b_end && !is_masked(b + 1)) step(std::false_type{});
+      while (b + 1 < b_end) step(std::true_type{});
+    }
+    products(buf, 1, z, dz, [&](int j) __attribute__((always_inline)) { early(buf, b * kRowsT + 32, std::true_type{}, z, j); });
+    additions(buf, 0, [&](int j) __attribute__((always_inline)) { weigh(buf, b * kRowsT + 32, std::true_type{}, z, dz, j); });
+    additions(buf, 1, [](int) {});
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // the ring is used again below
   }
 
-  // ------------------------------------------------ results: lane (n, h) holds dims 32i + 8(e/4) + 4h + e%4 of its row
-  auto store = [&](const f32x16& v, float f, uint16_t* y) {
+  // ------------------------------------------------ results
+  // Lane (n, h) holds dims 32 i + 8 (e / 4) + 4 h + e % 4 of its row.  They leave by rows, through an area of the wave's
+  // own in the ring: segments of 16 bytes, permuted by the row as above.  (Straight from the accumulators a store
+  // touches 32 rows; 15000 clocks a CTA instead of 5000.)
+  sync();
+  char* area = reinterpret_cast<char*>(&ring[0]) + wave * (kRing * sizeof(Tile) / kWaves);
+  auto lay = [&](const f32x16& v, float f, int row, int i, bool half, char* base) {
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
       uint2 p;
       p.x = pack_bf16x2(v[4 * e4 + 0] * f, v[4 * e4 + 1] * f);
       p.y = pack_bf16x2(v[4 * e4 + 2] * f, v[4 * e4 + 3] * f);
-      *reinterpret_cast<uint2*>(y + 8 * e4) = p;
+      const int seg = 4 * i + e4;
+      *reinterpret_cast<uint2*>(base + (half ? row * 2 * kRot + 16 * (seg ^ half_mix(row)) : row * 2 * kDim + 16 * (seg ^ wide_mix(row))) +
+                                8 * h) = p;
     }
   };
+  // rows 0 .. 32 NT - 1 of the wave from the area
+  auto leave = [&](const Grad& to, bool half, const char* base) {
+    const int per = half ? 8 : 4;                  // rows per store
+#pragma unroll 4
+    for (int c = 0; c < 32 * NT / per; ++c) {
+      const int r = per * c + (half ? lane >> 3 : lane >> 4), seg = half ? lane & 7 : lane & 15;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(
+          base + (half ? r * 2 * kRot + 16 * (seg ^ half_mix(r)) : r * 2 * kDim + 16 * (seg ^ wide_mix(r))));
+      if (w0 + r < limit) *reinterpret_cast<u32x4_at8*>(to.p + (base_x + w0 + r) * to.row + hd * to.head + 8 * seg) = v;
+    }
+  };
+  constexpr int kWide = 32 * NT * 2 * kDim;        // bytes of the wave's rows of 128 elements
+  static_assert(kWide * (KEYS ? 2 : 1) + 32 * NT * (KEYS ? 4 : 2) * kRot <= kRing * sizeof(Tile) / kWaves, "");
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int x = w0 + 32 * nt + n;
-    if (x >= limit) continue;
-    const int64_t mine = base_x + x;
-    const Grad to = KEYS ? a.d_k : a.d_q;
-    uint16_t* y = to.p + mine * to.row + hd * to.head + 4 * h;
+    const int row = 32 * nt + n;
 #pragma unroll
-    for (int i = 0; i < KO / 2; ++i) store(acc[i][nt], a.scale, y + 32 * i);
+    for (int i = 0; i < KO / 2; ++i) lay(acc[i][nt], a.scale, row, i, false, area);
     if constexpr (KEYS) {
-      uint16_t* yv = a.d_v.p + mine * a.d_v.row + hd * a.d_v.head + 4 * h;
 #pragma unroll
-      for (int i = 0; i < kDim / 32; ++i) store(acc[ND + i][nt], 1.f, yv + 32 * i);
-      float* yr = a.d_r + (static_cast<int64_t>(hd) * sq.total_kv_rows + mine) * kRot + 4 * h;
+      for (int i = 0; i < kDim / 32; ++i) lay(acc[ND + i][nt], 1.f, row, i, false, area + kWide);
 #pragma unroll
       for (int i = KO / 2; i < ND; ++i)
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4)
-          *reinterpret_cast<f32x4*>(yr + 32 * (i - KO / 2) + 8 * e4) =
+        for (int e4 = 0; e4 < 4; ++e4)             // fp32: rows of 256 bytes
+          *reinterpret_cast<f32x4*>(area + 2 * kWide + row * 4 * kRot + 16 * ((8 * (i - KO / 2) + 2 * e4 + h) ^ wide_mix(row))) =
               f32x4{acc[i][nt][4 * e4], acc[i][nt][4 * e4 + 1], acc[i][nt][4 * e4 + 2], acc[i][nt][4 * e4 + 3]};
     } else {
-      uint16_t* ye = a.d_e.p + mine * a.d_e.row + hd * a.d_e.head + 4 * h;
 #pragma unroll
-      for (int i = KO / 2; i < ND; ++i) store(acc[i][nt], a.scale, ye + 32 * (i - KO / 2));
+      for (int i = KO / 2; i < ND; ++i) lay(acc[i][nt], a.scale, row, i - KO / 2, true, area + kWide);
     }
+  }
+  leave(KEYS ? a.d_k : a.d_q, false, area);
+  if constexpr (KEYS) {
+    leave(a.d_v, false, area + kWide);
+#pragma unroll 4
+    for (int c = 0; c < 32 * NT / 4; ++c) {
+      const int r = 4 * c + (lane >> 4), seg = lane & 15;
+      const f32x4 v = *reinterpret_cast<const f32x4*>(area + 2 * kWide + r * 4 * kRot + 16 * (seg ^ wide_mix(r)));
+      if (w0 + r < limit)
+        *reinterpret_cast<f32x4*>(a.d_r + (static_cast<int64_t>(hd) * sq.total_kv_rows + base_x + w0 + r) * kRot + 4 * seg) = v;
+    }
+  } else {
+    leave(a.d_e, true, area + kWide);
   }
 }
 

@@ -129,9 +129,13 @@ def test_expanded_refuses(kw, want):
 
 
 def test_expanded_workspace():
-    a = _expanded(ws=None)
-    assert msa.lib().msa_latent_attn_workspace_size(ctypes.byref(a["seqs"]), 8) > 0 and _forward(a) == WS
-    assert _forward(_expanded(ws_bytes=100)) == WS and _forward(_expanded(ws=8)) == UNS
+    """A few rows on a long context are dealt out and take a workspace; one prompt's tiles need none."""
+    long = _seqs(total_q_rows=64, max_q_rows=64, total_kv_rows=9000, max_kv_len=9000)
+    size = lambda seqs: msa.lib().msa_latent_attn_workspace_size(ctypes.byref(seqs), 8)
+    assert size(long) > 0 and size(_seqs()) == 0
+    assert _forward(_expanded(seqs=long, ws=None)) == WS
+    assert _forward(_expanded(seqs=long, ws_bytes=size(long) - 1)) == WS
+    assert _forward(_expanded(seqs=long, ws=8)) == UNS
 
 
 @pytest.mark.parametrize("kw,want", [
