@@ -19,6 +19,7 @@
 // before, between which the weights are formed.  The shared part's gradient leaves
 // per head in fp32 and latent_sum_kernel adds the heads in their order; it also
 // clears what no sequence owns.
+#include <cmath>
 #include <initializer_list>
 #include <type_traits>
 
@@ -59,11 +60,18 @@ struct Tile {
   uint16_t own[kRowsT * kDim], other[kRowsT * kDim], rot[kRowsT * kRot];
 };
 
-__device__ __forceinline__ void copy4(const char* base, uint32_t offset, uint32_t lds) {   // lane l's 4 bytes land at lds + 4 l
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(offset), "s"(base), "s"(lds) : "m0", "memory");
-#pragma clang diagnostic pop
+// A streamed query's statistics as three bf16 each, the largest first, 24 bits
+// together: -LSE / scale in x and y, -D in z and w.  As an operand of a matrix
+// product against ones they start both scores' sums, in place of eight reads of four
+// numbers each per 32 rows: the reads of LDS are what bounds the keys' kernel.
+// kFar (of -scale's sign) takes every weight to 0; |scale| is at least kLeast, so that
+// the quotient of a scale of 0 is a number (all below it is 0 to an exponent).
+constexpr float kFar = 0x1p120f, kLeast = 0x1p-100f;
+__device__ __forceinline__ uint2 three_bf16(float x) {
+  const uint32_t hi = pack_bf16x2(x, 0.f) & 0xFFFFu;
+  const float r = x - __uint_as_float(hi << 16);
+  const uint32_t mid = pack_bf16x2(r, 0.f) & 0xFFFFu;
+  return make_uint2(hi | mid << 16, pack_bf16x2(r - __uint_as_float(mid << 16), 0.f) & 0xFFFFu);
 }
 
 struct Side {                            // [rows, heads] vectors: elements between rows and between heads
@@ -78,7 +86,7 @@ struct Args {
   Side q, e, k, v, r, o, d_o;            // k, v: a key's own part and values; r: the shared part (head 0)
   const float* lse;                      // [T, H]
   Grad d_q, d_e, d_k, d_v;
-  float* stat;                           // [2][H][T]: LSE in base 2, D
+  uint4* stat;                           // [H][T]
   float* d_r;                            // [H][total_kv][64], before the scale
   int H;
   float scale, scale_log2;
@@ -97,7 +105,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   constexpr int NK = 16 / kWaves, NR = 8 / kWaves; // copies of 1 KiB per wave: wide rows, half rows
   constexpr int kAhead = KEYS ? 5 : 3;
   __shared__ __align__(16) Tile ring[kRing];
-  __shared__ __align__(16) float stat[kRing][2][KEYS ? kRowsT : 4];   // streamed queries: LSE, D
+  __shared__ __align__(16) uint4 stat[kRing][KEYS ? kRowsT : 1];      // of streamed queries
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int n = lane & 31, h = lane >> 5;
@@ -167,30 +175,47 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     f.own = own_p + at * own_s;
     f.other = other_p + at * other_s;
     f.rot = rot_p + at * rot_s;
-    f.stat = reinterpret_cast<const char*>(a.stat + (static_cast<int64_t>(wave & 1) * a.H + hd) * sq.total_q_rows + row0 + at);
+    f.stat = reinterpret_cast<const char*>(a.stat + hd * sq.total_q_rows + row0 + at);
     f.last = streamed - 1 - b * kRowsT;
     f.dst = lds0 + buf * static_cast<uint32_t>(sizeof(Tile)) + 1024 * wave;
-    f.dst_stat = lds_address(&stat[0][0][0]) + (2 * buf + (wave & 1)) * static_cast<uint32_t>(sizeof(stat[0][0]));
+    f.dst_stat = lds_address(&stat[0][0]) + buf * static_cast<uint32_t>(sizeof(stat[0]));
     return f;
   };
-  auto copy_piece = [&](const From& f, int c, int ln) __attribute__((always_inline)) {
+  // (KEYS) a lane's offsets are held, and formed again for the last tile alone
+  auto offset = [&](int c, int ln, int last) __attribute__((always_inline)) -> uint32_t {
     if (c < 2 * NK) {
       const int r = 4 * ((c >> 1) * kWaves + wave) + (ln >> 4);
-      const uint32_t seg = 16 * ((ln & 15) ^ wide_mix(r)), rr = min(r, f.last);
-      if (c & 1) copy16(f.other, rr * other_s + seg, f.dst + kOtherAt + 1024 * kWaves * (c >> 1));
-      else copy16(f.own, rr * own_s + seg, f.dst + kOwnAt + 1024 * kWaves * (c >> 1));
-    } else if (c < kCopies) {
-      const int r = 8 * ((c - 2 * NK) * kWaves + wave) + (ln >> 3);
-      copy16(f.rot, min(r, f.last) * rot_s + 16 * ((ln & 7) ^ half_mix(r)), f.dst + kRotAt + 1024 * kWaves * (c - 2 * NK));
-    } else {
-      copy4(f.stat, 4 * min(ln, f.last), f.dst_stat);           // waves 2 and 3 the same again
+      return min(r, last) * (c & 1 ? other_s : own_s) + 16 * ((ln & 15) ^ wide_mix(r));
     }
+    const int r = 8 * ((c - 2 * NK) * kWaves + wave) + (ln >> 3);
+    return c < kCopies ? min(r, last) * rot_s + 16 * ((ln & 7) ^ half_mix(r)) : 16 * min(ln, last);
   };
   constexpr int kAllCopies = kCopies + (KEYS ? 1 : 0);
+  uint32_t held[KEYS ? kAllCopies : 1];
+  auto hold = [&](int last) __attribute__((always_inline)) {
+    if constexpr (KEYS)
+#pragma unroll
+      for (int c = 0; c < kAllCopies; ++c) {
+        held[c] = offset(c, lane, last);
+        asm volatile("" : "+v"(held[c]));
+      }
+  };
+  auto copy_piece = [&](const From& f, int c, int ln) __attribute__((always_inline)) {
+    const uint32_t at = KEYS ? held[KEYS ? c : 0] : offset(c, ln, f.last);
+    if (c < 2 * NK) {
+      if (c & 1) copy16(f.other, at, f.dst + kOtherAt + 1024 * kWaves * (c >> 1));
+      else copy16(f.own, at, f.dst + kOwnAt + 1024 * kWaves * (c >> 1));
+    } else if (c < kCopies) {
+      copy16(f.rot, at, f.dst + kRotAt + 1024 * kWaves * (c - 2 * NK));
+    } else {
+      copy16(f.stat, at, f.dst_stat);              // each wave the same: the count is alike
+    }
+  };
   auto copy = [&](int b, int buf) {
     const From f = source(b, buf);
     int ln = lane;
     asm volatile("" : "+v"(ln));                   // offsets are formed here each time: held, they spill
+    hold(f.last);
 #pragma unroll
     for (int c = 0; c < kAllCopies; ++c) copy_piece(f, c, ln);
   };
@@ -228,24 +253,49 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
       const float lse = a.lse[mine * a.H + hd];
       lane_lse[nt] = lse == -INFINITY ? INFINITY : lse * kLog2E;
       if (valid && h == 0) {
-        a.stat[static_cast<int64_t>(hd) * sq.total_q_rows + mine] = lane_lse[nt];
-        a.stat[(static_cast<int64_t>(a.H) + hd) * sq.total_q_rows + mine] = lane_d[nt];
+        const float far = copysignf(kFar, -a.scale_log2), x = lane_lse[nt] / -a.scale_log2;
+        const uint2 l = three_bf16(lse == -INFINITY ? far : x > kFar ? kFar : x < -kFar ? -kFar : x), d = three_bf16(-lane_d[nt]);
+        a.stat[hd * sq.total_q_rows + mine] = make_uint4(l.x, l.y, d.x, d.y);
       }
     }
   }
 
   // ------------------------------------------------ operand addresses
-  const uint32_t row_own = n * 2 * kDim + 16 * (h ^ wide_mix(n));
-  const uint32_t row_rot = n * 2 * kRot + 16 * (h ^ half_mix(n));
-  uint32_t col_own, col_rot;
+  // (KEYS) each held, from the start of the ring; else formed from the first where they are read: no register is left
+  constexpr int kWideAt = KEYS ? KO : 1, kHalfAt = KEYS ? kRot / 16 : 1;
+  uint32_t row_own[kWideAt], row_rot[kHalfAt], col_own[kWideAt], col_rot[kHalfAt];
   {
     // transposed operand: in each 16-lane group, lane j addresses row k0 + j/4, dims n0 + 4(j%4) .. +3 and
     // receives rows k0 .. k0+3 of dim n0 + j
     const int gq = lane >> 4, jj = lane & 15;
     const int rl = 4 * h + (jj >> 2), seg = 2 * (gq & 1) + ((jj & 3) >> 1);
-    col_own = rl * 2 * kDim + 16 * (seg ^ wide_mix(rl)) + 8 * (jj & 1);
-    col_rot = rl * 2 * kRot + 16 * (seg ^ half_mix(rl)) + 8 * (jj & 1);
+#pragma unroll
+    for (int j = 0; j < kWideAt; ++j) {
+      row_own[j] = n * 2 * kDim + 16 * (h ^ wide_mix(n)) ^ 32 * j;
+      col_own[j] = (rl * 2 * kDim + 16 * (seg ^ wide_mix(rl)) + 8 * (jj & 1)) ^ 32 * j;
+    }
+#pragma unroll
+    for (int j = 0; j < kHalfAt; ++j) {
+      row_rot[j] = n * 2 * kRot + 16 * (h ^ half_mix(n)) ^ 32 * j;
+      col_rot[j] = (rl * 2 * kRot + 16 * (seg ^ half_mix(rl)) + 8 * (jj & 1)) ^ (64 * (j >> 1) + 16 * (j & 1));
+    }
   }
+  // (KEYS) the rows', the columns' addresses on to another buffer
+  auto move = [&](uint32_t (&wide)[kWideAt], uint32_t (&half)[kHalfAt], int from, int to) __attribute__((always_inline)) {
+    if constexpr (KEYS) {
+      const int by = (to - from) * static_cast<int>(sizeof(Tile));
+#pragma unroll
+      for (int j = 0; j < kWideAt; ++j) {
+        wide[j] += by;
+        asm volatile("" : "+v"(wide[j]));
+      }
+#pragma unroll
+      for (int j = 0; j < kHalfAt; ++j) {
+        half[j] += by;
+        asm volatile("" : "+v"(half[j]));
+      }
+    }
+  };
   auto tr8 = [](const char* p0, const char* p1) {
     const uint2 y0 = lds_tr4(reinterpret_cast<const uint16_t*>(p0)), y1 = lds_tr4(reinterpret_cast<const uint16_t*>(p1));
     return __builtin_bit_cast(bf16x8, make_uint4(y0.x, y0.y, y1.x, y1.y));
@@ -258,27 +308,57 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     for (int nt = 0; nt < NT; ++nt) acc[i][nt] = f32x16{};
   bf16x8 ps[NT][2], pp[NT][2];                           // pending dS and (KEYS) P of 32 streamed rows, as B operands
 
+  // a statistic's three parts are elements 0 .. 2 of the lanes h = 0
+  const bf16x8 ones = __builtin_bit_cast(bf16x8, h == 0 ? make_uint4(0x3F803F80u, 0x3F80u, 0, 0) : make_uint4(0, 0, 0, 0));
+  // (KEYS) Each phase reads the first kAhead operands of the next in its last slots, where these are there: the reads'
+  // time is bare else.  (Of the queries' kernel, with products enough, it takes 3 % more time.)
+  bf16x8 pre[kAhead];
+  // operands of the products of rows 32 half .. + 31, and of the additions of those rows
+  auto read_row = [&](int buf, int half, int j) __attribute__((always_inline)) -> bf16x8 {
+    const char* t = reinterpret_cast<const char*>(&ring[KEYS ? 0 : buf]);
+    const int k = j < KS ? j : j - KS;             // 16 dimensions; KO .. KS - 1 of the shared part
+    uint32_t at;
+    if constexpr (KEYS) {
+      at = k < KO ? row_own[k < KO ? k : 0] : row_rot[k < KO ? 0 : k - KO];
+    } else {
+      at = (k < KO ? row_own[0] : row_rot[0]) ^ 32 * (k < KO ? k : k - KO);
+    }
+    t += k < KO ? (j < KS ? kOwnAt : kOtherAt) + half * 32 * 2 * kDim : kRotAt + half * 32 * 2 * kRot;
+    return ld_bf16x8(reinterpret_cast<const uint16_t*>(t + at));
+  };
+  auto read_col = [&](int buf, int half, int j) __attribute__((always_inline)) -> bf16x8 {
+    const char* t = reinterpret_cast<const char*>(&ring[KEYS ? 0 : buf]);
+    const int u = j / NA, i = j % NA;              // 16 streamed rows, accumulator tile
+    const int r = 32 * half + 16 * u;
+    const bool wide = i < KO / 2 || i >= ND;
+    const int k = i < KO / 2 ? i : i < ND ? i - KO / 2 : i - ND;
+    uint32_t at0, at1;
+    if constexpr (KEYS) {
+      at0 = wide ? col_own[wide ? 2 * k : 0] : col_rot[wide ? 0 : 2 * k];
+      at1 = wide ? col_own[wide ? 2 * k + 1 : 0] : col_rot[wide ? 0 : 2 * k + 1];
+    } else {
+      at0 = (wide ? col_own[0] : col_rot[0]) ^ 64 * k;
+      at1 = at0 ^ (wide ? 32 : 16);
+    }
+    t += wide ? (i < ND ? kOwnAt : kOtherAt) + r * 2 * kDim : kRotAt + r * 2 * kRot;
+    return tr8(t + at0, t + at1 + 8 * (wide ? 2 * kDim : 2 * kRot));
+  };
   // both score products of streamed rows 32 half .. + 31: lane (n, h) gets rows 8(i/4) + 4h + i%4 against its own
   auto products = [&](int buf, int half, f32x16 (&z)[NT], f32x16 (&dz)[NT], auto beside) __attribute__((always_inline)) {
-    const char* t = reinterpret_cast<const char*>(&ring[buf]);
-    const char* t_own = t + kOwnAt + half * 32 * 2 * kDim;
-    const char* t_rot = t + kRotAt + half * 32 * 2 * kRot;
-    const char* t_other = t + kOtherAt + half * 32 * 2 * kDim;
-    uint32_t at_own = row_own, at_rot = row_rot;
-    asm volatile("" : "+v"(at_own), "+v"(at_rot));   // as above
-    auto read = [&](int j) -> bf16x8 {
-      const char* p = j < KO ? t_own + (at_own ^ (32 * j)) : j < KS ? t_rot + (at_rot ^ (32 * (j - KO)))
-                                                                     : t_other + (at_own ^ (32 * (j - KS)));
-      return ld_bf16x8(reinterpret_cast<const uint16_t*>(p));
-    };
+    if constexpr (!KEYS) asm volatile("" : "+v"(row_own[0]), "+v"(row_rot[0]));    // as above
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) z[nt] = dz[nt] = f32x16{};
+    if constexpr (KEYS) {
+      const uint4 x = stat[buf][32 * half + n];
+      z[0] = mfma32x32x16(__builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, 0, 0)), ones, z[0]);
+      dz[0] = mfma32x32x16(__builtin_bit_cast(bf16x8, make_uint4(x.z, x.w, 0, 0)), ones, dz[0]);
+    }
     bf16x8 op[KS + KO];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) op[j] = read(j);
+    for (int j = 0; j < kAhead; ++j) op[j] = KEYS ? pre[j] : read_row(buf, half, j);
 #pragma unroll
     for (int j = 0; j < KS + KO; ++j) {
-      if (j + kAhead < KS + KO) op[j + kAhead] = read(j + kAhead);
+      if (j + kAhead < KS + KO) op[j + kAhead] = read_row(buf, half, j + kAhead);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         if (j < KS) z[nt] = mfma32x32x16(op[j], b1[nt][j < KS ? j : 0], z[nt]);
@@ -290,28 +370,14 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   };
   // adds the pending weights' products with their streamed rows; beside(j) after the j-th slot
   constexpr int kSlots = 2 * NA;
-  auto additions = [&](int buf, int half, auto beside) {
-    const char* t = reinterpret_cast<const char*>(&ring[buf]);
-    uint32_t at_own = col_own, at_rot = col_rot;
-    asm volatile("" : "+v"(at_own), "+v"(at_rot));   // as above
-    auto read = [&](int j) -> bf16x8 {
-      const int u = j / NA, i = j % NA;            // 16 streamed rows, accumulator tile
-      const int r = 32 * half + 16 * u;
-      if (i < KO / 2 || i >= ND) {
-        const char* p = t + (i < ND ? kOwnAt : kOtherAt) + r * 2 * kDim;
-        const uint32_t at = at_own ^ (64 * (i < ND ? i : i - ND));
-        return tr8(p + at, p + (at ^ 32) + 8 * 2 * kDim);
-      }
-      const char* p = t + kRotAt + r * 2 * kRot;
-      const uint32_t at = at_rot ^ (64 * (i - KO / 2));
-      return tr8(p + at, p + (at ^ 16) + 8 * 2 * kRot);
-    };
+  auto additions = [&](int buf, int half, auto beside) __attribute__((always_inline)) {
+    if constexpr (!KEYS) asm volatile("" : "+v"(col_own[0]), "+v"(col_rot[0]));    // as above
     bf16x8 op[kSlots];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) op[j] = read(j);
+    for (int j = 0; j < kAhead; ++j) op[j] = KEYS ? pre[j] : read_col(buf, half, j);
 #pragma unroll
     for (int j = 0; j < kSlots; ++j) {
-      if (j + kAhead < kSlots) op[j + kAhead] = read(j + kAhead);
+      if (j + kAhead < kSlots) op[j + kAhead] = read_col(buf, half, j + kAhead);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
         acc[j % NA][nt] = mfma32x32x16(op[j], j % NA < ND ? ps[nt][j / NA] : pp[nt][j / NA], acc[j % NA][nt]);
@@ -321,18 +387,15 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   };
   // P and dS of 32 streamed rows in kSlots pieces: z becomes P, dz dS.  The last two pieces pack them, each after the
   // last slot that adds what was there before.
-  f32x4 row_lse{}, row_d{};
+  const float far = copysignf(kFar, a.scale_log2);
   const int edge = (KEYS ? w0 + n - base_p : base_p + w0 + n) - 4 * h;
-  auto expo = [&](int buf, int row, auto masked, f32x16 (&z)[NT], int i) __attribute__((always_inline)) {
-    if constexpr (KEYS) {
-      if (i % 4 == 0) row_lse = *reinterpret_cast<const f32x4*>(&stat[buf][0][(row & (kRowsT - 1)) + 8 * (i / 4) + 4 * h]);
-    }
+  auto expo = [&](int row, auto masked, f32x16 (&z)[NT], int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float p = exp2_hw(fmaf(z[nt][i], a.scale_log2, KEYS ? -row_lse[i % 4] : -lane_lse[nt]));
-      if constexpr (decltype(masked)::value) {
+      float p = exp2_hw(KEYS ? z[nt][i] * a.scale_log2 : fmaf(z[nt][i], a.scale_log2, -lane_lse[nt]));
+      if constexpr (!KEYS && decltype(masked)::value) {
         const int y = 8 * (i / 4) + i % 4;         // of the streamed row, less row + 4 h
-        p = (KEYS ? y >= edge - row : y <= edge + 32 * nt - row) ? p : 0.f;
+        p = y <= edge + 32 * nt - row ? p : 0.f;
       }
       z[nt][i] = p;
     }
@@ -341,24 +404,21 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   // products do not cover all the work on 32 x 64 weights (8K rows of one sequence: 1.90 ms; with none 1.96, with 16
   // the same), those of 20 cover the work on 32 x 32.
   constexpr int kEarly = KEYS ? 0 : 12;
-  auto early = [&](int buf, int row, auto masked, f32x16 (&z)[NT], int j) __attribute__((always_inline)) {
+  auto early = [&](int row, auto masked, f32x16 (&z)[NT], int j) __attribute__((always_inline)) {
     constexpr int kFirst = KS + 1, kMany = KO - 1;
 #pragma unroll
     for (int i = 0; i < kEarly; ++i)
-      if (j == kFirst + i * kMany / max(kEarly, 1)) expo(buf, row, masked, z, i);
+      if (j == kFirst + i * kMany / max(kEarly, 1)) expo(row, masked, z, i);
   };
-  auto weigh = [&](int buf, int row, auto masked, f32x16 (&z)[NT], f32x16 (&dz)[NT], int j) __attribute__((always_inline)) {
+  auto weigh = [&](int row, auto masked, f32x16 (&z)[NT], f32x16 (&dz)[NT], int j) __attribute__((always_inline)) {
     constexpr int kLast = kSlots - 2;
     static_assert(kLast >= NA, "");
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (i * kLast / 16 != j) continue;
-      if constexpr (KEYS) {
-        if (i % 4 == 0) row_d = *reinterpret_cast<const f32x4*>(&stat[buf][1][(row & (kRowsT - 1)) + 8 * (i / 4) + 4 * h]);
-      }
-      if (i >= kEarly) expo(buf, row, masked, z, i);
+      if (i >= kEarly) expo(row, masked, z, i);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) dz[nt][i] = z[nt][i] * (dz[nt][i] - (KEYS ? row_d[i % 4] : lane_d[nt]));
+      for (int nt = 0; nt < NT; ++nt) dz[nt][i] = z[nt][i] * (KEYS ? dz[nt][i] : dz[nt][i] - lane_d[nt]);
     }
     if (j >= kLast) {
       const int u = j - kLast;
@@ -377,16 +437,24 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
       }
     }
   };
-  // whether some lane of the wave does not meet some row of tile b (rows past the queries' end aside, see below)
-  auto is_masked = [&](int b) {
-    return KEYS ? base_p + b * kRowsT < w0 + 32 * NT - 1 : (b + 1) * kRowsT > base_p + w0 + 1;
+  // (queries) whether some lane of the wave does not meet some row of tile b
+  auto is_masked = [&](int b) { return (b + 1) * kRowsT > base_p + w0 + 1; };
+  // (KEYS) the scores of streamed rows, from row on, that a key does not meet; the branch is free, two loops spill
+  auto mask = [&](int row, f32x16 (&z)[NT]) __attribute__((always_inline)) {
+    if constexpr (!KEYS) return;
+    if (base_p + row >= w0 + 31) return;
+    const int first = edge - row;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[0][i] = 8 * (i / 4) + i % 4 >= first ? z[0][i] : -far;
+    asm volatile("" : "+v"(z[0]));
   };
   auto sync = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-  // tile b's copies, all waves'; queries past the end get an LSE of +infinity, and so no weight
+  // tile b's copies, all waves'; queries past the end get no weight
   auto arrive = [&](int b, int buf) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if constexpr (KEYS) {
-      if ((b + 1) * kRowsT > streamed && (wave & 1) == 0 && b * kRowsT + lane >= streamed) stat[buf][0][lane] = INFINITY;
+      if ((b + 1) * kRowsT > streamed && b * kRowsT + lane >= streamed)
+        stat[buf][lane] = make_uint4(a.scale_log2 < 0 ? 0x7B80u : 0xFB80u, 0, 0, 0);     // kFar, of -scale's sign
     }
     sync();
   };
@@ -394,39 +462,68 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   if (b_begin < b_end) {
     arrive(b_begin, 0);
     f32x16 z[NT], dz[NT];
-    products(0, 0, z, dz, [&](int j) __attribute__((always_inline)) { early(0, b_begin * kRowsT, std::true_type{}, z, j); });
+    // the first operands of the products, of the additions that come next: behind slot j of j_end
+    auto rows_next = [&](int buf, int half, int j, int j_end) __attribute__((always_inline)) {
+      if (KEYS && j >= j_end - kAhead) pre[j - (j_end - kAhead)] = read_row(buf, half, j - (j_end - kAhead));
+    };
+    auto cols_next = [&](int buf, int half, int j, int j_end) __attribute__((always_inline)) {
+      if (KEYS && j >= j_end - kAhead) pre[j - (j_end - kAhead)] = read_col(buf, half, j - (j_end - kAhead));
+    };
 #pragma unroll
-    for (int j = 0; j < kSlots; ++j) weigh(0, b_begin * kRowsT, std::true_type{}, z, dz, j);
+    for (int j = 0; j < kAhead; ++j) rows_next(0, 0, j, kAhead);
+    products(0, 0, z, dz, [&](int j) __attribute__((always_inline)) {
+      early(b_begin * kRowsT, std::true_type{}, z, j);
+      rows_next(0, 1, j, KS + KO);
+    });
+    mask(b_begin * kRowsT, z);
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j) weigh(b_begin * kRowsT, std::true_type{}, z, dz, j);
     // Rows 32 .. 63 of tile b, then rows 0 .. 31 of tile b + 1: the products of these, the additions of those before.
     // Behind the barrier tile b + 1 is there and tile b - 1's readers are done: its buffer takes tile b + 2,
     // whose copies go out between the products.  (Behind the last tiles they repeat the last one.)
     int b = b_begin, buf = 0;
+    auto first = [&](auto masked) __attribute__((always_inline)) {
+      products(buf, 1, z, dz, [&](int j) __attribute__((always_inline)) {
+        early(b * kRowsT + 32, masked, z, j);
+        cols_next(buf, 0, j, KS + KO);
+      });
+      mask(b * kRowsT + 32, z);
+    };
     auto step = [&](auto masked) __attribute__((always_inline)) {
       const int next = buf == kRing - 1 ? 0 : buf + 1;
-      products(buf, 1, z, dz, [&](int j) __attribute__((always_inline)) { early(buf, b * kRowsT + 32, masked, z, j); });
-      additions(buf, 0, [&](int j) __attribute__((always_inline)) { weigh(buf, b * kRowsT + 32, masked, z, dz, j); });
+      first(masked);
+      additions(buf, 0, [&](int j) __attribute__((always_inline)) { weigh(b * kRowsT + 32, masked, z, dz, j); });
       arrive(b + 1, next);
+      move(row_own, row_rot, buf, next);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) rows_next(next, 0, j, kAhead);
       const From f = source(min(b + 2, b_end - 1), buf == 0 ? kRing - 1 : buf - 1);
       int ln = lane;
       asm volatile("" : "+v"(ln));
+      if (f.last < kRowsT - 1) hold(f.last);
       products(next, 0, z, dz, [&](int j) __attribute__((always_inline)) {
         if (j % 2 == 1 && j / 2 < kAllCopies) copy_piece(f, j / 2, ln);
-        early(next, (b + 1) * kRowsT, masked, z, j);
+        early((b + 1) * kRowsT, masked, z, j);
+        cols_next(buf, 1, j, KS + KO);
       });
       if constexpr (kAllCopies > (KS + KO) / 2) copy_piece(f, kAllCopies - 1, ln);
-      additions(buf, 1, [&](int j) __attribute__((always_inline)) { weigh(next, (b + 1) * kRowsT, masked, z, dz, j); });
+      mask((b + 1) * kRowsT, z);
+      additions(buf, 1, [&](int j) __attribute__((always_inline)) {
+        weigh((b + 1) * kRowsT, masked, z, dz, j);
+        rows_next(next, 1, j, kSlots);
+      });
+      move(col_own, col_rot, buf, next);
       ++b;
       buf = next;
     };
-    if constexpr (KEYS) {
-      while (b + 1 < b_end && (is_masked(b) || is_masked(b + 1))) step(std::true_type{});
-      while (b + 1 < b_end) step(std::false_type{});
-    } else {
+    if constexpr (!KEYS)
       while (b + 1 < b_end && !is_masked(b + 1)) step(std::false_type{});
-      while (b + 1 < b_end) step(std::true_type{});
-    }
-    products(buf, 1, z, dz, [&](int j) __attribute__((always_inline)) { early(buf, b * kRowsT + 32, std::true_type{}, z, j); });
-    additions(buf, 0, [&](int j) __attribute__((always_inline)) { weigh(buf, b * kRowsT + 32, std::true_type{}, z, dz, j); });
+    while (b + 1 < b_end) step(std::true_type{});
+    first(std::true_type{});
+    additions(buf, 0, [&](int j) __attribute__((always_inline)) {
+      weigh(b * kRowsT + 32, std::true_type{}, z, dz, j);
+      cols_next(buf, 1, j, kSlots);
+    });
     additions(buf, 1, [](int) {});
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // the ring is used again below
   }
@@ -538,7 +635,7 @@ int validate_backward(const msa_seqs* seqs, int H) {
   if (seqs->total_q_rows * H >= (int64_t(1) << 31) || seqs->total_kv_rows * H >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
   return MSA_OK;
 }
-size_t stat_bytes(const msa_seqs* s, int H) { return msa_host::align_up(sizeof(float) * 2 * H * s->total_q_rows, 256); }
+size_t stat_bytes(const msa_seqs* s, int H) { return msa_host::align_up(sizeof(uint4) * H * s->total_q_rows, 256); }
 size_t work_bytes(const msa_seqs* s, int H) { return stat_bytes(s, H) + sizeof(float) * kRot * H * s->total_kv_rows; }
 
 bool aligned(const void* p, int by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) == 0; }
@@ -599,11 +696,12 @@ extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t
   a.d_e = Grad{static_cast<uint16_t*>(d_q_rope), d_q_rope_stride, d_q_rope_head_stride};
   a.d_k = Grad{dkv, kv_row, kPair};
   a.d_v = Grad{dkv + kDim, kv_row, kPair};
-  a.stat = static_cast<float*>(workspace);
+  a.stat = static_cast<uint4*>(workspace);
   a.d_r = reinterpret_cast<float*>(static_cast<char*>(workspace) + stat_bytes(seqs, H));
   a.H = H;
   a.scale = softmax_scale;
   a.scale_log2 = softmax_scale * kLog2E;
+  if (std::fabs(a.scale_log2) < kLeast) a.scale_log2 = kLeast;
   int64_t tiles;
   const flash::Grid gr = flash::plan_grid(seqs, kRowTile, seqs->max_q_rows, &tiles);
   const int64_t key_tiles = seqs->num_seqs == 1 ? (std::min<int64_t>(seqs->max_kv_len, N) + kKeyTile - 1) / kKeyTile
