@@ -472,8 +472,9 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_kernel(const float* __
 // ---------------------------------------------------------------- latent cache rows
 // A row of the latent cache: the norm of the token's latent (R elements, a wave
 // with R / 64 each) and its shared key part, rotated (64 elements, one pair for
-// each of 32 lanes).  A wave takes every fourth of the CTA's rows; their elements
-// are requested before the rows are located.
+// each of 32 lanes).  A wave takes two rows at a time, since one row's pairs would
+// leave half of its lanes idle through the angles' sines, the longest part of the
+// arithmetic; their elements are requested before the rows are located.
 template <int R>
 __global__ __launch_bounds__(kThreads) void latent_append_kernel(const uint16_t* __restrict__ latent, int64_t latent_stride,
                                                                  const uint16_t* __restrict__ k_rope, int64_t k_rope_stride,
@@ -485,22 +486,26 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(const uint16_t*
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows;
   const int n = static_cast<int>(min(static_cast<int64_t>(rows), sq.total_q_rows - row0));
   const int lane = lane_id(), wave = threadIdx.x / kWave;
-  // the lane's pair (lanes below 32): rotated ones first, then the rest of the part
-  const int i = lane & 31;
+  // the lane's pair of row r + lane / 32: rotated ones first, then the rest of the part
+  const int i = lane & 31, mine = lane >> 5;
   const bool turned = i < sp.pairs;
   const int a = !turned ? 2 * i : sp.inter ? 2 * i : i;
   const int b = !turned || sp.inter ? a + 1 : sp.pairs + i;
-  uint2 x[2];                            // 8 or 4 elements
+  constexpr int kStep = 2 * kThreads / kWave;
+  uint2 x[2][2];                         // 8 or 4 elements of each row
   uint32_t ka = 0, kb = 0;
   auto load = [&](int r) {
-    const uint16_t* src = latent + (row0 + r) * latent_stride + N * lane;
-    x[0] = *reinterpret_cast<const uint2*>(src);
-    if constexpr (N == 8) x[1] = *reinterpret_cast<const uint2*>(src + 4);
-    const uint16_t* kr = k_rope + (row0 + r) * k_rope_stride;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {        // a row past the CTA's last is its last again
+      const uint16_t* src = latent + (row0 + min(r + j, n - 1)) * latent_stride + N * lane;
+      x[j][0] = *reinterpret_cast<const uint2*>(src);
+      if constexpr (N == 8) x[j][1] = *reinterpret_cast<const uint2*>(src + 4);
+    }
+    const uint16_t* kr = k_rope + (row0 + min(r + mine, n - 1)) * k_rope_stride;
     ka = kr[a];
     kb = kr[b];
   };
-  int r = wave;
+  int r = 2 * wave;
   if (r < n) load(r);
   if (threadIdx.x < kWave) locate_rows(sq, row0, n, pos, dst);
   float w[N];
@@ -508,12 +513,14 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(const uint16_t*
   for (int c = 0; c < N; ++c) w[c] = weight ? weight[N * lane + c] : 1.f;
   const double freq = turned ? sp.freq[i] : 0.0;
   __syncthreads();
-  for (; r < n; r += kThreads / kWave) {
-    const int64_t to = dst[r];
-    if (to >= 0) {                       // the same in every lane
-      float u[4], v[4] = {}, ra = __uint_as_float(ka << 16), rb = __uint_as_float(kb << 16);
-      unpack4(x[0], u);
-      if constexpr (N == 8) unpack4(x[1], v);
+  for (; r < n; r += kStep) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t to = r + j < n ? dst[r + j] : -1;
+      if (to < 0) continue;              // the same in every lane
+      float u[4], v[4] = {};
+      unpack4(x[j][0], u);
+      if constexpr (N == 8) unpack4(x[j][1], v);
       if (weight) {
         float ss = 0.f;
 #pragma unroll
@@ -528,8 +535,24 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(const uint16_t*
           if constexpr (N == 8) v[c] = v[c] * rstd * w[4 + c];
         }
       }
+      const int64_t at = to * (R + kRot) + N * lane;
+      if (code.on) {
+        uint8_t* y = static_cast<uint8_t*>(cache) + at;
+        *reinterpret_cast<uint32_t*>(y) = code4(u, code);
+        if constexpr (N == 8) *reinterpret_cast<uint32_t*>(y + 4) = code4(v, code);
+      } else {
+        // elements that nothing is applied to keep their bits (NaN payloads too)
+        uint16_t* y = static_cast<uint16_t*>(cache) + at;
+        *reinterpret_cast<uint2*>(y) = weight ? pack4(u) : x[j][0];
+        if constexpr (N == 8) *reinterpret_cast<uint2*>(y + 4) = weight ? pack4(v) : x[j][1];
+      }
+    }
+    const int rr = r + mine;
+    const int64_t to = rr < n ? dst[rr] : -1;
+    if (to >= 0) {
+      float ra = __uint_as_float(ka << 16), rb = __uint_as_float(kb << 16);
       if (turned) {
-        double turns = static_cast<double>(pos[r]) * freq * 0.15915494309189533577;   // 1 / (2 pi)
+        double turns = static_cast<double>(pos[rr]) * freq * 0.15915494309189533577;   // 1 / (2 pi)
         turns -= rint(turns);
         float s, c;
         sincospif(2.f * static_cast<float>(turns), &s, &c);
@@ -539,30 +562,21 @@ __global__ __launch_bounds__(kThreads) void latent_append_kernel(const uint16_t*
         rb = fmaf(rb, c, ra * s);
         ra = y;
       }
-      const int64_t at = to * (R + kRot);
+      const int64_t at = to * (R + kRot) + R;
       if (code.on) {
-        uint8_t* y = static_cast<uint8_t*>(cache) + at;
-        *reinterpret_cast<uint32_t*>(y + N * lane) = code4(u, code);
-        if constexpr (N == 8) *reinterpret_cast<uint32_t*>(y + N * lane + 4) = code4(v, code);
         const float pair[4] = {ra, rb, 0.f, 0.f};
         const uint32_t cd = code4(pair, code);
-        if (lane < 32) {
-          y[R + a] = static_cast<uint8_t>(cd);
-          y[R + b] = static_cast<uint8_t>(cd >> 8);
-        }
+        uint8_t* y = static_cast<uint8_t*>(cache) + at;
+        y[a] = static_cast<uint8_t>(cd);
+        y[b] = static_cast<uint8_t>(cd >> 8);
       } else {
-        // elements that nothing is applied to keep their bits (NaN payloads too)
-        uint16_t* y = static_cast<uint16_t*>(cache) + at;
-        *reinterpret_cast<uint2*>(y + N * lane) = weight ? pack4(u) : x[0];
-        if constexpr (N == 8) *reinterpret_cast<uint2*>(y + N * lane + 4) = weight ? pack4(v) : x[1];
         const uint32_t pr = turned ? pack_bf16x2(ra, rb) : (ka | (kb << 16));
-        if (lane < 32) {
-          y[R + a] = static_cast<uint16_t>(pr);
-          y[R + b] = static_cast<uint16_t>(pr >> 16);
-        }
+        uint16_t* y = static_cast<uint16_t*>(cache) + at;
+        y[a] = static_cast<uint16_t>(pr);
+        y[b] = static_cast<uint16_t>(pr >> 16);
       }
     }
-    if (r + kThreads / kWave < n) load(r + kThreads / kWave);
+    if (r + kStep < n) load(r + kStep);
   }
 }
 
@@ -729,6 +743,9 @@ int kv_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, 
 
 // Rows per CTA: four, one per wave, while there are more than 2048 CTAs (all that
 // run at once), else one, so that few rows spread over the chip.
+// Rows are located once per CTA, so there are few CTAs: 512 take 13.5 us for 18000 rows
+// of 512 elements into E4M3 (launch and events included), 1024 14.2, 2048 16.4, 4096 24.
+constexpr int64_t kLatentCtas = 512;
 int latent_append(const void* latent, int64_t latent_stride, const void* k_rope, int64_t k_rope_stride, bool fp8, float scale,
                   const msa_seqs* seqs, int R, const float* weight, float eps, const msa_rope* rope, void* cache,
                   hipStream_t stream) {
@@ -747,7 +764,7 @@ int latent_append(const void* latent, int64_t latent_stride, const void* k_rope,
   if (!aligned8(cache)) return MSA_ERR_UNSUPPORTED;
   const int64_t total = seqs->total_q_rows;
   int rows = 1;
-  while (rows < kMaxRows && (total + rows - 1) / rows > kCtas) rows *= 2;
+  while (rows < kMaxRows && (total + rows - 1) / rows > kLatentCtas) rows *= 2;
   const int64_t ctas = (total + rows - 1) / rows;
   if (ctas >= (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;          // a grid's limit
   const Code code = fp8 ? code_of(scale) : Code{};
