@@ -17,6 +17,9 @@
 // Few tiles: the steps (64 keys of a tile) of a head's tiles are dealt out evenly
 // over the chip (latent_steps.h), shared tiles leave their parts in fp32, and
 // latent_join_kernel joins them by the log-sum-exp rule in key order.
+//
+// Bound: matrix products.  8192 rows of 64 heads take 1264 us, 1.09 PFLOP/s (1145 us at
+// the rate of a large product); 2 x 512 rows on 16K keys 655 - 720 by the card (556).
 #include <initializer_list>
 #include <type_traits>
 
@@ -44,7 +47,9 @@ using steps::tile_geom;
 constexpr int kRot = 64;                 // elements of the shared key part
 constexpr int kPair = 2 * kDim;          // a key's own part and its values
 constexpr float kSlack = 8.f;
-constexpr int kMinSteps = 4;             // per share, where there are few
+// Steps per share, where there are few.  2 x 100 rows of 8 heads on 3000 keys, kernel and join with their launches:
+// 28.5 us with 2, 28.0 with 4, 29.7 with 8.
+constexpr int kMinSteps = 4;
 constexpr int kHeld = 256;               // CTAs of 8 waves that the chip holds
 
 struct ExpandedPlan {
@@ -477,15 +482,16 @@ int validate_expanded(const msa_seqs* seqs, int H) {
 // Waves per CTA (one CTA of 8 per CU, or two of 4), and whether the steps are
 // dealt out or each tile has a CTA: what takes least by the sizes.  A step of a
 // full tile of 8 waves takes 2.66 us, of 4 waves 1.25 alone on a CU and 2.8 with
-// another beside it; shares cost 18 us more for their ends, parts and join.  Tiles
+// another beside it; shares cost 7 % more a step and 18 us for their ends, parts and join.  Tiles
 // of a prompt see half of its keys on average, those of a chunk far behind a
 // context all, so they end in rounds.  (The lengths are on the device; the key
 // side's rows tell their mean where sequences lie one behind another.)
 // Measured, us, 8 waves / 4 waves / shares: one prompt of 777 rows, 20 heads 32.9 /
 // 23.5 / 30.9, 2000, 32 heads 73 / 61 / 88, 8000, 8 heads 236 / 200 / 211, 8192, 64
 // heads 1282 / 1296 / 1380; 20 documents of 100 - 1000 rows, 32 heads 81 / 66 / 113;
-// 2 x 512 rows on 16K keys, 64 heads 666 / 698 / 709; 2 x 500 on 8K, 20 heads 245 /
-// 183 / 125; 64 on 12K, 8 heads 207 / 226 / 33.
+// 2 x 512 rows on 16K keys, 64 heads 666 / 698 / 709, on 14 - 16K (another card) 720 /
+// - / 756; 2 x 500 on 8K, 20 heads 245 / 183 / 125; 64 on 12K, 8 heads 207 / 226 / 33.
+constexpr double kShareStep = 1.07;
 ExpandedPlan plan_of(const msa_seqs* seqs, int H, int* waves, int64_t* ctas) {
   const double rows = seqs->max_q_rows, keys = seqs->max_kv_len, seq_count = seqs->num_seqs;
   const bool chunk = 2 * rows <= keys;
@@ -508,7 +514,7 @@ ExpandedPlan plan_of(const msa_seqs* seqs, int H, int* waves, int64_t* ctas) {
   }
   // (shares have the last tiles' live waves alone to pay for)
   const double filled = std::min(u8, (seqs->total_q_rows / 32 + seq_count) / 8 * H);
-  const double shares = filled / kHeld * avg * (rows >= 256 ? 2.66 : t8) * mean + 18;
+  const double shares = filled / kHeld * avg * (rows >= 256 ? 2.66 : t8) * kShareStep * mean + 18;
   ExpandedPlan pl{};
   *waves = 8;
   if (H <= kHeld && shares < std::min(whole8, whole4)) {

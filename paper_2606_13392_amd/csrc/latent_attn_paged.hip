@@ -21,6 +21,16 @@
 // out evenly over the chip; a CTA forms the numbering from the lengths on the
 // device.  Where a tile is shared by several CTAs each leaves its part in fp32,
 // and latent_merge_kernel joins them by the log-sum-exp rule in key order.
+//
+// Bound: 64 heads of one token do 130 operations for each byte of a bf16 cache, so
+// memory and products both count.  32 tokens of 64 heads on 4K - 60K keys take 147 us
+// (123 at the rate of a large copy): a step of 72 KiB takes 7100 clocks, 2200 of them
+// waiting for memory, 5.1 TB/s while the steps run, the rest the start and the merge.
+// Elsewhere a step's own work bounds, some 4900 clocks, of which the matrix units are
+// busy 2180: a CTA has its CU alone (two buffers of keys fill the LDS, O and Q the
+// registers), so nothing runs under the softmax, the barriers and the copies' issue.
+// Four chunks of 20 - 150 rows of 32 heads, R = 256: 78 us (30 at the rate of a large
+// product); one token on 8K keys 21 us, of which the steps are 5.
 #include <initializer_list>
 #include <type_traits>
 
@@ -46,9 +56,12 @@ constexpr int kRows = 64;                // (row, head) pairs per tile
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kCtas = 256;               // one per CU: two buffers of keys fill its LDS
+// The merge of 32 tokens on 4K - 60K keys takes 17.3 us with 256 CTAs, 13.1 with 1024, 13.2 with 4096.
 constexpr int kMergeCtas = 1024;
-constexpr int kMinSteps = 2;             // steps per CTA, where there are few
-constexpr float kSlack = 8.f;
+// Steps per CTA, where there are few.  One token of 64 heads on 8K keys, kernel and merge with their launches: 31.5 us
+// with 1 (the merge has twice the parts), 28.0 with 2, 28.7 with 4.
+constexpr int kMinSteps = 2;
+constexpr float kSlack = 8.f;            // see the maxima below
 constexpr int kAheadK = 6, kAheadV = 3;  // LDS operands requested so many products ahead
 
 // A cache row in LDS: 16-byte segments, the low three bits of their number
@@ -354,7 +367,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       // The maxima that the weights are relative to move only when one is outgrown by 2^kSlack: among 64 rows
       // some true maximum moves in most steps, and each time O would be rescaled (384 instructions a wave at
-      // R = 512).  Weights stay below 2^kSlack, exact powers of two apart from the usual ones.
+      // R = 512; 32 tokens on 4K - 60K keys 171 us instead of 149, chunks at R = 256 87 instead of 77).  Weights stay
+      // below 2^kSlack, and their sums far from fp32's ends.
       float alpha[2] = {1.f, 1.f}, neg[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -488,9 +502,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
 // LSE = a + log sum 2^(LSE_c - a), O = sum 2^(LSE_c - LSE) O_c.  A CTA forms the
 // list of such tiles and takes every gridDim.x-th share of them.  Of many tiles a
 // wave joins the parts of a piece, 4 dimensions of 32 rows in each half of it; of
-// few the CTA's four waves have every fourth part, in order, and join in LDS.  (A
-// CTA per share and piece, most of them without a tile, took 16 us for one token
-// on 8209 keys, this 5.)
+// few the CTA's four waves have every fourth part, in order, and join in LDS.  One
+// tile of 65 parts takes 7.8 us by the second way and 11.9 by the first, 8 sequences'
+// draft rows of 128 heads (16 tiles and more) 16.0 and 11.1, 32 tokens 17.7 and 13.0.
 constexpr int kManyTiles = 16;
 template <int R>
 __global__ __launch_bounds__(kThreads) void latent_merge_kernel(msa_seqs sq, LatentPlan pl, LatentParts parts, int H,
