@@ -581,7 +581,8 @@ int msa_latent_attn_paged_fp8(const void* q, int64_t q_stride, int64_t q_head_st
  *
  * Supported: num_heads <= 256; contiguous key side; total_q_rows * num_heads < 2^31;
  * strides a multiple of 8 elements, k_rope_stride at most 2^20; tensors 16-byte
- * aligned (else MSA_ERR_UNSUPPORTED).  The query may give 0: then the workspace is
+ * aligned; (total_q_rows / 32 + 8 num_seqs) num_heads < 2^26, a grid's limit (else
+ * MSA_ERR_UNSUPPORTED).  The query may give 0: then the workspace is
  * not read and may be NULL.
  * ------------------------------------------------------------------------ */
 size_t msa_latent_attn_workspace_size(const msa_seqs* seqs, int num_heads);
@@ -614,7 +615,8 @@ int msa_latent_attn(const void* q, int64_t q_stride, int64_t q_head_stride, cons
  * bit-reproducible.  Key ranges of different sequences must not overlap (the
  * gradients of shared rows are unspecified).  No output may alias an input.
  *
- * Supported: as msa_latent_attn, with total_kv_rows * num_heads < 2^31, q_stride,
+ * Supported: as msa_latent_attn, with total_kv_rows * num_heads < 2^31, (the larger of
+ * total_q_rows / 256 and total_kv_rows / 128, + num_seqs) num_heads < 2^24, q_stride,
  * q_rope_stride and k_rope_stride at most 2^24, d_q and d_q_rope 8-byte aligned with
  * strides a multiple of 4 elements.
  * ------------------------------------------------------------------------ */

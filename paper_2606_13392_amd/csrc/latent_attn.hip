@@ -563,7 +563,7 @@ extern "C" int msa_latent_attn(const void* q, int64_t q_stride, int64_t q_head_s
   int waves;
   int64_t ctas;
   const ExpandedPlan pl = plan_of(seqs, num_heads, &waves, &ctas);
-  if (ctas >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
+  if (ctas * waves >= (int64_t(1) << 26)) return MSA_ERR_UNSUPPORTED;    // a grid's limit
   ExpandedParts parts{};
   if (pl.ranges > 0) {
     if (!workspace || workspace_bytes < part_bytes(ctas, waves)) return MSA_ERR_WORKSPACE;

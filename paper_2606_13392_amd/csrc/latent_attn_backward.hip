@@ -603,36 +603,38 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
 }
 
 // The shared part's gradient: the heads' sums, added in their order, times the
-// scale.  A wave takes a key row, one element per lane.  Rows that no sequence
+// scale.  A wave takes key rows, one element per lane.  Rows that no sequence
 // owns get zeros, in d_kv too.
+constexpr int64_t kSumCtas = 1 << 20;
 __global__ __launch_bounds__(256) void latent_sum_kernel(const float* __restrict__ d_r, msa_seqs sq, int H, float scale,
                                                          uint16_t* __restrict__ d_kv, uint16_t* __restrict__ out, int64_t out_row) {
   const int lane = lane_id();
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave;
-  if (row >= sq.total_kv_rows) return;
-  bool owned = false;
-  for (int c = 0; c < sq.num_seqs && !owned; c += kWave) {
-    bool here = false;
-    if (c + lane < sq.num_seqs) {
-      const int64_t start = seq_geom(sq, c + lane).kv_start;
-      here = row >= start && row < start + tile_geom(sq, c + lane).kv_len;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; row < sq.total_kv_rows;
+       row += static_cast<int64_t>(gridDim.x) * 4) {
+    bool owned = false;
+    for (int c = 0; c < sq.num_seqs && !owned; c += kWave) {
+      bool here = false;
+      if (c + lane < sq.num_seqs) {
+        const int64_t start = seq_geom(sq, c + lane).kv_start;
+        here = row >= start && row < start + tile_geom(sq, c + lane).kv_len;
+      }
+      owned = __ballot(here) != 0;
     }
-    owned = __ballot(here) != 0;
-  }
-  float sum = 0.f;
-  if (owned) {
-    for (int h0 = 0; h0 < H; h0 += 8) {
-      float v[8];
+    float sum = 0.f;
+    if (owned) {
+      for (int h0 = 0; h0 < H; h0 += 8) {
+        float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = d_r[(static_cast<int64_t>(min(h0 + i, H - 1)) * sq.total_kv_rows + row) * kRot + lane];
+        for (int i = 0; i < 8; ++i) v[i] = d_r[(static_cast<int64_t>(min(h0 + i, H - 1)) * sq.total_kv_rows + row) * kRot + lane];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += h0 + i < H ? v[i] : 0.f;
+        for (int i = 0; i < 8; ++i) sum += h0 + i < H ? v[i] : 0.f;
+      }
+    } else {
+      u32x4* y = reinterpret_cast<u32x4*>(d_kv + row * H * kPair);
+      for (int i = lane; i < H * kPair / 8; i += kWave) y[i] = u32x4{};
     }
-  } else {
-    u32x4* y = reinterpret_cast<u32x4*>(d_kv + row * H * kPair);
-    for (int i = lane; i < H * kPair / 8; i += kWave) y[i] = u32x4{};
+    out[row * out_row + lane] = static_cast<uint16_t>(pack_bf16x2(sum * scale, 0.f));
   }
-  out[row * out_row + lane] = static_cast<uint16_t>(pack_bf16x2(sum * scale, 0.f));
 }
 
 // ---------------------------------------------------------------- host side
@@ -716,13 +718,13 @@ extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t
   const flash::Grid gr = flash::plan_grid(seqs, kRowTile, seqs->max_q_rows, &tiles);
   const int64_t key_tiles = seqs->num_seqs == 1 ? (std::min<int64_t>(seqs->max_kv_len, N) + kKeyTile - 1) / kKeyTile
                                                 : N / kKeyTile + seqs->num_seqs;
-  if (std::max(tiles, key_tiles) * H >= (int64_t(1) << 31)) return MSA_ERR_UNSUPPORTED;
+  if (std::max(tiles, key_tiles) * H >= (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;     // a grid's limit
   if (T > 0)
     msa_prof::launch("latent_backward_q_kernel", latent_backward_kernel<false>, dim3(static_cast<unsigned>(tiles * H)),
                      dim3(kThreads), 0, stream, a, *seqs, gr);
   msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true>,
                    dim3(static_cast<unsigned>(key_tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
-  msa_prof::launch("latent_sum_kernel", latent_sum_kernel, dim3(static_cast<unsigned>((N + 3) / 4)), dim3(256), 0, stream,
+  msa_prof::launch("latent_sum_kernel", latent_sum_kernel, dim3(static_cast<unsigned>(std::min((N + 3) / 4, kSumCtas))), dim3(256), 0, stream,
                    static_cast<const float*>(a.d_r), *seqs, H, softmax_scale, dkv, static_cast<uint16_t*>(d_k_rope),
                    d_k_rope_stride);
   return msa_host::launch_status();

@@ -271,3 +271,10 @@ def test_absorbed_is_expanded():
     o1, l1, _ = O.latent_attention(q, e, np.einsum("hdr,nr->nhd", wk, c), r, np.einsum("hdr,nr->nhd", wv, c), lay, 0.2)
     o2, l2, _ = O.latent_attention(np.einsum("thd,hdr->thr", q, wk), e, c[:, None], r, c[:, None], lay, 0.2)
     assert np.abs(o1 - np.einsum("thr,hdr->thd", o2, wv)).max() < 1e-12 and np.abs(l1 - l2).max() < 1e-12
+
+
+def test_gradients_refuse_more_ctas_than_a_grid_has():
+    """A CTA of 256 threads per head and sequence at least, and a grid has 2^32 threads."""
+    n = 1 << 20
+    seqs = _seqs(num_seqs=n, total_q_rows=n, max_q_rows=1, total_kv_rows=n, max_kv_len=1)
+    assert _backward(_expanded(seqs=seqs, H=32, dqs=4096, des=2048)) == UNS
