@@ -199,9 +199,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
     // requests hang on a branch (behind one, each store into LDS would wait for all of them)
     auto codes_of = [&](int i, bool any) {
       const int key0 = i * kKeys + 16 * wave;
-      const char* src = any ? source(i) : reinterpret_cast<const char*>(cache);
-      const int rows = any ? min(max(g.kv_len - key0, 0), kGroup) : 0;
-      return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, rows * static_cast<int>(W * sizeof(T)), 0x00020000);
+      const uint64_t src = reinterpret_cast<uint64_t>(any ? source(i) : reinterpret_cast<const char*>(cache));
+      const int bytes = any ? min(max(g.kv_len - key0, 0), kGroup) * static_cast<int>(W * sizeof(T)) : 0;
+      // the same in every lane, which the compiler must be told, else it loops over the lanes for each request
+      const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(src));
+      const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(src >> 32));
+      return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0,
+                                               __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
     };
     auto get_codes = [&](auto from, int c, int piece) __attribute__((always_inline)) {
       if constexpr (kCodes) raw[c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, 16 * piece, c * 1024, 0));
