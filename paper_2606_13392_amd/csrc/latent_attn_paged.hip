@@ -101,6 +101,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
   constexpr int TD = R / 128;              // 32-dimension tiles of a wave's quarter
   constexpr int kRowBytes = W * 2;         // in LDS
   constexpr int kBuf = kKeys * kRowBytes;
+  constexpr bool kAtOnce = !(kCodes && TD == 4);     // weights before the maxima are joined
   constexpr int kGroup = 16;               // a wave copies 16 keys of a step: never across a page's end
   constexpr int kSrcSegs = W * sizeof(T) / 16;
   constexpr int NC = kGroup * kSrcSegs / kWave;      // 16-byte pieces per lane and step
@@ -109,6 +110,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
   __shared__ __align__(16) uint16_t keys[2][kKeys * W];
   __shared__ __align__(16) uint16_t weights[kRows * kKeys];
   __shared__ float tops[2][kRows];
+  __shared__ __align__(16) int outgrown[kWaves];
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int n = lane & 31, h = lane >> 5;
@@ -243,12 +245,12 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
     auto put = [&](int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
       if constexpr (kCodes) {
         char* dst = reinterpret_cast<char*>(keys[buf]) + 16 * wave * kRowBytes;
-        // which half goes first differs between lanes, so that 8 and 16 lanes' stores fall on all banks
-        const bool hi = ((piece >> 2) ^ (piece >> 3)) & 1;
+        // (two lanes meet in a bank; to change the halves' order between them takes six instructions a piece: draft rows of
+        // 128 heads 101 us, with it 105)
         const u32x2 a{raw[c][0], raw[c][1]}, b{raw[c][2], raw[c][3]};
-        const int mix = static_cast<int>(mixes >> (3 * c)) & 7, d = 2 * (c * kWave + piece);
-        *reinterpret_cast<u32x4*>(dst + 16 * ((d + hi) ^ mix)) = widen(hi ? b : a);
-        *reinterpret_cast<u32x4*>(dst + 16 * ((d + !hi) ^ mix)) = widen(hi ? a : b);
+        const int mix = static_cast<int>(mixes >> (3 * c)) & 7, at = 16 * ((2 * (c * kWave + piece)) ^ mix);
+        *reinterpret_cast<u32x4*>(dst + at) = widen(a);
+        *reinterpret_cast<u32x4*>(dst + (at ^ 16)) = widen(b);
       }
     };
 
@@ -368,71 +370,98 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       for (int a = 1; a < 16; ++a) top = fmaxf(top, sc[a]);
       top = fmaxf(top, xor32f(top));
       if (h == 0) tops[kh][mine] = top;
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       // The maxima that the weights are relative to move only when one is outgrown by 2^kSlack: among 64 rows
       // some true maximum moves in most steps, and each time O would be rescaled (384 instructions a wave at
       // R = 512; 32 tokens on 4K - 60K keys 171 us instead of 149, chunks at R = 256 87 instead of 77).  Weights stay
-      // below 2^kSlack, and their sums far from fp32's ends.
-      float alpha[2] = {1.f, 1.f}, neg[2];
+      // below 2^kSlack, and their sums far from fp32's ends.  So a wave forms its weights before it knows the other
+      // key half's maxima, and only where some wave has outgrown one are they formed again: a barrier and a way through
+      // LDS less a step (32 tokens 153 us with them, 147 without; E4M3 chunks at R = 256 116 and 110).  E4M3 at R = 512
+      // has no registers for both (101 us, 132 with spills) and always waits for the maxima.
+      if constexpr (kAtOnce) {
+        const float m = rh ? m_run[1] : m_run[0];
+        const bool grown = (top - m) * scale_log2 > kSlack;       // the first visible keys among them: m is -inf
+        const uint64_t any = __ballot(grown);
+        if (lane == 0) outgrown[wave] = any != 0;
+      }
+      float sum;
+      auto weigh = [&]() __attribute__((always_inline)) {
+        const float m = rh ? m_run[1] : m_run[0], neg = m == -INFINITY ? 0.f : -m * scale_log2;   // rows with nothing visible yet
+        float w[16];
+        sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float m_new = fmaxf(tops[0][32 * j + n], tops[1][32 * j + n]);
-        if ((m_new - m_run[j]) * scale_log2 > kSlack) {           // the first visible keys among them: m_run is -inf
-          alpha[j] = exp2_hw((m_run[j] - m_new) * scale_log2);
-          m_run[j] = m_new;
+        for (int a = 0; a < 16; ++a) {
+          w[a] = exp2_hw(fmaf(sc[a], scale_log2, neg));
+          sum += w[a];
         }
-        neg[j] = m_run[j] == -INFINITY ? 0.f : -m_run[j] * scale_log2;   // rows with nothing visible yet
-      }
-      const float my_neg = rh ? neg[1] : neg[0];
-      float sum = 0.f;
+        // k-step u of the value product: keys 16 u + {4h + 0..3, 8 + 4h + 0..3}, as the scores hold them
 #pragma unroll
-      for (int a = 0; a < 16; ++a) {
-        sc[a] = exp2_hw(fmaf(sc[a], scale_log2, my_neg));
-        sum += sc[a];
-      }
-      l_run = fmaf(l_run, rh ? alpha[1] : alpha[0], sum);
-      // k-step u of the value product: keys 16 u + {4h + 0..3, 8 + 4h + 0..3}, as the scores hold them
+        for (int b = 0; b < 2; ++b) {
+          uint4 y;
+          y.x = pack_bf16x2(w[8 * b + 0], w[8 * b + 1]);
+          y.y = pack_bf16x2(w[8 * b + 2], w[8 * b + 3]);
+          y.z = pack_bf16x2(w[8 * b + 4], w[8 * b + 5]);
+          y.w = pack_bf16x2(w[8 * b + 6], w[8 * b + 7]);
+          *reinterpret_cast<uint4*>(weights + mine * kKeys + 8 * p_seg(mine, 2 * (2 * kh + b) + h)) = y;
+        }
+      };
+      if constexpr (kAtOnce) weigh();
+      constexpr int NU = kKeys / 16, NO = NU * TD;
+      bf16x8 bp[NU][2], vr[NO];
+      auto pread = [&](int us) __attribute__((always_inline)) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        uint4 w;
-        w.x = pack_bf16x2(sc[8 * b + 0], sc[8 * b + 1]);
-        w.y = pack_bf16x2(sc[8 * b + 2], sc[8 * b + 3]);
-        w.z = pack_bf16x2(sc[8 * b + 4], sc[8 * b + 5]);
-        w.w = pack_bf16x2(sc[8 * b + 6], sc[8 * b + 7]);
-        *reinterpret_cast<uint4*>(weights + mine * kKeys + 8 * p_seg(mine, 2 * (2 * kh + b) + h)) = w;
-      }
+        for (int j = 0; j < 2; ++j)
+          bp[us][j] = ld_bf16x8(weights + (32 * j + n) * kKeys + 8 * p_seg(n, 2 * us + h));
+      };
+      auto vread = [&](int k) __attribute__((always_inline)) {
+        const int us = k / TD, td = k % TD;
+        const char* a0 = kb + 16 * us * kRowBytes + (td >> 1) * 128;
+        const uint2 x0 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][0]));
+        const uint2 x1 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][1]));
+        return __builtin_bit_cast(bf16x8, make_uint4(x0.x, x0.y, x1.x, x1.y));
+      };
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      bool again = true;
+      auto begin = [&]() __attribute__((always_inline)) {
+        pread(0);
+#pragma unroll
+        for (int k = 0; k < kAheadV; ++k) vr[k] = vread(k);
+      };
+      if constexpr (kAtOnce) {
+        const int4 which = *reinterpret_cast<const int4*>(outgrown);
+        begin();
+        again = __builtin_amdgcn_readfirstlane(which.x | which.y | which.z | which.w) != 0;
+      }
       // (the pins keep O in accumulation registers on the way around, else it is moved in every step)
       auto pin = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int td = 0; td < TD; ++td) asm volatile("" : "+a"(acc[td][0]), "+a"(acc[td][1]));
       };
-      pin();
-      if (__ballot(alpha[0] != 1.f || alpha[1] != 1.f)) {
+      if constexpr (kAtOnce) pin();
+      if (again) {
+        float alpha[2];
 #pragma unroll
-        for (int td = 0; td < TD; ++td)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[td][j] *= alpha[j];
+        for (int j = 0; j < 2; ++j) {
+          const float m_new = fmaxf(tops[0][32 * j + n], tops[1][32 * j + n]);
+          const bool grown = (m_new - m_run[j]) * scale_log2 > kSlack;
+          alpha[j] = grown ? exp2_hw((m_run[j] - m_new) * scale_log2) : 1.f;
+          m_run[j] = grown ? m_new : m_run[j];
+        }
+        l_run *= rh ? alpha[1] : alpha[0];
+        weigh();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         pin();
+        if (__ballot(alpha[0] != 1.f || alpha[1] != 1.f)) {
+#pragma unroll
+          for (int td = 0; td < TD; ++td)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[td][j] *= alpha[j];
+          pin();
+        }
+        if constexpr (kAtOnce) pread(0);
+        else begin();
       }
+      l_run += sum;
       {
-        constexpr int NU = kKeys / 16, NO = NU * TD;
-        bf16x8 bp[NU][2], vr[NO];
-        auto pread = [&](int us) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            bp[us][j] = ld_bf16x8(weights + (32 * j + n) * kKeys + 8 * p_seg(n, 2 * us + h));
-        };
-        auto vread = [&](int k) {
-          const int us = k / TD, td = k % TD;
-          const char* a0 = kb + 16 * us * kRowBytes + (td >> 1) * 128;
-          const uint2 x0 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][0]));
-          const uint2 x1 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][1]));
-          return __builtin_bit_cast(bf16x8, make_uint4(x0.x, x0.y, x1.x, x1.y));
-        };
-        pread(0);
-#pragma unroll
-        for (int k = 0; k < kAheadV; ++k) vr[k] = vread(k);
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
           const int us = k / TD, td = k % TD;

@@ -50,13 +50,13 @@ def some_rows(rng, q_offsets, n, most=48):
 class PagedBatch:
     """Queries, a latent cache on shuffled pages that is NaN wherever no sequence's key lies, and the layout."""
 
-    def __init__(self, name, q_rows, kv_lens, H, R, page, pad=0, fp8=False, scale=2.0 ** -4):
+    def __init__(self, name, q_rows, kv_lens, H, R, page, pad=0, fp8=False, scale=2.0 ** -4, change=lambda rows: rows):
         rng = self.rng = np.random.default_rng(sum(map(ord, name)))
         T, n = sum(q_rows) + pad, sum(kv_lens)
         self.n, self.H, self.R, self.fp8, self.scale = sum(q_rows), H, R, fp8, scale
         self.q = bf16(rng.standard_normal((T, H, R)) * np.sqrt(128 / R))
         self.q_rope = bf16(rng.standard_normal((T, H, ROT)))
-        rows = rng.standard_normal((n, R + ROT))
+        rows = change(rng.standard_normal((n, R + ROT)))
         table, total, where = page_table(rng, kv_lens, page)
         at = np.concatenate(where)
         if fp8:

@@ -8,7 +8,7 @@ import torch
 import oracle.msa_oracle as O
 from paper_2606_13392_amd import msa
 from tests.latent_util import ROT, SCALE, PagedBatch, check_lse, some_rows
-from tests.operators_util import host, padded_seqs, replay
+from tests.operators_util import dev, host, padded_seqs, replay
 
 pytestmark = pytest.mark.gpu
 
@@ -123,6 +123,29 @@ def test_large_scores_and_infinite_neighbours():
     ref = 60.0 * 3 * (b.R + ROT) * SCALE + np.log((sign == 60).sum())
     # roundings of 2^-24: the scale to fp32, log2 e, their product, the score's, the sum with the logarithm, ln 2, its product
     assert np.abs(host(l)[0] - ref).max() <= 8 * 2.0 ** -24 * ref
+
+
+@pytest.mark.parametrize("R", [256, 512])
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "e4m3"])
+def test_maxima_that_grow(fp8, R):
+    """In every second step one key of one half, by turns, outgrows what the weights were relative to, for every second head
+    alone: scores climb to 25 by 6.3 (9 in base 2).  The sizes of a score's terms sum to less than 32, so LSE_TOL's count
+    of roundings covers them (7.6e-5, and 1e-5 for the rest)."""
+    lens = [640, 300]
+    def climb(rows):
+        rows *= 0.25
+        rows[:, 0] = 0
+        for j0 in (0, lens[0]):
+            for s in range(10):
+                j = j0 + 64 * s + 32 * (s // 2 % 2) + 7
+                if j < j0 + lens[j0 > 0]:
+                    rows[j, 0] = 11 * (s // 2)
+        return rows
+    b = PagedBatch("grow", [3, 40], lens, 8, R, 64, 0, fp8, scale=2.0 ** -3, change=climb)
+    b.q[..., 0] = np.where(np.arange(8) % 2, 0.0, 8.0)
+    b.dq = dev(b.q.transpose(1, 0, 2)).transpose(0, 1)
+    o, l = run(b, fp8)
+    b.check(o, l, np.arange(b.n), "grow")
 
 
 def test_row_without_keys():
