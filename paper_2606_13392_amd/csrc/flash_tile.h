@@ -94,6 +94,12 @@ __device__ __forceinline__ uint2 lds_tr4(const uint16_t* p) {
       (__attribute__((address_space(3))) v4i16*)(v4i16*)(const_cast<uint16_t*>(p)));
   return __builtin_bit_cast(uint2, x);
 }
+// The same on bytes: lane j of 16 addresses 8 bytes of row j / 2 and receives 8 rows' byte j.
+__device__ __forceinline__ u32x2 lds_tr8(const char* p) {
+  typedef __attribute__((__vector_size__(2 * sizeof(int)))) int v2i32;
+  const v2i32 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i32*)(v2i32*)(const_cast<char*>(p)));
+  return __builtin_bit_cast(u32x2, x);
+}
 // global_load_lds: lane l's 16 bytes land at dst + 16 l (dst wave-uniform).
 __device__ __forceinline__ void dma16(const void* src, uint16_t* dst) {
   __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);

@@ -45,6 +45,7 @@ using flash::kLn_2;
 using flash::kLog2E;
 using flash::lds_address;
 using flash::lds_tr4;
+using flash::lds_tr8;
 using flash::xor32f;
 using steps::kKeys;
 using steps::Share;
@@ -69,6 +70,9 @@ constexpr int kAheadK = 6, kAheadV = 3;  // LDS operands requested so many produ
 // reads of 4 rows x 4 segments, fall on all banks.  (A row is an odd multiple of
 // 128 bytes: odd rows start in the other half of the banks.)
 __device__ __forceinline__ int row_mix(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
+// Codes: a row is an odd multiple of 64 bytes, so the low two bits, and half of the rows' reads lie in the other half.
+template <typename T>
+__device__ __forceinline__ int key_mix(int r) { return sizeof(T) == 1 ? (r >> 1) & 3 : row_mix(r); }
 // The weights in LDS: 64 keys = 8 segments per row.
 __device__ __forceinline__ int p_seg(int r, int s) { return s ^ ((r >> 1) & 7); }
 
@@ -96,18 +100,17 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
     uint32_t q_flip, float o_scale, uint16_t* __restrict__ o, float* __restrict__ lse) {
   constexpr bool kCodes = sizeof(T) == 1;
   constexpr int W = R + kRot;              // elements of a cache row
-  constexpr int kSegs = W / 8;             // 16-byte segments of a row in LDS
   constexpr int KS = W / 16;               // k-steps of the scores
   constexpr int TD = R / 128;              // 32-dimension tiles of a wave's quarter
-  constexpr int kRowBytes = W * 2;         // in LDS
+  constexpr int kRowBytes = W * static_cast<int>(sizeof(T));       // in LDS as in memory
   constexpr int kBuf = kKeys * kRowBytes;
-  constexpr bool kAtOnce = !(kCodes && TD == 4);     // weights before the maxima are joined
   constexpr int kGroup = 16;               // a wave copies 16 keys of a step: never across a page's end
-  constexpr int kSrcSegs = W * sizeof(T) / 16;
+  constexpr int kSrcSegs = kRowBytes / 16;
   constexpr int NC = kGroup * kSrcSegs / kWave;      // 16-byte pieces per lane and step
-  constexpr int kEarly = (NC + 2) / 2;     // bf16: copies among the score products, the others among the value products
+  constexpr int kEarly = (NC + 2) / 2;     // copies among the score products, the others among the value products
   static_assert(kGroup * kSrcSegs % kWave == 0, "");
-  __shared__ __align__(16) uint16_t keys[2][kKeys * W];
+  constexpr int kQBytes = kRows * W * 2;   // the tile's queries, once, behind the first buffer
+  __shared__ __align__(16) char keys[kBuf + (kBuf > kQBytes ? kBuf : kQBytes)];
   __shared__ __align__(16) uint16_t weights[kRows * kKeys];
   __shared__ float tops[2][kRows];
   __shared__ __align__(16) int outgrown[kWaves];
@@ -127,29 +130,35 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
   const int tile_heads = min(pl.heads, H - block * pl.heads);     // of this block
   const uint32_t heads_inv = (65536 + tile_heads - 1) / tile_heads;
   auto per_row = [&](int r) { return static_cast<int>((static_cast<uint32_t>(r) * heads_inv) >> 16); };   // r / tile_heads, r < 64
-  // K operand: row n of the wave's half, segment 2 st + h
-  uint32_t k_at[4];
+  // K operand: row n of the wave's half; bf16: segment 2 st + h; codes: segment 2 j + h, whose 16 elements are those of
+  // k-steps 2 j and 2 j + 1
+  constexpr int kGroupSegs = kCodes ? 4 : 8;         // that the rows' permutation stays in
+  uint32_t k_at[kGroupSegs / 2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) k_at[i] = (32 * kh + n) * kRowBytes + 16 * (((2 * i + h) & 7) ^ row_mix(n));
-  // C^T operand: in each 16-lane group lane j addresses row k0 + j / 4, dims
-  // n0 + 4 (j % 4) .. + 3, and receives rows k0 .. k0 + 3 of dim n0 + j
-  uint32_t v_at[2][2];
+  for (int i = 0; i < kGroupSegs / 2; ++i) k_at[i] = (32 * kh + n) * kRowBytes + 16 * ((2 * i + h) ^ key_mix<T>(n));
+  // C^T operand, a transposing read of 16 keys x 32 dims: in each 16-lane group lane j addresses (bf16) row k0 + j / 4, dims
+  // n0 + 4 (j % 4) .. + 3, and receives rows k0 .. k0 + 3 of dim n0 + j, twice; (codes) row k0 + j / 2, dims n0 + 8 (j % 2)
+  // .. + 7, and receives rows k0 .. k0 + 7
+  uint32_t v_at[2][kCodes ? 1 : 2];
   {
     const int gq = lane >> 4, jj = lane & 15;
-    const int rl = 4 * h + (jj >> 2);
+    const int rl = kCodes ? 8 * h + (jj >> 1) : 4 * h + (jj >> 2);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int seg = 4 * i + 2 * (gq & 1) + ((jj & 3) >> 1);
-        v_at[i][b] = (rl + 8 * b) * kRowBytes + wave * (R / 4) * 2 + 16 * (seg ^ row_mix(rl + 8 * b)) + 8 * (jj & 1);
+      for (int b = 0; b < (kCodes ? 1 : 2); ++b) {
+        const int r = rl + 8 * b;
+        if constexpr (kCodes)
+          v_at[i][b] = r * kRowBytes + wave * (R / 4) + 16 * ((2 * i + (gq & 1)) ^ key_mix<T>(r)) + 8 * (jj & 1);
+        else
+          v_at[i][b] = r * kRowBytes + wave * (R / 4) * 2 + 16 * ((4 * i + 2 * (gq & 1) + ((jj & 3) >> 1)) ^ key_mix<T>(r)) + 8 * (jj & 1);
       }
   }
-  const uint32_t lds_keys = lds_address(keys[0]);
+  const uint32_t lds_keys = lds_address(keys);
   uint64_t piece_mixes = 0;                // row_mix of the row of each of the lane's pieces
 #pragma unroll
   for (int c = 0; c < NC; ++c)
-    piece_mixes |= static_cast<uint64_t>(row_mix((c * kWave + lane) / kSrcSegs)) << (3 * c);
+    piece_mixes |= static_cast<uint64_t>(key_mix<T>((c * kWave + lane) / kSrcSegs)) << (3 * c);
   const int lg_page = 31 - __clz(sq.page_size);
   const int max_page = static_cast<int>(sq.total_kv_rows >> lg_page) - 1;
 
@@ -190,30 +199,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       cur = fetch(w0 + lane);
       nxt = fetch(w0 + kWave + lane);
     }
-    // Keys of a step: bf16 into a buffer by copies of 1 KiB; codes into registers.
-    // Piece c * 64 + lane of the wave's 16 rows is 16 bytes; by copy it lands at its own
-    // number, so it is the segment that the row's permutation stores there.  (Rows are a
-    // multiple of 8 segments, so the permutation is one of the piece's low three bits.)
+    // Keys of a step go into a buffer by copies of 1 KiB.  Piece c * 64 + lane of the wave's 16 rows is 16 bytes; it
+    // lands at its own number, so it is the segment that the row's permutation stores there.  (Rows are a
+    // multiple of 8 segments, of 4 codes', so the permutation is one of the piece's low bits.)
     // Offsets are formed anew each time: held, they spill.
-    u32x4 raw[kCodes ? NC : 1];
     auto source = [&](int i) { return reinterpret_cast<const char*>(cache) + place(i) * (W * static_cast<int64_t>(sizeof(T))); };
-    // codes: through a buffer whose end is the sequence's, so that keys past it read as zeros; no step's
-    // requests hang on a branch (behind one, each store into LDS would wait for all of them)
-    auto codes_of = [&](int i, bool any) {
-      const int key0 = i * kKeys + 16 * wave;
-      const uint64_t src = reinterpret_cast<uint64_t>(any ? source(i) : reinterpret_cast<const char*>(cache));
-      const int bytes = any ? min(max(g.kv_len - key0, 0), kGroup) * static_cast<int>(W * sizeof(T)) : 0;
-      // the same in every lane, which the compiler must be told, else it loops over the lanes for each request
-      const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(src));
-      const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(src >> 32));
-      return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(static_cast<uint64_t>(hi) << 32 | lo), 0,
-                                               __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-    };
-    auto get_codes = [&](auto from, int c, int piece) __attribute__((always_inline)) {
-      if constexpr (kCodes) raw[c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, 16 * piece, c * 1024, 0));
-    };
-    // copies: pieces past the sequence's end repeat its last one (what memory holds there may be NaN), and behind the
-    // last step all repeat one; no copy hangs on a branch
+    // Pieces past the sequence's end repeat its last one (what memory holds there may be NaN), and behind the
+    // last step all repeat one; no copy hangs on a branch.
     struct Source {
       const char* from;
       uint32_t limit;                        // offset of the last piece that may be read
@@ -232,26 +224,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       int piece = lane;
       uint64_t mixes = piece_mixes;
       asm volatile("" : "+v"(piece), "+v"(mixes));
-      if constexpr (kCodes) {
-        const auto from = codes_of(i, true);
+      const Source src = keys_of(i);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) get_codes(from, c, piece);
-      } else {
-        const Source src = keys_of(i);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) get(src, buf, c, piece, mixes);
-      }
-    };
-    auto put = [&](int buf, int c, int piece, uint64_t mixes) __attribute__((always_inline)) {
-      if constexpr (kCodes) {
-        char* dst = reinterpret_cast<char*>(keys[buf]) + 16 * wave * kRowBytes;
-        // (two lanes meet in a bank; to change the halves' order between them takes six instructions a piece: draft rows of
-        // 128 heads 101 us, with it 105)
-        const u32x2 a{raw[c][0], raw[c][1]}, b{raw[c][2], raw[c][3]};
-        const int mix = static_cast<int>(mixes >> (3 * c)) & 7, at = 16 * ((2 * (c * kWave + piece)) ^ mix);
-        *reinterpret_cast<u32x4*>(dst + at) = widen(a);
-        *reinterpret_cast<u32x4*>(dst + (at ^ 16)) = widen(b);
-      }
+      for (int c = 0; c < NC; ++c) get(src, buf, c, piece, mixes);
     };
 
     // Q of the tile's rows, through the second buffer: its own parts, 2 R bytes a row, segments in an order of the row
@@ -281,24 +256,26 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
                lds_keys + kBuf + kRows * R * 2 + 1024 * c);
       }
     };
-    // k-step st holds elements 16 st + 8 h .. + 7 of the lane's row
+    // k-step st holds elements 16 st + 8 h .. + 7 of the lane's row; codes: 32 (st / 2) + 16 h + 8 (st % 2) .. + 7
     bf16x8 bq[KS];
     auto read_q = [&]() {
       int r = mine;
       asm volatile("" : "+v"(r));
-      const uint16_t* own = keys[1] + r * R;
-      const uint16_t* rot = keys[1] + kRows * R + r * kRot;
+      const uint16_t* own = reinterpret_cast<const uint16_t*>(keys + kBuf) + r * R;
+      const uint16_t* rot = reinterpret_cast<const uint16_t*>(keys + kBuf) + kRows * R + r * kRot;
 #pragma unroll
-      for (int st = 0; st < KS; ++st)
-        bq[st] = ld_bf16x8(st < R / 16 ? own + 8 * ((2 * st + h) ^ (r & 15)) : rot + 8 * ((2 * (st - R / 16) + h) ^ row_mix(r)));
+      for (int st = 0; st < KS; ++st) {
+        const int sg = kCodes ? 4 * (st >> 1) + 2 * h + (st & 1) : 2 * st + h;       // of 8 elements
+        bq[st] = ld_bf16x8(st < R / 16 ? own + 8 * (sg ^ (r & 15)) : rot + 8 * ((sg - R / 8) ^ row_mix(r)));
+      }
       if (q_flip != 0) {
 #pragma unroll
         for (int st = 0; st < KS; ++st) bq[st] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, bq[st]) ^ q_flip);
       }
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        // the accumulation registers are for the sums; with codes under way half of Q fits beside these
-        if (st < (kCodes ? KS / 2 : TD == 4 ? 10 : 0)) asm volatile("" : "+a"(bq[st]));
+        // (accumulation registers are for the sums; some of Q fits beside them)
+        if (st < (TD == 4 ? 10 : 0)) asm volatile("" : "+a"(bq[st]));
         else asm volatile("" : "+v"(bq[st]));
       }
     };
@@ -310,51 +287,41 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
     if (b_begin < b_end) {
       get_q();
       get_all(b_begin, 0);
-      if constexpr (kCodes) {
-#pragma unroll
-        for (int c = 0; c < NC; ++c) put(0, c, lane, piece_mixes);
-        if (b_begin + 1 < b_end) get_all(b_begin + 1, 1);
-      }
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCodes ? NC : 0) : "memory");
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       read_q();
     }
-    // Step i: its keys are in buffer i - b_begin (mod 2).  bf16: the copies of step i + 1 go out
+    // Step i: its keys are in buffer i - b_begin (mod 2).  The copies of step i + 1 go out
     // between the products of both kinds, one by one, so that requests are under
-    // way all the time.  Codes: those of step i + 1, in registers, are stored between the
-    // score products, and those of i + 2 requested.
+    // way all the time.
     for (int i = b_begin; i < b_end; ++i) {
       const int buf = (i - b_begin) & 1;
-      const char* kb = reinterpret_cast<const char*>(keys[buf]);
+      const char* kb = keys + buf * kBuf;
       int piece = lane;
       uint64_t mixes = piece_mixes;
       asm volatile("" : "+v"(piece), "+v"(mixes));
       // everyone's keys of step i are in place, and the readers of step i - 1's are done
-      if constexpr (!kCodes) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      Source next{};
-      if constexpr (!kCodes) next = keys_of(i + 1);
-      const auto codes = codes_of(i + 2, kCodes && i + 2 < b_end);
+      asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      const Source next = keys_of(i + 1);
       f32x16 sc = {};
       {
-        // fenced slots: LDS operands are requested kAheadK products before their use
-        auto kread = [&](int st) {
-          return ld_bf16x8(reinterpret_cast<const uint16_t*>(kb + k_at[st & 3] + (st >> 2) * 128));
+        // fenced slots: LDS operands are requested kAheadK products before their use (codes: two products' with a read)
+        constexpr int kPer = kCodes ? 2 : 1, kReads = KS / kPer, kFront = kAheadK / kPer;
+        auto kread = [&](int j) {
+          return *reinterpret_cast<const u32x4*>(kb + k_at[j & (kGroupSegs / 2 - 1)] + j / (kGroupSegs / 2) * 16 * kGroupSegs);
         };
-        bf16x8 kr[KS];
+        u32x4 kr[kReads];
 #pragma unroll
-        for (int st = 0; st < kAheadK; ++st) kr[st] = kread(st);
+        for (int j = 0; j < kFront; ++j) kr[j] = kread(j);
 #pragma unroll
         for (int st = 0; st < KS; ++st) {
-          if (st + kAheadK < KS) kr[st + kAheadK] = kread(st + kAheadK);
-          sc = mfma32x32x16(kr[st], bq[st], sc);
-          if constexpr (!kCodes)
-            if (st % 3 == 1 && st / 3 < kEarly) get(next, buf ^ 1, st / 3, piece, mixes);
-          if constexpr (kCodes)
-            if (st % 4 == 1 && st / 4 < NC) {
-              put(buf ^ 1, st / 4, piece, mixes);     // behind the last step: a buffer that nobody reads
-              get_codes(codes, st / 4, piece);
-            }
+          const int j = st / kPer;
+          if (st % kPer == 0 && j + kFront < kReads) kr[j + kFront] = kread(j + kFront);
+          bf16x8 kk;
+          if constexpr (kCodes) kk = widen_bf16x8(st & 1 ? u32x2{kr[j][2], kr[j][3]} : u32x2{kr[j][0], kr[j][1]});
+          else kk = __builtin_bit_cast(bf16x8, kr[j]);
+          sc = mfma32x32x16(kk, bq[st], sc);
+          if (st % 3 == 1 && st / 3 < kEarly) get(next, buf ^ 1, st / 3, piece, mixes);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -375,9 +342,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       // R = 512; 32 tokens on 4K - 60K keys 171 us instead of 149, chunks at R = 256 87 instead of 77).  Weights stay
       // below 2^kSlack, and their sums far from fp32's ends.  So a wave forms its weights before it knows the other
       // key half's maxima, and only where some wave has outgrown one are they formed again: a barrier and a way through
-      // LDS less a step (32 tokens 153 us with them, 147 without; E4M3 chunks at R = 256 116 and 110).  E4M3 at R = 512
-      // has no registers for both (101 us, 132 with spills) and always waits for the maxima.
-      if constexpr (kAtOnce) {
+      // LDS less a step (32 tokens 153 us with them, 147 without).
+      {
         const float m = rh ? m_run[1] : m_run[0];
         const bool grown = (top - m) * scale_log2 > kSlack;       // the first visible keys among them: m is -inf
         const uint64_t any = __ballot(grown);
@@ -393,20 +359,29 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
           w[a] = exp2_hw(fmaf(sc[a], scale_log2, neg));
           sum += w[a];
         }
-        // k-step u of the value product: keys 16 u + {4h + 0..3, 8 + 4h + 0..3}, as the scores hold them
+        // k-step u of the value product, lanes h: keys 16 u + {4h + 0..3, 8 + 4h + 0..3}, as the scores hold them; codes:
+        // 16 u + 8h + 0..7, as they are read
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          uint4 y;
-          y.x = pack_bf16x2(w[8 * b + 0], w[8 * b + 1]);
-          y.y = pack_bf16x2(w[8 * b + 2], w[8 * b + 3]);
-          y.z = pack_bf16x2(w[8 * b + 4], w[8 * b + 5]);
-          y.w = pack_bf16x2(w[8 * b + 6], w[8 * b + 7]);
-          *reinterpret_cast<uint4*>(weights + mine * kKeys + 8 * p_seg(mine, 2 * (2 * kh + b) + h)) = y;
+          uint2 lo, hi;
+          lo.x = pack_bf16x2(w[8 * b + 0], w[8 * b + 1]);
+          lo.y = pack_bf16x2(w[8 * b + 2], w[8 * b + 3]);
+          hi.x = pack_bf16x2(w[8 * b + 4], w[8 * b + 5]);
+          hi.y = pack_bf16x2(w[8 * b + 6], w[8 * b + 7]);
+          uint16_t* row = weights + mine * kKeys;
+          const int u = 2 * kh + b;
+          if constexpr (kCodes) {
+            *reinterpret_cast<uint2*>(row + 8 * p_seg(mine, 2 * u) + 4 * h) = lo;
+            *reinterpret_cast<uint2*>(row + 8 * p_seg(mine, 2 * u + 1) + 4 * h) = hi;
+          } else {
+            *reinterpret_cast<uint4*>(row + 8 * p_seg(mine, 2 * u + h)) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+          }
         }
       };
-      if constexpr (kAtOnce) weigh();
+      weigh();
       constexpr int NU = kKeys / 16, NO = NU * TD;
-      bf16x8 bp[NU][2], vr[NO];
+      bf16x8 bp[NU][2];
+      Raw<T> vr[NO];
       auto pread = [&](int us) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -414,30 +389,27 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       };
       auto vread = [&](int k) __attribute__((always_inline)) {
         const int us = k / TD, td = k % TD;
-        const char* a0 = kb + 16 * us * kRowBytes + (td >> 1) * 128;
-        const uint2 x0 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][0]));
-        const uint2 x1 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][1]));
-        return __builtin_bit_cast(bf16x8, make_uint4(x0.x, x0.y, x1.x, x1.y));
+        const char* a0 = kb + 16 * us * kRowBytes + (td >> 1) * 16 * kGroupSegs;
+        if constexpr (kCodes) {
+          return lds_tr8(a0 + v_at[td & 1][0]);
+        } else {
+          const uint2 x0 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][0]));
+          const uint2 x1 = lds_tr4(reinterpret_cast<const uint16_t*>(a0 + v_at[td & 1][1]));
+          return u32x4{x0.x, x0.y, x1.x, x1.y};
+        }
       };
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      bool again = true;
-      auto begin = [&]() __attribute__((always_inline)) {
-        pread(0);
+      const int4 which = *reinterpret_cast<const int4*>(outgrown);
+      pread(0);
 #pragma unroll
-        for (int k = 0; k < kAheadV; ++k) vr[k] = vread(k);
-      };
-      if constexpr (kAtOnce) {
-        const int4 which = *reinterpret_cast<const int4*>(outgrown);
-        begin();
-        again = __builtin_amdgcn_readfirstlane(which.x | which.y | which.z | which.w) != 0;
-      }
+      for (int k = 0; k < kAheadV; ++k) vr[k] = vread(k);
       // (the pins keep O in accumulation registers on the way around, else it is moved in every step)
       auto pin = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int td = 0; td < TD; ++td) asm volatile("" : "+a"(acc[td][0]), "+a"(acc[td][1]));
       };
-      if constexpr (kAtOnce) pin();
-      if (again) {
+      pin();
+      if (__builtin_amdgcn_readfirstlane(which.x | which.y | which.z | which.w) != 0) {
         float alpha[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -457,8 +429,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
             for (int j = 0; j < 2; ++j) acc[td][j] *= alpha[j];
           pin();
         }
-        if constexpr (kAtOnce) pread(0);
-        else begin();
+        pread(0);
       }
       l_run += sum;
       {
@@ -468,9 +439,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
           if (td == 0 && us + 1 < NU) pread(us + 1);
           if (k + kAheadV < NO) vr[k + kAheadV] = vread(k + kAheadV);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[td][j] = mfma32x32x16(vr[k], bp[us][j], acc[td][j]);
-          if constexpr (!kCodes)
-            if (k % 2 == 0 && kEarly + k / 2 < NC) get(next, buf ^ 1, kEarly + k / 2, piece, mixes);
+          for (int j = 0; j < 2; ++j) acc[td][j] = mfma32x32x16(widen_bf16x8(vr[k]), bp[us][j], acc[td][j]);
+          if (k % 2 == 0 && kEarly + k / 2 < NC) get(next, buf ^ 1, kEarly + k / 2, piece, mixes);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
