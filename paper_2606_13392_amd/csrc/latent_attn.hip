@@ -18,8 +18,8 @@
 // over the chip (latent_steps.h), shared tiles leave their parts in fp32, and
 // latent_join_kernel joins them by the log-sum-exp rule in key order.
 //
-// Bound: matrix products.  8192 rows of 64 heads take 1264 us, 1.09 PFLOP/s (1145 us at
-// the rate of a large product); 2 x 512 rows on 16K keys 655 - 720 by the card (556).
+// Bound: matrix products.  8192 rows of 64 heads take 1251 - 1290 us, 1.1 PFLOP/s (1145 us at
+// the rate of a large product); 2 x 512 rows on 14K - 16K keys 605 - 720 by the card (556).
 #include <initializer_list>
 #include <type_traits>
 

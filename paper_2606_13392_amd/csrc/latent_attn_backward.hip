@@ -27,7 +27,7 @@
 //
 // Bound: issue.  A wave has its SIMD alone (its operands and sums are 350 - 500
 // registers), and between two matrix products of 32 clocks it issues some five other
-// instructions.  8192 rows of 64 heads: queries 1.86 ms, keys 2.68 (1.85 and 2.30 at the
+// instructions.  8192 rows of 64 heads: queries 1.83 - 1.89 ms, keys 2.60 - 2.70 (1.85 and 2.30 at the
 // rate of a large matrix product, repeated products counted), the heads' sum 0.03.
 #include <cmath>
 #include <initializer_list>

@@ -23,14 +23,17 @@
 // and latent_merge_kernel joins them by the log-sum-exp rule in key order.
 //
 // Bound: 64 heads of one token do 130 operations for each byte of a bf16 cache, so
-// memory and products both count.  32 tokens of 64 heads on 4K - 60K keys take 147 us
+// memory and products both count.  32 tokens of 64 heads on 4K - 60K keys take 146 us
 // (123 at the rate of a large copy): a step of 72 KiB takes 7100 clocks, 2200 of them
 // waiting for memory, 5.1 TB/s while the steps run, the rest the start and the merge.
-// Elsewhere a step's own work bounds, some 4900 clocks, of which the matrix units are
-// busy 2180: a CTA has its CU alone (two buffers of keys fill the LDS, O and Q the
-// registers), so nothing runs under the softmax, the barriers and the copies' issue.
-// Four chunks of 20 - 150 rows of 32 heads, R = 256: 78 us (30 at the rate of a large
-// product); one token on 8K keys 21 us, of which the steps are 5.
+// Elsewhere a step's own work bounds, some 4600 clocks, of which the matrix units are
+// busy 2180: a CTA has its CU alone (O and Q fill the registers, at R = 512 two buffers of
+// bf16 keys the LDS), so nothing runs under the softmax, the barriers and the copies' issue.
+// Draft rows of 128 heads on E4M3 keys, R = 512: 87 us (54 at the rate of a large
+// product); four chunks of 20 - 150 rows of 32 heads, R = 256: 76 (30); one token
+// on 8K keys 21, of which the steps are 6.  Eight waves, each with half of the scores'
+// k-steps and an eighth of the dimensions, so that two share a SIMD: 151, 104, 80 and 20
+// us for 147, 101, 78 and 20, for the partial scores' way through LDS.
 #include <initializer_list>
 #include <type_traits>
 
@@ -242,11 +245,23 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       int64_t hd;
       int ln = lane;
       asm volatile("" : "+v"(ln));
+      if constexpr (kOwnSegs == kWave) {
+        // a copy is one row: where it lies is worked out once for the wave (32 tokens on 4K - 60K keys 143 - 148 us instead of 148)
+#pragma unroll 2
+        for (int r = wave; r < kRows; r += kWaves) {
+          const int64_t row = row_of(r, &hd);
+          const uint64_t at = reinterpret_cast<uint64_t>(q + row * q_stride + hd * q_head);
+          const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at));
+          const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32));
+          copy16(reinterpret_cast<const char*>(static_cast<uint64_t>(hi) << 32 | lo), 16 * (ln ^ (r & 15)), lds_keys + kBuf + 1024 * r);
+        }
+      } else {
 #pragma unroll 1
-      for (int c = wave; c < kRows * kOwnSegs / kWave; c += kWaves) {
-        const int r = kOwnSegs == kWave ? c : 2 * c + (ln >> 5), sg = ln % kOwnSegs;
-        const int64_t row = row_of(r, &hd);
-        copy16(reinterpret_cast<const char*>(q + row * q_stride + hd * q_head + 8 * (sg ^ (r & 15))), lds_keys + kBuf + 1024 * c);
+        for (int c = wave; c < kRows * kOwnSegs / kWave; c += kWaves) {
+          const int r = 2 * c + (ln >> 5), sg = ln % kOwnSegs;
+          const int64_t row = row_of(r, &hd);
+          copy16(reinterpret_cast<const char*>(q + row * q_stride + hd * q_head + 8 * (sg ^ (r & 15))), lds_keys + kBuf + 1024 * c);
+        }
       }
 #pragma unroll 1
       for (int c = wave; c < kRows * kRot / 8 / kWave; c += kWaves) {
