@@ -8,7 +8,7 @@
 //
 // Two kernels of one form, so that every sum has an order of its own and no
 // result depends on which CTA comes first: a wave keeps rows of one side as matrix
-// operands in registers (64 queries and dO, or 32 keys and values), the CTA streams
+// operands in registers (64 or 32 queries and dO, or 32 keys and values), the CTA streams
 // the other side 64 rows at a time through LDS, and a wave forms both score products
 // and adds the weights' products with the streamed rows, read down their columns.
 // What this repeats, the score products of the second kernel, is 20 of 72 matrix
@@ -102,18 +102,22 @@ struct Args {
   float scale, scale_log2;
 };
 
-// KEYS: keys are stationary, 32 to a wave, and queries streamed; else queries are
-// stationary, 64 to a wave, so that an operand read from LDS feeds two products
-// (the keys' sums leave no registers for that), and keys streamed.
-template <bool KEYS>
+// KEYS: keys are stationary, 32 to a wave (NT = 1), and queries streamed; else queries are
+// stationary, 32 NT to a wave, and keys streamed.  With 64 an operand read from LDS
+// feeds two products (the keys' sums leave no registers for that), with 32 a tile takes
+// little more than half the time and there are twice the CTAs.  Queries' kernel, 64 and 32 to a wave:
+// 1 x 512 rows, 8 heads (16 CTAs of 256 rows) 35 and 22 us, 1 x 2048, 20 (160) 107 and 70, 1 x 4096,
+// 16 (256) 226 and 171, 10 x 300, 20 (400) 60 and 48, documents of 300 - 3000 rows, 32 (928) 241 and 245.
+constexpr int64_t kFewTiles = 768;
+template <bool KEYS, int NT>
 __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, msa_seqs sq, flash::Grid gr) {
   constexpr int KO = kDim / 16, KS = (kDim + kRot) / 16;
   constexpr int ND = KS / 2;                       // 32-dimension tiles of own and shared part
   constexpr int NA = KEYS ? ND + kDim / 32 : ND;   // accumulator tiles
-  constexpr int NT = KEYS ? 1 : 2;                 // 32-row tiles of stationary rows per wave
+  constexpr bool kRoomy = NT == 1;                 // registers are left for addresses
   constexpr int kTileRows = 32 * NT * kWaves;
   constexpr int NK = 16 / kWaves, NR = 8 / kWaves; // copies of 1 KiB per wave: wide rows, half rows
-  constexpr int kAhead = KEYS ? 5 : 3;
+  constexpr int kAhead = kRoomy ? 5 : 3;
   __shared__ __align__(16) Tile ring[kRing];
   __shared__ __align__(16) uint4 stat[kRing][KEYS ? kRowsT : 1];      // of streamed queries
   const int lane = lane_id();
@@ -208,7 +212,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     f.dst_stat = lds_address(&stat[0][0]) + buf * static_cast<uint32_t>(sizeof(stat[0]));
     return f;
   };
-  // (KEYS) a lane's offsets are held, and formed again for the last tile alone
+  // Where registers are left a lane's offsets are held, and formed again for the last tile alone
   auto offset = [&](int c, int ln, int last) __attribute__((always_inline)) -> uint32_t {
     if (c < 2 * NK) {
       const int r = 4 * ((c >> 1) * kWaves + wave) + (ln >> 4);
@@ -218,9 +222,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     return c < kCopies ? min(r, last) * rot_s + 16 * ((ln & 7) ^ half_mix(r)) : 16 * min(ln, last);
   };
   constexpr int kAllCopies = kCopies + (KEYS ? 1 : 0);
-  uint32_t held[KEYS ? kAllCopies : 1];
+  uint32_t held[kRoomy ? kAllCopies : 1];
   auto hold = [&](int last) __attribute__((always_inline)) {
-    if constexpr (KEYS)
+    if constexpr (kRoomy)
 #pragma unroll
       for (int c = 0; c < kAllCopies; ++c) {
         held[c] = offset(c, lane, last);
@@ -228,7 +232,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
       }
   };
   auto copy_piece = [&](const From& f, int c, int ln) __attribute__((always_inline)) {
-    const uint32_t at = KEYS ? held[KEYS ? c : 0] : offset(c, ln, f.last);
+    const uint32_t at = kRoomy ? held[kRoomy ? c : 0] : offset(c, ln, f.last);
     if (c < 2 * NK) {
       if (c & 1) copy16(f.other, at, f.dst + kOtherAt + 1024 * kWaves * (c >> 1));
       else copy16(f.own, at, f.dst + kOwnAt + 1024 * kWaves * (c >> 1));
@@ -288,8 +292,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   }
 
   // ------------------------------------------------ operand addresses
-  // (KEYS) each held, from the start of the ring; else formed from the first where they are read: no register is left
-  constexpr int kWideAt = KEYS ? KO : 1, kHalfAt = KEYS ? kRot / 16 : 1;
+  // Where registers are left each is held, from the start of the ring; else formed from the first where they are read: no register is left
+  constexpr int kWideAt = kRoomy ? KO : 1, kHalfAt = kRoomy ? kRot / 16 : 1;
   uint32_t row_own[kWideAt], row_rot[kHalfAt], col_own[kWideAt], col_rot[kHalfAt];
   {
     // transposed operand: in each 16-lane group, lane j addresses row k0 + j/4, dims n0 + 4(j%4) .. +3 and
@@ -307,9 +311,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
       col_rot[j] = (rl * 2 * kRot + 16 * (seg ^ half_mix(rl)) + 8 * (jj & 1)) ^ (64 * (j >> 1) + 16 * (j & 1));
     }
   }
-  // (KEYS) the rows', the columns' addresses on to another buffer
+  // the rows', the columns' addresses on to another buffer, where they are held
   auto move = [&](uint32_t (&wide)[kWideAt], uint32_t (&half)[kHalfAt], int from, int to) __attribute__((always_inline)) {
-    if constexpr (KEYS) {
+    if constexpr (kRoomy) {
       const int by = (to - from) * static_cast<int>(sizeof(Tile));
 #pragma unroll
       for (int j = 0; j < kWideAt; ++j) {
@@ -337,15 +341,15 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
 
   // a statistic's three parts are elements 0 .. 2 of the lanes h = 0
   const bf16x8 ones = __builtin_bit_cast(bf16x8, h == 0 ? make_uint4(0x3F803F80u, 0x3F80u, 0, 0) : make_uint4(0, 0, 0, 0));
-  // (KEYS) Each phase reads the first kAhead operands of the next in its last slots, where these are there: the reads'
+  // (Roomy) Each phase reads the first kAhead operands of the next in its last slots, where these are there: the reads'
   // time is bare else.  (Of the queries' kernel, with products enough, it takes 3 % more time.)
   bf16x8 pre[kAhead];
   // operands of the products of rows 32 half .. + 31, and of the additions of those rows
   auto read_row = [&](int buf, int half, int j) __attribute__((always_inline)) -> bf16x8 {
-    const char* t = reinterpret_cast<const char*>(&ring[KEYS ? 0 : buf]);
+    const char* t = reinterpret_cast<const char*>(&ring[kRoomy ? 0 : buf]);
     const int k = j < KS ? j : j - KS;             // 16 dimensions; KO .. KS - 1 of the shared part
     uint32_t at;
-    if constexpr (KEYS) {
+    if constexpr (kRoomy) {
       at = k < KO ? row_own[k < KO ? k : 0] : row_rot[k < KO ? 0 : k - KO];
     } else {
       at = (k < KO ? row_own[0] : row_rot[0]) ^ 32 * (k < KO ? k : k - KO);
@@ -354,13 +358,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     return ld_bf16x8(reinterpret_cast<const uint16_t*>(t + at));
   };
   auto read_col = [&](int buf, int half, int j) __attribute__((always_inline)) -> bf16x8 {
-    const char* t = reinterpret_cast<const char*>(&ring[KEYS ? 0 : buf]);
+    const char* t = reinterpret_cast<const char*>(&ring[kRoomy ? 0 : buf]);
     const int u = j / NA, i = j % NA;              // 16 streamed rows, accumulator tile
     const int r = 32 * half + 16 * u;
     const bool wide = i < KO / 2 || i >= ND;
     const int k = i < KO / 2 ? i : i < ND ? i - KO / 2 : i - ND;
     uint32_t at0, at1;
-    if constexpr (KEYS) {
+    if constexpr (kRoomy) {
       at0 = wide ? col_own[wide ? 2 * k : 0] : col_rot[wide ? 0 : 2 * k];
       at1 = wide ? col_own[wide ? 2 * k + 1 : 0] : col_rot[wide ? 0 : 2 * k + 1];
     } else {
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   };
   // both score products of streamed rows 32 half .. + 31: lane (n, h) gets rows 8(i/4) + 4h + i%4 against its own
   auto products = [&](int buf, int half, f32x16 (&z)[NT], f32x16 (&dz)[NT], auto beside) __attribute__((always_inline)) {
-    if constexpr (!KEYS) asm volatile("" : "+v"(row_own[0]), "+v"(row_rot[0]));    // as above
+    if constexpr (!kRoomy) asm volatile("" : "+v"(row_own[0]), "+v"(row_rot[0]));    // as above
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) z[nt] = dz[nt] = f32x16{};
     if constexpr (KEYS) {
@@ -382,7 +386,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     }
     bf16x8 op[KS + KO];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) op[j] = KEYS ? pre[j] : read_row(buf, half, j);
+    for (int j = 0; j < kAhead; ++j) op[j] = kRoomy ? pre[j] : read_row(buf, half, j);
 #pragma unroll
     for (int j = 0; j < KS + KO; ++j) {
       if (j + kAhead < KS + KO) op[j + kAhead] = read_row(buf, half, j + kAhead);
@@ -398,10 +402,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
   // adds the pending weights' products with their streamed rows; beside(j) after the j-th slot
   constexpr int kSlots = 2 * NA;
   auto additions = [&](int buf, int half, auto beside) __attribute__((always_inline)) {
-    if constexpr (!KEYS) asm volatile("" : "+v"(col_own[0]), "+v"(col_rot[0]));    // as above
+    if constexpr (!kRoomy) asm volatile("" : "+v"(col_own[0]), "+v"(col_rot[0]));    // as above
     bf16x8 op[kSlots];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) op[j] = KEYS ? pre[j] : read_col(buf, half, j);
+    for (int j = 0; j < kAhead; ++j) op[j] = kRoomy ? pre[j] : read_col(buf, half, j);
 #pragma unroll
     for (int j = 0; j < kSlots; ++j) {
       if (j + kAhead < kSlots) op[j + kAhead] = read_col(buf, half, j + kAhead);
@@ -491,10 +495,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
     f32x16 z[NT], dz[NT];
     // the first operands of the products, of the additions that come next: behind slot j of j_end
     auto rows_next = [&](int buf, int half, int j, int j_end) __attribute__((always_inline)) {
-      if (KEYS && j >= j_end - kAhead) pre[j - (j_end - kAhead)] = read_row(buf, half, j - (j_end - kAhead));
+      if (kRoomy && j >= j_end - kAhead) pre[j - (j_end - kAhead)] = read_row(buf, half, j - (j_end - kAhead));
     };
     auto cols_next = [&](int buf, int half, int j, int j_end) __attribute__((always_inline)) {
-      if (KEYS && j >= j_end - kAhead) pre[j - (j_end - kAhead)] = read_col(buf, half, j - (j_end - kAhead));
+      if (kRoomy && j >= j_end - kAhead) pre[j - (j_end - kAhead)] = read_col(buf, half, j - (j_end - kAhead));
     };
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) rows_next(0, 0, j, kAhead);
@@ -732,14 +736,16 @@ extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t
   a.scale_log2 = softmax_scale * kLog2E;
   if (std::fabs(a.scale_log2) < kLeast) a.scale_log2 = kLeast;
   int64_t tiles;
-  const flash::Grid gr = flash::plan_grid(seqs, kRowTile, seqs->max_q_rows, &tiles);
+  flash::Grid gr = flash::plan_grid(seqs, kRowTile, seqs->max_q_rows, &tiles);
+  const bool few = tiles * H < kFewTiles;
+  if (few) gr = flash::plan_grid(seqs, kRowTile / 2, seqs->max_q_rows, &tiles);
   const int64_t key_tiles = seqs->num_seqs == 1 ? (std::min<int64_t>(seqs->max_kv_len, N) + kKeyTile - 1) / kKeyTile
                                                 : N / kKeyTile + seqs->num_seqs;
   if (std::max(tiles, key_tiles) * H >= (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;     // a grid's limit
   if (T > 0)
-    msa_prof::launch("latent_backward_q_kernel", latent_backward_kernel<false>, dim3(static_cast<unsigned>(tiles * H)),
-                     dim3(kThreads), 0, stream, a, *seqs, gr);
-  msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true>,
+    msa_prof::launch("latent_backward_q_kernel", few ? latent_backward_kernel<false, 1> : latent_backward_kernel<false, 2>,
+                     dim3(static_cast<unsigned>(tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
+  msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true, 1>,
                    dim3(static_cast<unsigned>(key_tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
   msa_prof::launch("latent_sum_kernel", latent_sum_kernel, dim3(static_cast<unsigned>(std::min((N + 3) / 4, kSumCtas))), dim3(256), 0, stream,
                    static_cast<const float*>(a.d_r), *seqs, H, softmax_scale, dkv, static_cast<uint16_t*>(d_k_rope),

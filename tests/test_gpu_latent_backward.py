@@ -35,6 +35,8 @@ CASES = [
     ("few_on_many", [3], [700], 2, 0),
     ("many_heads", [20, 33], [20, 40], 64, 0),
     ("70_sequences", [1 + 3 * i % 20 for i in range(70)], [1 + 3 * i % 20 + i % 7 for i in range(70)], 2, 1),
+    # so many tiles that a wave takes 64 queries, in one of them several tiles long
+    ("long_among_many", [700, 300] + [2] * 385, [700, 500] + [2] * 385, 2, 0),
     # none, one and several tiles of keys each, some sequences without rows
     ("600_sequences", [i % 3 for i in range(600)], [i % 3 + (130 * (i % 17 == 0)) for i in range(600)], 2, 1),
 ]
