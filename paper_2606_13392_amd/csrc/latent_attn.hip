@@ -91,13 +91,17 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void latent_attn_kernel(
   auto k_row = [&](int c) { return 4 * (c * WAVES + wave) + (lane >> 4); };
   auto s_row = [&](int c) { return 8 * (c * WAVES + wave) + (lane >> 3); };
   uint32_t koff[NK], voff[NK], roff[NR];
+  // offsets of a sub-block's pieces; keys past row `last` repeat it: their values are finite, their weight zero
+  auto hold_k = [&](int last) __attribute__((always_inline)) {
 #pragma unroll
-  for (int c = 0; c < NK; ++c) {
-    koff[c] = k_row(c) * kv_row + 16 * k_seg(k_row(c), lane & 15);
-    voff[c] = k_row(c) * kv_row + 2 * kDim + 16 * v_seg(k_row(c), lane & 15);
-  }
+    for (int c = 0; c < NK; ++c) koff[c] = min(k_row(c), last) * kv_row + 16 * k_seg(k_row(c), lane & 15);
 #pragma unroll
-  for (int c = 0; c < NR; ++c) roff[c] = s_row(c) * r_row + 16 * r_seg(s_row(c), lane & 7);
+    for (int c = 0; c < NR; ++c) roff[c] = min(s_row(c), last) * r_row + 16 * r_seg(s_row(c), lane & 7);
+  };
+  auto hold_v = [&](int last) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < NK; ++c) voff[c] = min(k_row(c), last) * kv_row + 2 * kDim + 16 * v_seg(k_row(c), lane & 15);
+  };
   const uint32_t lds_k = lds_address(ring.k[0]), lds_v = lds_address(ring.v[0]), lds_r = lds_address(ring.r[0]);
   // MFMA operand reads, relative to a buffer
   uint32_t ks_at[KO], rs_at[KS - KO], vs_at[kDim / 32];
@@ -146,27 +150,25 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void latent_attn_kernel(
       const int64_t first = seq_geom(sq, s).kv_start;
       const char* kb = reinterpret_cast<const char*>(kv + (first * H + hd) * kPair);
       const char* rb = reinterpret_cast<const char*>(kr + first * kr_stride);
-      // keys past the sequence's end repeat its last one: their values are finite, their weight zero
-      auto copy_k = [&](int b, int buf) {
+      // The offsets are formed again for the sequence's last sub-block alone, where it is not full.
+      hold_k(kKeys - 1);
+      hold_v(kKeys - 1);
+      auto copy_k = [&](int b, int buf) __attribute__((always_inline)) {
         const char* src = kb + static_cast<int64_t>(b) * kKeys * kv_row;
         const char* rsrc = rb + static_cast<int64_t>(b) * kKeys * r_row;
         const int last = g.kv_len - 1 - b * kKeys;
+        if (last < kKeys - 1) hold_k(last);
 #pragma unroll
-        for (int c = 0; c < NK; ++c)
-          copy16(src, last >= kKeys - 1 ? koff[c] : min(k_row(c), last) * kv_row + 16 * k_seg(k_row(c), lane & 15),
-                 lds_k + buf * 2 * kKeys * kDim + 1024 * (c * WAVES + wave));
+        for (int c = 0; c < NK; ++c) copy16(src, koff[c], lds_k + buf * 2 * kKeys * kDim + 1024 * (c * WAVES + wave));
 #pragma unroll
-        for (int c = 0; c < NR; ++c)
-          copy16(rsrc, last >= kKeys - 1 ? roff[c] : min(s_row(c), last) * r_row + 16 * r_seg(s_row(c), lane & 7),
-                 lds_r + buf * 2 * kKeys * kRot + 1024 * (c * WAVES + wave));
+        for (int c = 0; c < NR; ++c) copy16(rsrc, roff[c], lds_r + buf * 2 * kKeys * kRot + 1024 * (c * WAVES + wave));
       };
-      auto copy_v = [&](int b, int buf) {
+      auto copy_v = [&](int b, int buf) __attribute__((always_inline)) {
         const char* src = kb + static_cast<int64_t>(b) * kKeys * kv_row;
         const int last = g.kv_len - 1 - b * kKeys;
+        if (last < kKeys - 1) hold_v(last);
 #pragma unroll
-        for (int c = 0; c < NK; ++c)
-          copy16(src, last >= kKeys - 1 ? voff[c] : min(k_row(c), last) * kv_row + 2 * kDim + 16 * v_seg(k_row(c), lane & 15),
-                 lds_v + buf * 2 * kKeys * kDim + 1024 * (c * WAVES + wave));
+        for (int c = 0; c < NK; ++c) copy16(src, voff[c], lds_v + buf * 2 * kKeys * kDim + 1024 * (c * WAVES + wave));
       };
       bf16x8 bq[KS];                              // the query rows, as the B operand of S^T
 
