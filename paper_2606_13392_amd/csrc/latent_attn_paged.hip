@@ -32,8 +32,9 @@
 // Draft rows of 128 heads on E4M3 keys, R = 512: 87 us (54 at the rate of a large
 // product); four chunks of 20 - 150 rows of 32 heads, R = 256: 76 (30); one token
 // on 8K keys 21, of which the steps are 6.  Eight waves, each with half of the scores'
-// k-steps and an eighth of the dimensions, so that two share a SIMD: 151, 104, 80 and 20
-// us for 147, 101, 78 and 20, for the partial scores' way through LDS.
+// k-steps and an eighth of the dimensions, so that two share a SIMD, take 151, 104, 80 and
+// 20 us for these four's kernels, four 147, 101, 78 and 20 (before the codes lay in LDS):
+// the partial scores' way through LDS.
 #include <initializer_list>
 #include <type_traits>
 
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
       asm volatile("" : "+v"(ln));
       if constexpr (kOwnSegs == kWave) {
         // a copy is one row: where it lies is worked out once for the wave (32 tokens on 4K - 60K keys 143 - 148 us instead of 148)
-#pragma unroll 2
+#pragma unroll 1
         for (int r = wave; r < kRows; r += kWaves) {
           const int64_t row = row_of(r, &hd);
           const uint64_t at = reinterpret_cast<uint64_t>(q + row * q_stride + hd * q_head);
