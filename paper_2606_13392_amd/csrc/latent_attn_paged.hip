@@ -22,7 +22,7 @@
 // device.  Where a tile is shared by several CTAs each leaves its part in fp32,
 // and latent_merge_kernel joins them by the log-sum-exp rule in key order.
 //
-// Bound: 64 heads of one token do 130 operations for each byte of a bf16 cache, so
+// Bound: 64 heads of one token do 121 operations for each byte of a bf16 cache, so
 // memory and products both count.  32 tokens of 64 heads on 4K - 60K keys take 146 us
 // (123 at the rate of a large copy): a step of 72 KiB takes 7100 clocks, 2200 of them
 // waiting for memory, 5.1 TB/s while the steps run, the rest the start and the merge.
