@@ -461,7 +461,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
         }
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the buffers' readers are done
+    // The buffers' readers are done, and every wave's copies, those behind the tile's last step among them, have landed:
+    // the next tile's queries may go where another wave's were still under way, and no wave ends with one.
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
     // ------------------------------------------------ the tile's rows, or the share's part of them
     l_run += xor32f(l_run);
