@@ -668,13 +668,6 @@ struct WaveBuf {
 };
 static_assert(sizeof(WaveBuf) >= 32 * kRedStride * sizeof(float), "joined rows do not fit");
 
-// Orders a wave's own LDS accesses (they complete in issue order; this keeps
-// the compiler from moving them across).
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 template <typename T, bool SMALL>
 __global__ __launch_bounds__(kRowWaves* kWave, 1) void paged_rows_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, msa_seqs sq, Plan pl, Parts parts, int H_q,

@@ -608,6 +608,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_backward_kernel(Args a, ms
       for (int i = KO / 2; i < ND; ++i) lay(acc[i][nt], a.scale, row, i - KO / 2, true, area + kWide);
     }
   }
+  wave_lds_order();                                // a lane stores what other lanes laid down
   leave(KEYS ? a.d_k : a.d_q, false, area);
   if constexpr (KEYS) {
     leave(a.d_v, false, area + kWide);

@@ -110,6 +110,13 @@ __device__ __forceinline__ uint64_t readlane_u64(uint64_t v, int lane) {
   return (static_cast<uint64_t>(hi) << 32) | lo;
 }
 
+// Orders a wave's own LDS accesses (they complete in issue order; this keeps
+// the compiler from moving them across).
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Value of lane (lane ^ J), all in the vector ALU: DPP quad permutes for J = 1,
 // 2, a half-row mirror and a quad mirror for 4, a row rotation for 8, permlane
 // swaps for 16 and 32.

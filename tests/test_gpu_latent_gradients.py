@@ -1,0 +1,65 @@
+"""msa_latent_attn_backward: gradients in every layout that its strides allow, and long sequences."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2606_13392_amd import msa
+from tests.latent_util import ROT
+from tests.test_gpu_latent_backward import check, make, run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    msa.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+def joint(T, H, pad):
+    """A head's own and rotated part side by side, ``pad`` elements behind them."""
+    t = torch.full((T, H, 128 + ROT + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+    return t, t[..., :128], t[..., 128:128 + ROT]
+
+
+def heads_first(T, H, pad):
+    own = torch.full((H, T, 128 + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+    rot = torch.full((H, T, ROT + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+    return (own, rot), own[..., :128].transpose(0, 1), rot[..., :ROT].transpose(0, 1)
+
+
+@pytest.mark.parametrize("many", [False, True], ids=["32_a_wave", "64_a_wave"])
+@pytest.mark.parametrize("layout,pad", [(joint, 0), (joint, 8), (heads_first, 0), (heads_first, 8)],
+                         ids=["joint", "joint_padded", "heads_first", "heads_first_padded"])
+def test_strides(layout, pad, many):
+    """Inputs and gradients in other layouts: the bits of contiguous ones, and nothing written beside them."""
+    q_rows, kv_lens = ([300, 1, 40] + [2] * 300, [300, 7, 170] + [2] * 300) if many else ([70, 1, 130], [70, 7, 200])
+    b, o, lse = make(("strides", q_rows, kv_lens, 3, 1))
+    T, n = b.n + 1, b.n
+    want = run(b, o, lse)
+    _, q, e = layout(T, 3, pad)
+    q.copy_(b.dq)
+    e.copy_(b.dq_rope)
+    whole, d_q, d_e = layout(T, 3, 4 if pad else 0)         # rows that are 8 bytes aligned alone
+    wide = torch.full((b.N, ROT + 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = msa.latent_attn_backward(q, e, b.dkv, b.dk_rope.contiguous(), o, lse, b.d_o_dev, b.seqs, d_q=d_q, d_q_rope=d_e,
+                                   d_k_rope=wide[:, 1:])    # 2 bytes aligned
+    for x, y in zip(got[:2], want[:2]):
+        assert torch.equal(x[:n], y[:n]) and bool((x[n:] == 7.0).all())
+    assert torch.equal(got[2], want[2]) and torch.equal(got[3], want[3])
+    assert bool((wide[:, 0] == 7.0).all())
+    if pad:
+        beside = (whole[..., 128 + ROT:],) if layout is joint else (whole[0][..., 128:], whole[1][..., ROT:])
+        assert all(bool((x == 7.0).all()) for x in beside)
+
+
+@pytest.mark.parametrize("case", [("long_prompt", [1500], [1500], 1, 0), ("long_chunk", [600], [1900], 1, 0),
+                                  # so many tiles that a wave takes 64 queries
+                                  ("long_among_many", [1500] + [2] * 780, [1500] + [2] * 780, 1, 0)], ids=lambda c: c[0])
+def test_long(case):
+    b, o, lse = make(case)
+    check(b, o, lse, run(b, o, lse))
