@@ -608,8 +608,9 @@ int msa_latent_attn(const void* q, int64_t q_stride, int64_t q_head_stride, cons
  *   d_kv       bf16 [total_kv_rows, num_heads, 256]   OUTPUT: dk, then dv
  *   d_k_rope   bf16 rows d_k_rope_stride elements apart, of 64 elements   OUTPUT
  *
- * Every key row is written (zeros where no query attends); query rows behind the last
- * sequence are left as they are and take no part.  P and dS are rounded to bf16 for
+ * Every key row is written (zeros where no query attends); a query row without a
+ * visible key gets zeros, also where there is no key row at all; query rows behind the
+ * last sequence are left as they are and take no part.  P and dS are rounded to bf16 for
  * the products, everything else is fp32 with one rounding of each result; the heads'
  * shares of d_k_rope are added in fp32 in the heads' order.  Every output is
  * bit-reproducible.  Key ranges of different sequences must not overlap (the

@@ -691,9 +691,9 @@ extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t
   if (st != MSA_OK) return st;
   const int H = num_heads;
   const int64_t T = seqs->total_q_rows, N = seqs->total_kv_rows;
-  if (N == 0) return MSA_OK;                           // then there are no rows either
+  if (N == 0 && T == 0) return MSA_OK;
   if (T > 0 && (!q || !q_rope || !o || !lse || !d_o || !d_q || !d_q_rope)) return MSA_ERR_INVALID;
-  if (!kv || !k_rope || !d_kv || !d_k_rope) return MSA_ERR_INVALID;
+  if (N > 0 && (!kv || !k_rope || !d_kv || !d_k_rope)) return MSA_ERR_INVALID;
   // rows and heads of the results do not overlap
   auto apart = [&](int64_t row, int64_t head, int dim) {
     if ((T > 1 && row < dim) || (H > 1 && head < dim)) return false;
@@ -746,10 +746,12 @@ extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t
   if (T > 0)
     msa_prof::launch("latent_backward_q_kernel", few ? latent_backward_kernel<false, 1> : latent_backward_kernel<false, 2>,
                      dim3(static_cast<unsigned>(tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
-  msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true, 1>,
-                   dim3(static_cast<unsigned>(key_tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
-  msa_prof::launch("latent_sum_kernel", latent_sum_kernel, dim3(static_cast<unsigned>(std::min((N + 3) / 4, kSumCtas))), dim3(256), 0, stream,
-                   static_cast<const float*>(a.d_r), *seqs, H, softmax_scale, dkv, static_cast<uint16_t*>(d_k_rope),
-                   d_k_rope_stride);
+  if (N > 0) {
+    msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true, 1>,
+                     dim3(static_cast<unsigned>(key_tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
+    msa_prof::launch("latent_sum_kernel", latent_sum_kernel, dim3(static_cast<unsigned>(std::min((N + 3) / 4, kSumCtas))), dim3(256), 0,
+                     stream, static_cast<const float*>(a.d_r), *seqs, H, softmax_scale, dkv, static_cast<uint16_t*>(d_k_rope),
+                     d_k_rope_stride);
+  }
   return msa_host::launch_status();
 }

@@ -63,3 +63,15 @@ def test_strides(layout, pad, many):
 def test_long(case):
     b, o, lse = make(case)
     check(b, o, lse, run(b, o, lse))
+
+
+def test_no_key_rows():
+    """Query rows and a key side of no rows: O and the queries' gradients are zeros, as for other rows without a key."""
+    T, H = 70, 3
+    seqs = msa.Seqs([60, 10], [60, 10], [0, 0], 0, "cuda")
+    t = lambda *s: torch.ones(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    q, e, d_o, kv, k_rope = t(T, H, 128), t(T, H, ROT), t(T, H, 128), t(0, H, 256), t(0, ROT)
+    o, lse = msa.latent_attn(q, e, kv, k_rope, seqs, out=t(T, H, 128))
+    assert bool((o == 0).all()) and bool((lse == -float("inf")).all())
+    d_q, d_e, d_kv, d_r = msa.latent_attn_backward(q, e, kv, k_rope, o, lse, d_o, seqs, d_q=t(T, H, 128), d_q_rope=t(T, H, ROT))
+    assert bool((d_q == 0).all()) and bool((d_e == 0).all()) and d_kv.numel() == d_r.numel() == 0

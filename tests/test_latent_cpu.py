@@ -278,3 +278,10 @@ def test_gradients_refuse_more_ctas_than_a_grid_has():
     n = 1 << 20
     seqs = _seqs(num_seqs=n, total_q_rows=n, max_q_rows=1, total_kv_rows=n, max_kv_len=1)
     assert _backward(_expanded(seqs=seqs, H=32, dqs=4096, des=2048)) == UNS
+
+
+@pytest.mark.parametrize("kw,want", [(dict(dq=None), INV), (dict(de=None), INV), (dict(d_o=None), INV), (dict(ws=None), WS)])
+def test_gradients_of_rows_without_a_key_side(kw, want):
+    """Query rows and no key row at all: no tensor of the key side, all of the others."""
+    a = dict(seqs=_seqs(total_kv_rows=0), kv=None, r=None, dkv=None, dr=None)
+    assert _backward(_expanded(**{**a, **kw})) == want
