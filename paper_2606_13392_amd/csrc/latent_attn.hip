@@ -493,6 +493,10 @@ int validate_expanded(const msa_seqs* seqs, int H) {
 // heads 1282 / 1296 / 1380; 20 documents of 100 - 1000 rows, 32 heads 81 / 66 / 113;
 // 2 x 512 rows on 16K keys, 64 heads 666 / 698 / 709, on 14 - 16K (another card) 720 /
 // - / 756; 2 x 500 on 8K, 20 heads 245 / 183 / 125; 64 on 12K, 8 heads 207 / 226 / 33.
+// Beyond 128 heads a head would have one share, which splits nothing and runs its tiles one behind another: 8 x 32
+// rows on 2K, 129 heads 251 / 220 / 352, 3 x 256 on 16K, 136 heads 1132 / 1265 / 1354.  Where the heads do not divide 256
+// fewer CTAs run, each faster for it, so the cost stays one of the whole chip: 2 x 200 on 8K, 100 heads (200
+// CTAs) 265 / 304 / 267, of which 299 / 272 / 241 are told here, and 303 for the shares' CTAs counted.
 constexpr double kShareStep = 1.07;
 ExpandedPlan plan_of(const msa_seqs* seqs, int H, int* waves, int64_t* ctas) {
   const double rows = seqs->max_q_rows, keys = seqs->max_kv_len, seq_count = seqs->num_seqs;
@@ -517,10 +521,11 @@ ExpandedPlan plan_of(const msa_seqs* seqs, int H, int* waves, int64_t* ctas) {
   // (shares have the last tiles' live waves alone to pay for)
   const double filled = std::min(u8, (seqs->total_q_rows / 32 + seq_count) / 8 * H);
   const double shares = filled / kHeld * avg * (rows >= 256 ? 2.66 : t8) * kShareStep * mean + 18;
+  const int ranges = kHeld / H;            // shares per head
   ExpandedPlan pl{};
   *waves = 8;
-  if (H <= kHeld && shares < std::min(whole8, whole4)) {
-    pl.ranges = std::max(1, kHeld / H);
+  if (ranges > 1 && shares < std::min(whole8, whole4)) {
+    pl.ranges = ranges;
     pl.min_steps = kMinSteps;
     *ctas = static_cast<int64_t>(pl.ranges) * H;
     return pl;

@@ -285,3 +285,11 @@ def test_gradients_of_rows_without_a_key_side(kw, want):
     """Query rows and no key row at all: no tensor of the key side, all of the others."""
     a = dict(seqs=_seqs(total_kv_rows=0), kv=None, r=None, dkv=None, dr=None)
     assert _backward(_expanded(**{**a, **kw})) == want
+
+
+@pytest.mark.parametrize("heads", [129, 136, 160, 200, 256])
+@pytest.mark.parametrize("num,rows,keys", [(3, 256, 16384), (8, 32, 2048), (1, 64, 4096), (2, 64, 8192), (4, 1, 60000)])
+def test_one_share_per_head_is_none(heads, num, rows, keys):
+    """Beyond 128 heads the steps of a head's tiles would be one CTA's, one tile behind another: each tile has a CTA instead."""
+    seqs = _seqs(num_seqs=num, total_q_rows=num * rows, max_q_rows=rows, total_kv_rows=num * keys, max_kv_len=keys)
+    assert msa.lib().msa_latent_attn_workspace_size(ctypes.byref(seqs), heads) == 0
