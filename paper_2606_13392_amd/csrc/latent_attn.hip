@@ -583,7 +583,8 @@ extern "C" int msa_latent_attn(const void* q, int64_t q_stride, int64_t q_head_s
   const flash::LogitScale scale = flash::logit_scale(softmax_scale * kLog2E);
   auto run = [&](auto count) {
     constexpr int W = decltype(count)::value;
-    msa_prof::launch("latent_attn_kernel", latent_attn_kernel<W>, dim3(static_cast<unsigned>(ctas)), dim3(W * kWave), 0, stream,
+    msa_prof::launch(W == 8 ? "latent_attn_kernel" : "latent_attn_narrow_kernel", latent_attn_kernel<W>,
+                     dim3(static_cast<unsigned>(ctas)), dim3(W * kWave), 0, stream,
                      static_cast<const uint16_t*>(q), q_stride, q_head_stride, static_cast<const uint16_t*>(q_rope),
                      q_rope_stride, q_rope_head_stride, static_cast<const uint16_t*>(kv), static_cast<const uint16_t*>(k_rope),
                      k_rope_stride, *seqs, pl, parts, num_heads, scale.log2, scale.q_flip, static_cast<uint16_t*>(o), lse);

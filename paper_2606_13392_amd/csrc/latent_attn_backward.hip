@@ -744,7 +744,8 @@ extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t
                                                 : N / kKeyTile + seqs->num_seqs;
   if (std::max(tiles, key_tiles) * H >= (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;     // a grid's limit
   if (T > 0)
-    msa_prof::launch("latent_backward_q_kernel", few ? latent_backward_kernel<false, 1> : latent_backward_kernel<false, 2>,
+    msa_prof::launch(few ? "latent_backward_q_narrow_kernel" : "latent_backward_q_kernel",
+                     few ? latent_backward_kernel<false, 1> : latent_backward_kernel<false, 2>,
                      dim3(static_cast<unsigned>(tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
   if (N > 0) {
     msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true, 1>,
