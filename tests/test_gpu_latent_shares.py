@@ -65,3 +65,33 @@ def test_shares_that_go_on_after_an_odd_number_of_steps(heads, steps, R, fp8):
     for _ in range(3):
         o2, l2 = call(b)
         assert torch.equal(o, o2) and torch.equal(lse, l2)
+
+
+# name, q_rows, kv_lens, heads, latent, page
+MANY_TILES = [
+    ("three_rows_a_tile", [400, 250], [900, 260], 20, 256, 64),          # 134 and 84 tiles
+    ("five_rows_a_tile", [700], [700], 12, 512, 16),                     # 140
+    ("six_rows_a_tile", [3, 900], [300, 1500], 10, 256, 128),            # 150
+    ("nine_rows_a_tile", [1200, 1, 600], [1300, 70, 600], 7, 256, 32),   # 134 and 67
+]
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("case", MANY_TILES, ids=[c[0] for c in MANY_TILES])
+def test_tiles_beyond_a_period(case, fp8):
+    """Steps of tiles whose rows are no power of two repeat after 64 tiles; sequences of more tiles than that."""
+    name, q_rows, kv_lens, H, R, page = case
+    assert max(-(-q // (64 // H)) for q in q_rows) > 128
+    b = PagedBatch(name, q_rows, kv_lens, H, R, page, 0, fp8)
+    o, lse = call(b)
+    assert bool(torch.isfinite(o).all()) and bool(torch.isfinite(lse).all())
+    b.check(o, lse, np.arange(0, b.n, 2), name)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("H,R", [(200, 512), (600, 512), (1000, 256), (1024, 512)])
+def test_many_head_blocks(H, R, fp8):
+    """4, 10 and 16 blocks of heads, the last of them smaller or not."""
+    b = PagedBatch(f"blocks_{H}", [1, 2, 1], [700, 130, 1], H, R, 64, 0, fp8)
+    o, lse = call(b)
+    b.check(o, lse, np.arange(b.n), "blocks")
