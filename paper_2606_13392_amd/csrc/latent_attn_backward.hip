@@ -740,19 +740,21 @@ extern "C" int msa_latent_attn_backward(const void* q, int64_t q_stride, int64_t
   flash::Grid gr = flash::plan_grid(seqs, kRowTile, seqs->max_q_rows, &tiles);
   const bool few = tiles * H < kFewTiles;
   if (few) gr = flash::plan_grid(seqs, kRowTile / 2, seqs->max_q_rows, &tiles);
-  const int64_t key_tiles = seqs->num_seqs == 1 ? (std::min<int64_t>(seqs->max_kv_len, N) + kKeyTile - 1) / kKeyTile
-                                                : N / kKeyTile + seqs->num_seqs;
+  // none where no sequence has a key: the rows that there are get zeros all the same
+  const int64_t key_tiles = N == 0                ? 0
+                            : seqs->num_seqs == 1 ? (std::min<int64_t>(seqs->max_kv_len, N) + kKeyTile - 1) / kKeyTile
+                                                  : N / kKeyTile + seqs->num_seqs;
   if (std::max(tiles, key_tiles) * H >= (int64_t(1) << 24)) return MSA_ERR_UNSUPPORTED;     // a grid's limit
   if (T > 0)
     msa_prof::launch(few ? "latent_backward_q_narrow_kernel" : "latent_backward_q_kernel",
                      few ? latent_backward_kernel<false, 1> : latent_backward_kernel<false, 2>,
                      dim3(static_cast<unsigned>(tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
-  if (N > 0) {
+  if (key_tiles > 0)
     msa_prof::launch("latent_backward_kv_kernel", latent_backward_kernel<true, 1>,
                      dim3(static_cast<unsigned>(key_tiles * H)), dim3(kThreads), 0, stream, a, *seqs, gr);
+  if (N > 0)
     msa_prof::launch("latent_sum_kernel", latent_sum_kernel, dim3(static_cast<unsigned>(std::min((N + 3) / 4, kSumCtas))), dim3(256), 0,
                      stream, static_cast<const float*>(a.d_r), *seqs, H, softmax_scale, dkv, static_cast<uint16_t*>(d_k_rope),
                      d_k_rope_stride);
-  }
   return msa_host::launch_status();
 }

@@ -75,3 +75,14 @@ def test_no_key_rows():
     assert bool((o == 0).all()) and bool((lse == -float("inf")).all())
     d_q, d_e, d_kv, d_r = msa.latent_attn_backward(q, e, kv, k_rope, o, lse, d_o, seqs, d_q=t(T, H, 128), d_q_rope=t(T, H, ROT))
     assert bool((d_q == 0).all()) and bool((d_e == 0).all()) and d_kv.numel() == d_r.numel() == 0
+
+
+@pytest.mark.parametrize("sequences", [1, 3])
+def test_sequences_without_keys(sequences):
+    """No sequence has a key, but the key side has rows: they get zeros."""
+    seqs = msa.Seqs([0] * sequences, [0] * sequences, [5] * sequences, 60, "cuda")
+    t = lambda *s: torch.ones(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    d_kv, d_r = t(60, 4, 256), t(60, ROT)
+    msa.latent_attn_backward(t(0, 4, 128), t(0, 4, ROT), t(60, 4, 256), t(60, ROT), t(0, 4, 128), torch.ones((0, 4), device="cuda"),
+                             t(0, 4, 128), seqs, d_kv=d_kv, d_k_rope=d_r)
+    assert bool((d_kv == 0).all()) and bool((d_r == 0).all())
