@@ -613,8 +613,9 @@ int msa_latent_attn(const void* q, int64_t q_stride, int64_t q_head_stride, cons
  * last sequence are left as they are and take no part.  P and dS are rounded to bf16 for
  * the products, everything else is fp32 with one rounding of each result; the heads'
  * shares of d_k_rope are added in fp32 in the heads' order.  Every output is
- * bit-reproducible.  Key ranges of different sequences must not overlap (the
- * gradients of shared rows are unspecified).  No output may alias an input.
+ * bit-reproducible.  Key ranges of different sequences must not overlap (the call
+ * cannot tell; d_kv and d_k_rope are then unspecified, of other rows too).  No output
+ * may alias an input.
  *
  * Supported: as msa_latent_attn, with total_kv_rows * num_heads < 2^31, (the larger of
  * total_q_rows / 256 and total_kv_rows / 128, + num_seqs) num_heads < 2^24, q_stride,
