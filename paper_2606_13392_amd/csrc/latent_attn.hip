@@ -18,8 +18,8 @@
 // over the chip (latent_steps.h), shared tiles leave their parts in fp32, and
 // latent_join_kernel joins them by the log-sum-exp rule in key order.
 //
-// Bound: matrix products.  8192 rows of 64 heads take 1251 - 1290 us, 1.1 PFLOP/s (1145 us at
-// the rate of a large product); 2 x 512 rows on 14K - 16K keys 605 - 720 by the card (556).
+// Bound: matrix products.  8192 rows of 64 heads take 1226 - 1290 us, 1.1 PFLOP/s (1145 us at
+// the rate of a large product); 2 x 512 rows on 14K - 16K keys 602 - 720 by the card (556).
 #include <initializer_list>
 #include <type_traits>
 
@@ -47,8 +47,8 @@ using steps::tile_geom;
 constexpr int kRot = 64;                 // elements of the shared key part
 constexpr int kPair = 2 * kDim;          // a key's own part and its values
 constexpr float kSlack = 8.f;
-// Steps per share, where there are few.  2 x 100 rows of 8 heads on 3000 keys, kernel and join with their launches:
-// 28.5 us with 2, 28.0 with 4, 29.7 with 8.
+// Steps per share, where there are few.  2 x 100 rows of 8 heads on 3000 keys, kernel and join in a graph: 24.9 us with
+// 2, 24.3 with 4, 26.1 with 8.
 constexpr int kMinSteps = 4;
 constexpr int kHeld = 256;               // CTAs of 8 waves that the chip holds
 

@@ -27,10 +27,14 @@
 // (123 at the rate of a large copy): a step of 72 KiB takes 7100 clocks, 2200 of them
 // waiting for memory, 5.1 TB/s while the steps run, the rest the start and the merge.
 // Elsewhere a step's own work bounds, some 4600 clocks, of which the matrix units are
-// busy 2180: a CTA has its CU alone (O and Q fill the registers, at R = 512 two buffers of
-// bf16 keys the LDS), so nothing runs under the softmax, the barriers and the copies' issue.
+// busy 2180 (R = 256: 1150): a CTA has its CU alone, so nothing runs under the softmax, the
+// barriers and the copies' issue.  At R = 512 that cannot be otherwise in this form: O and Q take
+// 494 - 510 of 512 registers, two buffers of bf16 keys 153 of 160 KiB.  At R = 256 it can:
+// 300 registers and 89 KiB (codes 69) leave room for a third buffer, or for more waves on other
+// rows, which has not been tried.
 // Draft rows of 128 heads on E4M3 keys, R = 512: 87 us (54 at the rate of a large
-// product); four chunks of 20 - 150 rows of 32 heads, R = 256: 76 (30); one token
+// product); four chunks of 20 - 150 rows of 32 heads, R = 256: 76, on E4M3 70 (30); the 32
+// tokens on E4M3 114 - 118 (64), of R = 256 91 (68); one token
 // on 8K keys 21, of which the steps are 6.  Eight waves, each with half of the scores'
 // k-steps and an eighth of the dimensions, so that two share a SIMD, take 151, 104, 80 and
 // 20 us for these four's kernels, four 147, 101, 78 and 20 (before the codes lay in LDS):
@@ -60,11 +64,12 @@ constexpr int kRot = 64;                 // elements of the shared rotated part
 constexpr int kRows = 64;                // (row, head) pairs per tile
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-constexpr int kCtas = 256;               // one per CU: two buffers of keys fill its LDS
-// The merge of 32 tokens on 4K - 60K keys takes 17.3 us with 256 CTAs, 13.1 with 1024, 13.2 with 4096.
+constexpr int kCtas = 256;               // one per CU: at R = 512 it fills the registers and the LDS
+// The merge of 32 tokens on 4K - 60K keys takes 15.7 us with 256 CTAs, 11.3 with 1024, 11.0 with 4096; of four chunks
+// of 32 heads, R = 256, 10.9, 7.6 and 8.2.
 constexpr int kMergeCtas = 1024;
-// Steps per CTA, where there are few.  One token of 64 heads on 8K keys, kernel and merge with their launches: 31.5 us
-// with 1 (the merge has twice the parts), 28.0 with 2, 28.7 with 4.
+// Steps per CTA, where there are few.  One token of 64 heads on 8K keys, kernel and merge: 21.0 + 6.9 us with 1 (the
+// merge has twice the parts), 18.4 + 5.3 with 2, 19.8 + 4.3 with 4.
 constexpr int kMinSteps = 2;
 constexpr float kSlack = 8.f;            // see the maxima below
 constexpr int kAheadK = 6, kAheadV = 3;  // LDS operands requested so many products ahead
@@ -524,8 +529,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_paged_kernel(
 // list of such tiles and takes every gridDim.x-th share of them.  Of many tiles a
 // wave joins the parts of a piece, 4 dimensions of 32 rows in each half of it; of
 // few the CTA's four waves have every fourth part, in order, and join in LDS.  One
-// tile of 65 parts takes 7.8 us by the second way and 11.9 by the first, 8 sequences'
-// draft rows of 128 heads (16 tiles and more) 16.0 and 11.1, 32 tokens 17.7 and 13.0.
+// tile of 65 parts takes 5.3 us by the second way and 9.3 by the first, 8 sequences'
+// draft rows of 128 heads (16 tiles and more) 13.8 and 9.0, 32 tokens 15.7 and 11.3.
 constexpr int kManyTiles = 16;
 template <int R>
 __global__ __launch_bounds__(kThreads) void latent_merge_kernel(msa_seqs sq, LatentPlan pl, LatentParts parts, int H,
