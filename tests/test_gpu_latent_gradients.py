@@ -86,3 +86,22 @@ def test_sequences_without_keys(sequences):
     msa.latent_attn_backward(t(0, 4, 128), t(0, 4, ROT), t(60, 4, 256), t(60, ROT), t(0, 4, 128), torch.ones((0, 4), device="cuda"),
                              t(0, 4, 128), seqs, d_kv=d_kv, d_k_rope=d_r)
     assert bool((d_kv == 0).all()) and bool((d_r == 0).all())
+
+
+def test_keys_past_4_gib():
+    """Key rows, and gradients of them, whose bytes lie past 2^32 of their tensors: the bits of the same rows in a small one."""
+    H, rows, keys = 64, 140000, 300                         # 32 KiB each: 4.6 GB, and 2.3 GB of workspace
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs 20 GB")
+    b, o, lse = make(("past", [100], [keys], H, 0))
+    want = run(b, o, lse)
+    kv = torch.empty((rows, H, 256), dtype=torch.bfloat16, device="cuda")
+    k_rope = torch.empty((rows, ROT), dtype=torch.bfloat16, device="cuda")
+    at, first = rows - keys - 10, b.lay.kv_starts[0]
+    kv[at:at + keys], k_rope[at:at + keys] = b.dkv[first:first + keys], b.dk_rope[first:first + keys]
+    d_kv = torch.full_like(kv, 7.0)
+    got = msa.latent_attn_backward(b.dq, b.dq_rope, kv, k_rope, o, lse, b.d_o_dev, msa.Seqs([100], [keys], [at], rows, "cuda"), d_kv=d_kv)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for x, y in zip(got[2:], want[2:]):
+        assert torch.equal(x[at:at + keys], y[first:first + keys])
+        assert bool((x[:at] == 0).all()) and bool((x[at + keys:] == 0).all())
